@@ -441,6 +441,84 @@ cogdl_status cogdl_act_decompress(int64_t n, int32_t F, int32_t bits, int32_t gr
                                   cogdl_dtype out_dtype, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits (beside the codec above: bytes instead of
+ * bit planes, nearest instead of stochastic rounding, in a form that
+ * cogdl_grouped_linear_backward multiplies as it stands).  Each row of the
+ * n x F array A (fp32 / bf16 / fp16) is cut into blocks of COGDL_CKPT_BLOCK
+ * consecutive features (the last one may be shorter).  With M the block's
+ * largest magnitude, its exponent byte is
+ *     b = clamp(biased_exponent(bits_fp32(M) + 2^16) - 6, lo, hi)
+ * lo, hi = 1, 248 (fp16: 103, 136), its step s = 2^(b - 127), and feature x
+ * has the code q = clamp(round_to_nearest_even(x / s), -127, 127); a decoded
+ * value is q * s, within s / 2 of x, s <= M / 63.75 (blocks past 127.5 steps of
+ * hi saturate; values under half the step of lo become 0).  q * s is a bf16
+ * without rounding, and from fp16 activations an fp16.  A block with a value
+ * that is not finite gets b = 255 and codes 0 and decodes to NaN.
+ * codes: int8, n x F; exps: uint8, n x ceil(F / COGDL_CKPT_BLOCK).
+ * cogdl_act_restore rounds decoded values to out_dtype (to nearest even).
+ * F >= 1.
+ * ---------------------------------------------------------------------- */
+#define COGDL_CKPT_BLOCK 32
+
+cogdl_status cogdl_act_checkpoint(int64_t n, int32_t F, const void *A, cogdl_dtype a_dtype,
+                                  int8_t *codes, uint8_t *exps, hipStream_t stream);
+cogdl_status cogdl_act_restore(int64_t n, int32_t F, const int8_t *codes, const uint8_t *exps,
+                               void *out, cogdl_dtype out_dtype, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Dense layer with a weight matrix per group of rows (node types, relations,
+ * experts): cogdl_linear over rows that lie sorted by group.  Group g is the
+ * rows [offsets[g], offsets[g + 1]), and may have none:
+ *     Y[i, c] = act(sum_j X[i, j] * W[g, c, j] + bias[g, c]),  i in group g
+ * offsets: device int32, E + 1 entries, 0 <= offsets[0] <= ... <= offsets[E]
+ * <= n (read on the device; entries outside [0, n] count as its ends).  X: n x k,
+ * W: E x m x k, both bf16 or both fp16 (dtype); bias: fp32 E x m or NULL;
+ * Y: n x m of y_dtype.  fp32 accumulation on the matrix cores.  Rows outside
+ * [offsets[0], offsets[E]) belong to no group: Y keeps what it held there.
+ * codes and exps, both or neither: also write the 8-bit checkpoint of X that
+ * cogdl_act_checkpoint would (rows of no group: written or not), for the
+ * backward pass.  1 <= E <= COGDL_MAX_GROUPS, n < 2^31 (COGDL_ERR_TOO_LARGE
+ * past either).
+ * ---------------------------------------------------------------------- */
+#define COGDL_MAX_GROUPS 4096
+
+cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m,
+                                  const int32_t *offsets, const void *X, const void *W,
+                                  cogdl_dtype dtype, const float *bias, cogdl_act act, void *Y,
+                                  cogdl_dtype y_dtype, int8_t *codes, uint8_t *exps,
+                                  hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Gradients of cogdl_grouped_linear (with one group, of cogdl_linear) for
+ * dY = dL/dY, n x m of dtype.  With dZ = dY * act'(Y), where the activation's
+ * slope follows from its output Y (n x m of dtype; ReLU Y > 0, ELU 1 where
+ * Y > 0 and Y + 1 elsewhere; NULL for COGDL_ACT_NONE):
+ *   dX[i, j]    = sum_c dZ[i, c] * W[g, c, j]            (n x k of dtype)
+ *   dW[g, c, j] = sum_{i in group g} dZ[i, c] * X[i, j]  (E x m x k, fp32 or dtype)
+ *   db[g, c]    = sum_{i in group g} dZ[i, c]            (E x m fp32)
+ * The input comes as X (n x k of dtype) or as its checkpoint (codes and exps),
+ * exactly one of them where dW is asked for; the checkpoint's values enter the
+ * products as they are (a checkpoint of bf16 or fp32 activations read in fp16
+ * is rounded to it).  dX, dW and db may each be NULL (not computed; W is then
+ * not needed for dX, nor X for dW).  Groups of no rows get dW = 0 and db = 0;
+ * rows of no group keep what dX held there.  The products take dZ rounded to
+ * dtype (exact without an activation and for ReLU); db sums it unrounded.
+ * fp32 accumulation, in a fixed order.  workspace: device scratch for partial
+ * sums, at least the size that cogdl_grouped_linear_backward_workspace reports
+ * (0 for few rows: NULL is then accepted), 16-byte aligned; its contents are
+ * clobbered, and calls in flight together need one each.
+ * ---------------------------------------------------------------------- */
+cogdl_status cogdl_grouped_linear_backward_workspace(int64_t n, int32_t E, int32_t k, int32_t m,
+                                                     size_t *bytes);
+cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int32_t m,
+                                           const int32_t *offsets, const void *dY, const void *W,
+                                           const void *X, const int8_t *codes,
+                                           const uint8_t *exps, cogdl_dtype dtype, const void *Y,
+                                           cogdl_act act, void *dX, void *dW,
+                                           cogdl_dtype dw_dtype, float *db, void *workspace,
+                                           size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Dot-product SDDMM -- section 2.2, T = A (.) (P Q^T), per head: for every
  * edge k = (i, col[k]) and head h
  *     out[k * H + h] = sum_d P[i, h, d] * Q[col[k], h, d]

@@ -14,6 +14,10 @@ fallback.
     gat_aggregate(rowptr, col, s_dst, s_src, X, slope, ...)       -> Y [n, H, D] (, alpha)
     sddmm_dot(rowptr, col, P, Q)                                  -> <P[i,h], Q[j,h]> per edge
     gat_backward(rowptr, col, colptr, row_t, perm, ..., dY)       -> dX, dalpha, dscore, ds_dst, ds_src
+    linear(X, W, bias, act)                                       -> Y = act(X W^T + b)
+    grouped_linear(X, W, offsets, bias, act, save=False)          -> Y, rows of group g by W[g] (, checkpoint of X)
+    grouped_linear_backward(dY, W, offsets, X | codes, exps, ...) -> dX, dW, db
+    act_checkpoint(A) / act_restore(codes, exps)                  -> activations in 8 bits and back
     Plan(rowptr, nnz, max_feat, max_heads, mode, group_size)      -> the workload balancer
 """
 from __future__ import annotations
@@ -80,6 +84,13 @@ def lib():
     L.cogdl_act_codec_size.argtypes = [i64, i32, i32, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     L.cogdl_act_compress.argtypes = [i64, i32, P, ctypes.c_int, i32, i32, ctypes.c_uint64, P, P, P]
     L.cogdl_act_decompress.argtypes = [i64, i32, i32, i32, P, P, P, ctypes.c_int, P]
+    L.cogdl_act_checkpoint.argtypes = [i64, i32, P, ctypes.c_int, P, P, P]
+    L.cogdl_act_restore.argtypes = [i64, i32, P, P, P, ctypes.c_int, P]
+    L.cogdl_grouped_linear.argtypes = [i64, i32, i32, i32, P, P, P, ctypes.c_int, P, ctypes.c_int, P,
+                                       ctypes.c_int, P, P, P]
+    L.cogdl_grouped_linear_backward_workspace.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
+    L.cogdl_grouped_linear_backward.argtypes = [i64, i32, i32, i32, P, P, P, P, P, P, ctypes.c_int, P,
+                                                ctypes.c_int, P, P, ctypes.c_int, P, P, sz, P]
     L.cogdl_spmm_t.argtypes = [i32, i32, i64, P, P, P, i32, P, ctypes.c_int, P, ctypes.c_int, P, P]
     L.cogdl_csr_to_csc_workspace.argtypes = [i32, i32, i64, ctypes.POINTER(sz)]
     L.cogdl_csr_to_csc.argtypes = [i32, i32, i64, P, P, P, P, P, P, P, P, sz, P]
@@ -105,7 +116,8 @@ def lib():
                  "cogdl_gat_aggregate_act", "cogdl_gat_aggregate_proj", "cogdl_gat_aggregate_stats",
                  "cogdl_linear",
                  "cogdl_head_scores", "cogdl_act_codec_size", "cogdl_act_compress",
-                 "cogdl_act_decompress"):
+                 "cogdl_act_decompress", "cogdl_act_checkpoint", "cogdl_act_restore", "cogdl_grouped_linear",
+                 "cogdl_grouped_linear_backward_workspace", "cogdl_grouped_linear_backward"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -876,3 +888,183 @@ def act_decompress(codes, stats, n: int, F: int, bits: int, group: int, out_dtyp
     _check(lib().cogdl_act_decompress(n, F, bits, group, _ptr(codes), _ptr(stats), _ptr(out),
                                       _dtype_code(out), _stream()), "cogdl_act_decompress")
     return out
+
+
+CKPT_BLOCK = 32        # COGDL_CKPT_BLOCK: features that share an exponent byte
+MAX_GROUPS = 4096      # COGDL_MAX_GROUPS
+
+
+def _on_device(*tensors):
+    """A context with the tensors' device current (they must share one)."""
+    import torch
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise CogdlError(f"the tensors lie on several devices: {sorted(map(str, devices))}")
+    return torch.cuda.device(devices.pop())
+
+
+def _ckpt_blocks(F):
+    return (F + CKPT_BLOCK - 1) // CKPT_BLOCK
+
+
+def act_checkpoint(A, codes=None, exps=None):
+    """The 8-bit checkpoint of activations A [n, F] (cogdl_act_checkpoint): returns (codes int8
+    [n, F], exps uint8 [n, ceil(F / 32)]).  Feature x of a block of 32 is kept as q * 2^(b - 127),
+    b its exponent byte, within half a step (at most 1/127.5 of the block's largest magnitude)."""
+    import torch
+    n, F = _dims(A, "A", 2)
+    if F < 1:
+        raise CogdlError("A needs at least one feature")
+    nb = _ckpt_blocks(F)
+    _numel(codes, "codes", n * F)
+    _numel(exps, "exps", n * nb)
+    _dev(A, "A")
+    dt = _dtype_code(A)
+    if codes is None:
+        codes = torch.empty((n, F), dtype=torch.int8, device=A.device)
+    if exps is None:
+        exps = torch.empty((n, nb), dtype=torch.uint8, device=A.device)
+    _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
+    with _on_device(A, codes, exps):
+        _check(lib().cogdl_act_checkpoint(n, F, _ptr(A), dt, _ptr(codes), _ptr(exps), _stream()),
+               "cogdl_act_checkpoint")
+    return codes, exps
+
+
+def act_restore(codes, exps, out_dtype=None, out=None):
+    """The activations [n, F] that a checkpoint (act_checkpoint) stands for, in out_dtype (fp32 by
+    default; bf16 holds every value exactly, fp16 those of fp16 activations)."""
+    import torch
+    n, F = _dims(codes, "codes", 2)
+    if F < 1:
+        raise CogdlError("codes need at least one feature")
+    _numel(exps, "exps", n * _ckpt_blocks(F))
+    _numel(out, "out", n * F)
+    _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
+    if out is None:
+        out = torch.empty((n, F), dtype=out_dtype or torch.float32, device=codes.device)
+    _dev(out, "out")
+    with _on_device(codes, exps, out):
+        _check(lib().cogdl_act_restore(n, F, _ptr(codes), _ptr(exps), _ptr(out), _dtype_code(out), _stream()),
+               "cogdl_act_restore")
+    return out
+
+
+def _groups(W, offsets):
+    """(E, m, k) of grouped weights, with the offsets' size checked."""
+    E, m, k = _dims(W, "W", 3)
+    if E < 1 or E > MAX_GROUPS:
+        raise CogdlError(f"W has {E} groups, 1 to {MAX_GROUPS} are supported")
+    _dims(offsets, "offsets", 1)
+    _numel(offsets, "offsets", E + 1)
+    return E, m, k
+
+
+def grouped_linear(X, W, offsets, bias=None, act: str = "none", out_dtype=None, out=None, save: bool = False,
+                   codes=None, exps=None):
+    """linear() with a weight matrix per group of rows: Y[i] = act(X[i] W[g]^T + bias[g]) for the rows i
+    in [offsets[g], offsets[g + 1]) of group g (sorted node types, relations, experts; a group may have
+    none).  X [n, k] and W [E, m, k] both bf16 or both fp16; offsets int32 [E + 1] on the device; bias
+    fp32 [E, m] or None.  Rows before offsets[0] and from offsets[E] on belong to no group: ``out`` keeps
+    what it held there, a fresh output holds anything.  With ``save`` (or codes and exps given) returns
+    (Y, codes, exps), the 8-bit checkpoint of X for grouped_linear_backward."""
+    import torch
+    if act not in ACT:
+        raise ValueError(f"act must be one of {sorted(ACT)}")
+    n, k = _dims(X, "X", 2)
+    E, m, kw = _groups(W, offsets)
+    if kw != k or X.dtype != W.dtype:
+        raise CogdlError("X must be [n, k] and W [E, m, k] of the same dtype")
+    if (codes is None) != (exps is None):
+        raise CogdlError("give codes and exps together")
+    save = save or codes is not None
+    if save and k < 1:
+        raise CogdlError("X needs at least one feature to be saved")
+    _numel(bias, "bias", E * m)
+    _numel(out, "out", n * m)
+    _numel(codes, "codes", n * k)
+    _numel(exps, "exps", n * _ckpt_blocks(k))
+    _dev(X, "X"), _dev(W, "W"), _dev(offsets, "offsets", torch.int32), _dev(bias, "bias", torch.float32)
+    if out is None:
+        out = torch.empty((n, m), dtype=out_dtype or X.dtype, device=X.device)
+    if save and codes is None:
+        codes = torch.empty((n, k), dtype=torch.int8, device=X.device)
+        exps = torch.empty((n, _ckpt_blocks(k)), dtype=torch.uint8, device=X.device)
+    _dev(out, "out"), _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
+    with _on_device(X, W, offsets, bias, out, codes, exps):
+        _check(lib().cogdl_grouped_linear(n, E, k, m, _ptr(offsets), _ptr(X), _ptr(W), _dtype_code(X), _ptr(bias),
+                                          ACT[act], _ptr(out), _dtype_code(out), _ptr(codes), _ptr(exps),
+                                          _stream()), "cogdl_grouped_linear")
+    return (out, codes, exps) if save else out
+
+
+def grouped_linear_backward_workspace(n: int, E: int, k: int, m: int) -> int:
+    """Bytes of scratch that grouped_linear_backward takes for n rows and E groups of k features to m outputs."""
+    b = ctypes.c_size_t()
+    _check(lib().cogdl_grouped_linear_backward_workspace(n, E, k, m, ctypes.byref(b)),
+           "cogdl_grouped_linear_backward_workspace")
+    return b.value
+
+
+def grouped_linear_backward(dY, W, offsets, X=None, codes=None, exps=None, Y=None, act: str = "none",
+                            dw_dtype=None, out=None, workspace=None):
+    """Gradients of grouped_linear for dY = dL/dY [n, m]: returns dict(dX [n, k], dW [E, m, k], db fp32
+    [E, m]).  The input comes as X [n, k] or as its 8-bit checkpoint (codes, exps), which the products read
+    as it is.  With an activation, Y is the forward's output in dY's dtype.  dw_dtype: dY's dtype (default)
+    or fp32.  ``out`` may supply the tensors; a None among them leaves that gradient out.  Groups without
+    rows get zeros; rows of no group keep what dX held there (anything in a fresh one).  ``workspace``: at
+    least grouped_linear_backward_workspace bytes."""
+    import torch
+    if act not in ACT:
+        raise ValueError(f"act must be one of {sorted(ACT)}")
+    n, m = _dims(dY, "dY", 2)
+    E, mw, k = _groups(W, offsets)
+    if mw != m or dY.dtype != W.dtype:
+        raise CogdlError("dY must be [n, m] and W [E, m, k] of the same dtype")
+    o = dict(out or {})
+    sizes = {"dX": n * k, "dW": E * m * k, "db": E * m}
+    for name, t in o.items():
+        if name not in sizes:
+            raise CogdlError(f"unknown output {name!r}")
+        _numel(t, name, sizes[name])
+    if (codes is None) != (exps is None):
+        raise CogdlError("give codes and exps together")
+    if X is not None and codes is not None:
+        raise CogdlError("give X or its checkpoint (codes and exps), not both")
+    if o.get("dW", 0) is not None and X is None and codes is None:
+        raise CogdlError("dW needs X or its checkpoint (codes and exps)")
+    if X is not None and (_dims(X, "X", 2) != (n, k) or X.dtype != dY.dtype):
+        raise CogdlError(f"X must be [{n}, {k}] of dY's dtype")
+    if codes is not None and _dims(codes, "codes", 2) != (n, k):
+        raise CogdlError(f"codes must be [{n}, {k}], got {tuple(codes.shape)}")
+    _numel(exps, "exps", n * _ckpt_blocks(k))
+    if act == "none":
+        Y = None
+    elif Y is None:
+        raise CogdlError("the activation's gradient needs Y, the forward's output")
+    elif _dims(Y, "Y", 2) != (n, m) or Y.dtype != dY.dtype:
+        raise CogdlError(f"Y must be [{n}, {m}] of dY's dtype")
+    need = grouped_linear_backward_workspace(n, E, k, m)
+    if workspace is not None:
+        _at_least(workspace, "workspace", (need + workspace.element_size() - 1) // workspace.element_size())
+    _dev(dY, "dY"), _dev(W, "W"), _dev(offsets, "offsets", torch.int32), _dev(X, "X"), _dev(Y, "Y")
+    _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
+    dev = dY.device
+    if "dX" not in o:
+        o["dX"] = torch.empty((n, k), dtype=dY.dtype, device=dev)
+    if "dW" not in o:
+        o["dW"] = torch.empty((E, m, k), dtype=dw_dtype or dY.dtype, device=dev)
+    if "db" not in o:
+        o["db"] = torch.empty((E, m), dtype=torch.float32, device=dev)
+    dX, dW, db = o["dX"], o["dW"], o["db"]
+    _dev(dX, "dX", dY.dtype), _dev(dW, "dW"), _dev(db, "db", torch.float32)
+    if workspace is None and need > 0 and (dW is not None or db is not None):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _dev(workspace, "workspace")
+    with _on_device(dY, W, offsets, X, codes, exps, Y, dX, dW, db, workspace):
+        _check(lib().cogdl_grouped_linear_backward(
+            n, E, k, m, _ptr(offsets), _ptr(dY), _ptr(W), _ptr(X), _ptr(codes), _ptr(exps), _dtype_code(dY),
+            _ptr(Y), ACT[act], _ptr(dX), _ptr(dW), _dtype_code(dY if dW is None else dW), _ptr(db),
+            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+            _stream()), "cogdl_grouped_linear_backward")
+    return o

@@ -1,0 +1,60 @@
+// The 8-bit checkpoint format, shared by the kernels that write, read and multiply it.
+//
+// A block of kCkptBlock consecutive features of a row (the last block of a row may be
+// shorter) has one exponent byte b and an int8 code per feature; feature x is kept as
+// q 2^(b - 127).  With M the block's largest magnitude, b is the biased exponent of M
+// less 6, one more where M / 2^(b - 127) would round to 128, so |q| <= 127 and
+// |x - q s| <= s / 2 with s <= M / 63.75.  Powers of two keep both ways exact: x / s is
+// exact, so codes depend on nothing but x and M, and q s has 7 significant bits and is a
+// bf16 (from fp16 activations, an fp16) as it stands: a product reads a checkpoint at no
+// rounding of its own.  A block that holds a value that is not finite gets b = 255 and
+// codes 0, which decodes to NaN.
+#pragma once
+
+#include "common.hpp"
+
+namespace cogdl {
+
+constexpr int kCkptBlock = COGDL_CKPT_BLOCK;
+constexpr int kCkptBad = 255;
+
+// Bounds of the exponent byte: steps of the activations' own format at least (fp16
+// subnormals are multiples of 2^-24) and decoded values below its overflow at most
+// (127 2^121 in bf16 and fp32, 127 2^9 in fp16: larger blocks saturate at 127).
+template <typename T> struct CkptRange { static constexpr int lo = 1, hi = 248; };
+template <> struct CkptRange<f16_t> { static constexpr int lo = 103, hi = 136; };
+
+// The exponent byte of a block whose largest |x| has these fp32 bits.  Adding 2^16 carries
+// into the exponent exactly where M's mantissa is 1.9921875 or more (127.5 / 64).
+template <typename T>
+__device__ __forceinline__ int ckpt_exponent(uint32_t max_bits)
+{
+    if (max_bits >= 0x7f800000u) return kCkptBad;
+    const int b = (int)((max_bits + 0x10000u) >> 23) - 6;
+    return b < CkptRange<T>::lo ? CkptRange<T>::lo : (b > CkptRange<T>::hi ? CkptRange<T>::hi : b);
+}
+
+// 4 codes of 4 features, the first in the low byte; rs = 2^(127 - b), 0 for a bad block.
+__device__ __forceinline__ uint32_t ckpt_encode4(float a, float b, float c, float d, float rs)
+{
+    const auto one = [&](float x) {
+        return (uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(x * rs), -127.f, 127.f);
+    };
+    const uint32_t lo = __builtin_amdgcn_perm(one(b), one(a), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(one(d), one(c), 0x0c0c0400u);
+    return lo | (hi << 16);
+}
+
+// The 4 values of 4 codes (exact: 7 bits times a power of two).
+__device__ __forceinline__ void ckpt_decode4(uint32_t codes, float s, float (&v)[4])
+{
+    v[0] = (float)(int8_t)codes * s;
+    v[1] = (float)(int8_t)(codes >> 8) * s;
+    v[2] = (float)(int8_t)(codes >> 16) * s;
+    v[3] = (float)((int32_t)codes >> 24) * s;
+}
+
+// 2^(b - 127), infinite for the bad block, whose codes of 0 then give NaN.
+__device__ __forceinline__ float ckpt_scale(uint32_t b) { return __uint_as_float(b << 23); }
+
+}  // namespace cogdl
