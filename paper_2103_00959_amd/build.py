@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "libcogdl_mi355.so")
 # counter-calibration kernels (known traffic), a library of their own
 CALIB_LIB = os.path.join(HERE, "libcogdl_calib.so")
 CALIB_SOURCES = ["calib.hip"]
-SOURCES = ["primitives.hip", "plan.hip", "spmm.hip", "gspmm.hip", "gat.hip", "gat_proj.hip", "gat_bwd.hip", "dense.hip", "grouped.hip", "codec.hip",
+SOURCES = ["primitives.hip", "plan.hip", "spmm.hip", "gspmm.hip", "gat.hip", "gat_proj.hip", "gat_bwd.hip", "dense.hip", "grouped_rows.hip", "grouped_weights.hip", "codec.hip",
            "checkpoint.hip", "csc.hip", "trace.hip"]
 
 ARCH = "gfx950"

@@ -1,0 +1,209 @@
+// Products of rows that lie sorted by group (node types, relations, experts), each group
+// with a weight matrix of its own, and the gradient of their input:
+//     Y[i, c]  = act(sum_j X[i, j] W[g, c, j] + bias[g, c])        rows i of group g
+//     dX[i, j] = sum_c dZ[i, c] W[g, c, j]                          dZ = dY act'(Y)
+// The offsets stay on the device: the grid covers the most tiles that n rows in E groups can
+// have, and each workgroup finds its group by a scan of the group sizes.
+#include "grouped_tile.hpp"
+
+namespace cogdl {
+namespace {
+
+// WAVES wavefronts, TM rows by TN columns; DX: the gradient, A from SRC.
+template <typename T, int WAVES, int TM, int TN, bool DX, int SRC, int SRCB>
+__global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
+{
+    constexpr int N = WAVES * kWave;
+    constexpr int WAVES_C = TN >= 256 ? 4 : TN >= 128 ? 2 : 1, WAVES_R = WAVES / WAVES_C;
+    constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
+    extern __shared__ __align__(16) char lds[];
+    int64_t piece;
+    int tile;
+    tile_of(a.tiles_c, piece, tile);
+    Span s;
+    if (!find_span(a.off, a.E, a.n, TM, piece, s)) return;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
+    const int have = (int)(s.hi - s.lo);
+    const int wx = DX ? a.m : a.k;                      // x
+    const int wc = DX ? a.k : a.m;                      // outputs of a row
+    const int col0 = tile * TN;
+    const T *__restrict__ W = static_cast<const T *>(a.W) + (int64_t)s.g * a.m * a.k;
+    RowOperand<T, TM, N, SRC> A;
+    A.open(static_cast<const T *>(DX ? a.dY : a.X) + s.lo * wx,
+           SRC == kSloped ? static_cast<const T *>(a.Y) + s.lo * wx : nullptr, have, wx, a.act);
+    std::conditional_t<DX, ColOperand<T, TN, N, SRCB, false>, RowOperand<T, TN, N, SRCB>> B;
+    if constexpr (DX) B.open(W, nullptr, nullptr, nullptr, col0, a.k, a.m, 0);
+    else B.open(W + (int64_t)col0 * a.k, nullptr, a.m - col0 < TN ? a.m - col0 : TN, a.k, 0);
+    Acc<WR, WC> acc;
+    acc.clear();
+    multiply<T, TM, TN>(lds, A, B, wx, r0, c0, acc, [](const uint4 (&)[WR]) {});
+    // a lane's columns stay the same from row to row
+    float bias[8];
+    {
+        const float *__restrict__ p = !DX && a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
+        const int c = col0 + c0 + (int)(threadIdx.x % (4 * WC)) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bias[e] = p && c + e < wc ? p[c + e] : 0.f;
+    }
+    for_outputs<WR, WC>(lds, wave, acc, [&](int r, int c, float (&v)[8]) {
+        r += r0;
+        c += col0 + c0;
+        if (r >= have || c >= wc) return;
+        if constexpr (!DX) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = apply_act(v[e] + bias[e], a.act);
+        }
+        store8(a.out, a.out_dtype, (s.lo + r) * wc, c, wc, v);
+    });
+}
+
+struct Variant {
+    GroupedKernel kern;
+    int waves, tm, tn;
+};
+
+template <typename T, int WAVES, int TM, int TN>
+GroupedKernel pick(bool dx, bool act, bool direct)
+{
+    if (!dx) return direct ? k_grouped_rows<T, WAVES, TM, TN, false, kDirect, kDirect>
+                           : k_grouped_rows<T, WAVES, TM, TN, false, kStaged, kStaged>;
+    if (act) return direct ? k_grouped_rows<T, WAVES, TM, TN, true, kSloped, kDirect>
+                           : k_grouped_rows<T, WAVES, TM, TN, true, kSloped, kStaged>;
+    return direct ? k_grouped_rows<T, WAVES, TM, TN, true, kDirect, kDirect>
+                  : k_grouped_rows<T, WAVES, TM, TN, true, kStaged, kStaged>;
+}
+
+template <typename T>
+Variant pick_tile(int64_t n, int wc, bool dx, bool act, bool direct)
+{
+    if (wc > 128 && n >= 256 && direct && !act)
+        return {dx ? k_grouped_rows<T, 8, 256, 256, true, kDirect, kDirect>
+                   : k_grouped_rows<T, 8, 256, 256, false, kDirect, kDirect>, 8, 256, 256};
+    if (wc > 64) return {pick<T, 4, 128, 128>(dx, act, direct), 4, 128, 128};
+    return {pick<T, 4, 128, 64>(dx, act, direct), 4, 128, 64};
+}
+
+}  // namespace
+
+cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl_dtype dtype, hipStream_t stream)
+{
+    const bool act = dx && a.act != COGDL_ACT_NONE;
+    // direct loads: every row of both operands on the 16-byte grid
+    const bool direct = on_grid(dx ? a.dY : a.X, dx ? a.m : a.k) && on_grid(a.W, a.k);
+    const int wc = dx ? a.k : a.m;
+    const Variant v = dtype == COGDL_BF16 ? pick_tile<bf16_t>(a.n, wc, dx, act, direct)
+                                          : pick_tile<f16_t>(a.n, wc, dx, act, direct);
+    a.tiles_c = (int32_t)(((int64_t)wc + v.tn - 1) / v.tn);
+    const unsigned grid = piece_tiles(most_pieces(a.n, a.E, v.tm), a.tiles_c);
+    if (grid == 0) return COGDL_ERR_TOO_LARGE;
+    COGDL_LAUNCH_SHM(name, v.kern, grid, v.waves * kWave, (size_t)2 * (v.tm + v.tn) * kX * 2, stream, a);
+    return COGDL_OK;
+}
+
+}  // namespace cogdl
+
+using namespace cogdl;
+
+extern "C" {
+
+static cogdl_status check_grouped(int64_t n, int32_t E, int32_t k, int32_t m, const int32_t *offsets, int dtype)
+{
+    if (n < 0 || E < 1 || k < 0 || m < 0) return COGDL_ERR_INVALID;
+    if (dtype != COGDL_BF16 && dtype != COGDL_F16) return COGDL_ERR_DTYPE;
+    if (n > INT32_MAX || E > COGDL_MAX_GROUPS || k > kMaxWidth || m > kMaxWidth) return COGDL_ERR_TOO_LARGE;
+    if (!offsets) return COGDL_ERR_INVALID;
+    return COGDL_OK;
+}
+
+// A grid of the smallest tiles would not fit a launch: refused before anything runs.
+static bool too_many_tiles(int64_t n, int32_t E, int64_t wc)
+{
+    return piece_tiles(most_pieces(n, E, 128), (wc + 63) / 64) == 0;
+}
+
+cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m, const int32_t *offsets,
+                                  const void *X, const void *W, cogdl_dtype dtype, const float *bias,
+                                  cogdl_act act, void *Y, cogdl_dtype y_dtype, int8_t *codes, uint8_t *exps,
+                                  hipStream_t stream)
+{
+    const cogdl_status st = check_grouped(n, E, k, m, offsets, dtype);
+    if (st != COGDL_OK) return st;
+    if (act < COGDL_ACT_NONE || act > COGDL_ACT_ELU) return COGDL_ERR_INVALID;
+    if (!dtype_ok(y_dtype)) return COGDL_ERR_DTYPE;
+    if ((codes == nullptr) != (exps == nullptr)) return COGDL_ERR_INVALID;
+    if (n > 0 && m > 0 && !Y) return COGDL_ERR_INVALID;
+    if (n > 0 && k > 0 && !X) return COGDL_ERR_INVALID;
+    if (n > 0 && m > 0 && k > 0 && !W) return COGDL_ERR_INVALID;
+    if (n == 0) return COGDL_OK;
+    if (m > 0 && too_many_tiles(n, E, m)) return COGDL_ERR_TOO_LARGE;
+    if (codes && k > 0) {
+        const cogdl_status cs = cogdl_act_checkpoint(n, k, X, dtype, codes, exps, stream);
+        if (cs != COGDL_OK) return cs;
+    }
+    if (m == 0) return COGDL_OK;
+    GroupedArgs a{};
+    a.n = n; a.E = E; a.k = k; a.m = m;
+    a.off = offsets;
+    a.X = X; a.W = W;
+    a.bias = bias;
+    a.act = (int32_t)act;
+    a.out = Y;
+    a.out_dtype = (int32_t)y_dtype;
+    return grouped_rows_launch("grouped_linear", a, false, dtype, stream);
+}
+
+cogdl_status cogdl_grouped_linear_backward_workspace(int64_t n, int32_t E, int32_t k, int32_t m, size_t *bytes)
+{
+    if (n < 0 || E < 1 || k < 0 || m < 0 || !bytes) return COGDL_ERR_INVALID;
+    if (n > INT32_MAX || E > COGDL_MAX_GROUPS || k > kMaxWidth || m > kMaxWidth) return COGDL_ERR_TOO_LARGE;
+    const Chunks c = chunks_of(n, E, k, m);
+    *bytes = (size_t)c.slots * ((size_t)m * k + m) * sizeof(float);
+    return COGDL_OK;
+}
+
+cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int32_t m, const int32_t *offsets,
+                                           const void *dY, const void *W, const void *X, const int8_t *codes,
+                                           const uint8_t *exps, cogdl_dtype dtype, const void *Y, cogdl_act act,
+                                           void *dX, void *dW, cogdl_dtype dw_dtype, float *db, void *workspace,
+                                           size_t workspace_bytes, hipStream_t stream)
+{
+    const cogdl_status st = check_grouped(n, E, k, m, offsets, dtype);
+    if (st != COGDL_OK) return st;
+    if (act < COGDL_ACT_NONE || act > COGDL_ACT_ELU) return COGDL_ERR_INVALID;
+    if (dw_dtype != COGDL_F32 && dw_dtype != dtype) return COGDL_ERR_DTYPE;
+    const bool rows = n > 0 && m > 0;
+    if (rows && (dX || dW || db) && (!dY || (act != COGDL_ACT_NONE && !Y))) return COGDL_ERR_INVALID;
+    if (rows && k > 0 && dX && !W) return COGDL_ERR_INVALID;
+    if ((codes == nullptr) != (exps == nullptr)) return COGDL_ERR_INVALID;
+    if (rows && k > 0 && dW && (X != nullptr) == (codes != nullptr)) return COGDL_ERR_INVALID;
+    const Chunks c = chunks_of(n, E, k, m);
+    const size_t need = (size_t)c.slots * ((size_t)m * k + m) * sizeof(float);
+    const bool weights = (dW && k > 0 && m > 0) || (db && m > 0);
+    if (weights && need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < need))
+        return COGDL_ERR_INVALID;
+    if (n > 0 && dX && k > 0 && too_many_tiles(n, E, k)) return COGDL_ERR_TOO_LARGE;
+    if (n > 0 && weights && piece_tiles(most_pieces(n, E, c.per), (int64_t)((m + 63) / 64) * ((k + 64) / 64)) == 0)
+        return COGDL_ERR_TOO_LARGE;
+    GroupedArgs a{};
+    a.n = n; a.E = E; a.k = k; a.m = m;
+    a.off = offsets;
+    a.X = X; a.codes = codes; a.exps = exps;
+    a.W = W;
+    a.act = (int32_t)act;
+    a.dY = dY; a.Y = Y;
+    if (dX && n > 0 && k > 0) {
+        a.out = dX;
+        a.out_dtype = (int32_t)dtype;
+        const cogdl_status s = grouped_rows_launch("grouped_linear_dx", a, true, dtype, stream);
+        if (s != COGDL_OK) return s;
+    }
+    if (!weights) return COGDL_OK;
+    a.out = k > 0 ? dW : nullptr;
+    a.out_dtype = (int32_t)dw_dtype;
+    a.db = db;
+    a.part = static_cast<float *>(workspace);
+    return grouped_weights_launch(a, c, dtype, stream);
+}
+
+}  // extern "C"
