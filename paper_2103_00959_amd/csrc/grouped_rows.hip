@@ -9,7 +9,7 @@
 namespace cogdl {
 namespace {
 
-// WAVES wavefronts, TM rows by TN columns; DX: the gradient, A from SRC.
+// WAVES wavefronts, tiles of TM rows by TN columns; DX: the gradient.  The operands from SRC, SRCB.
 template <typename T, int WAVES, int TM, int TN, bool DX, int SRC, int SRCB>
 __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
 {
@@ -17,45 +17,46 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
     constexpr int WAVES_C = TN >= 256 ? 4 : TN >= 128 ? 2 : 1, WAVES_R = WAVES / WAVES_C;
     constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
     extern __shared__ __align__(16) char lds[];
-    int64_t piece;
-    int tile;
-    tile_of(a.tiles_c, piece, tile);
-    Span s;
-    if (!find_span(a.off, a.E, a.n, TM, piece, s)) return;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
-    const int have = (int)(s.hi - s.lo);
     const int wx = DX ? a.m : a.k;                      // x
     const int wc = DX ? a.k : a.m;                      // outputs of a row
-    const int col0 = tile * TN;
-    const T *__restrict__ W = static_cast<const T *>(a.W) + (int64_t)s.g * a.m * a.k;
+    Walk walk;
+    walk.start(a.off, a.E, a.n, TM, a.tiles_c, false);
     RowOperand<T, TM, N, SRC> A;
-    A.open(static_cast<const T *>(DX ? a.dY : a.X) + s.lo * wx,
-           SRC == kSloped ? static_cast<const T *>(a.Y) + s.lo * wx : nullptr, have, wx, a.act);
     std::conditional_t<DX, ColOperand<T, TN, N, SRCB, false>, RowOperand<T, TN, N, SRCB>> B;
-    if constexpr (DX) B.open(W, nullptr, nullptr, nullptr, col0, a.k, a.m, 0);
-    else B.open(W + (int64_t)col0 * a.k, nullptr, a.m - col0 < TN ? a.m - col0 : TN, a.k, 0);
-    Acc<WR, WC> acc;
-    acc.clear();
-    multiply<T, TM, TN>(lds, A, B, wx, r0, c0, acc, [](const uint4 (&)[WR]) {});
-    // a lane's columns stay the same from row to row
-    float bias[8];
-    {
-        const float *__restrict__ p = !DX && a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
-        const int c = col0 + c0 + (int)(threadIdx.x % (4 * WC)) * 8;
+    const auto open = [&](const Span &s) {
+        const T *__restrict__ W = static_cast<const T *>(a.W) + (int64_t)s.g * a.m * a.k;
+        const int col0 = s.tile * TN;
+        A.open(static_cast<const T *>(DX ? a.dY : a.X) + s.lo * wx,
+               SRC == kSloped ? static_cast<const T *>(a.Y) + s.lo * wx : nullptr, s.have, wx, a.act);
+        if constexpr (DX) B.open(W, nullptr, nullptr, nullptr, col0, a.k, a.m, 0, false);
+        else B.open(W + (int64_t)col0 * a.k, nullptr, a.m - col0 < TN ? a.m - col0 : TN, a.k, 0);
+        return wx;
+    };
+    char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
+    run_tiles<T, decltype(A), decltype(B), WR, WC>(
+        lds, walk, A, B, r0, c0, open, [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
+        [&](const Span &s, const Acc<WR, WC> &acc) {
+            const int col0 = s.tile * TN + c0;
+            const float *__restrict__ bias = !DX && a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
+            for_outputs<WR, WC>(mine, acc, [&](int r, int c, float (&v)[8]) {
+                r += r0;
+                c += col0;
+                if (r >= s.have || c >= wc) return;
+                if constexpr (!DX) {
+                    if (bias) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) bias[e] = p && c + e < wc ? p[c + e] : 0.f;
-    }
-    for_outputs<WR, WC>(lds, wave, acc, [&](int r, int c, float (&v)[8]) {
-        r += r0;
-        c += col0 + c0;
-        if (r >= have || c >= wc) return;
-        if constexpr (!DX) {
+                        for (int e = 0; e < 8; ++e) v[e] += bias[c + e < wc ? c + e : wc - 1];
+                    }
+                    if (a.act != COGDL_ACT_NONE) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = apply_act(v[e] + bias[e], a.act);
-        }
-        store8(a.out, a.out_dtype, (s.lo + r) * wc, c, wc, v);
-    });
+                        for (int e = 0; e < 8; ++e) v[e] = apply_act(v[e], a.act);
+                    }
+                }
+                store8(a.out, a.out_dtype, (s.lo + r) * wc, c, wc, v);
+            });
+        });
 }
 
 struct Variant {
@@ -64,14 +65,15 @@ struct Variant {
 };
 
 template <typename T, int WAVES, int TM, int TN>
-GroupedKernel pick(bool dx, bool act, bool direct)
+Variant pick(bool dx, bool act, bool direct)
 {
-    if (!dx) return direct ? k_grouped_rows<T, WAVES, TM, TN, false, kDirect, kDirect>
-                           : k_grouped_rows<T, WAVES, TM, TN, false, kStaged, kStaged>;
-    if (act) return direct ? k_grouped_rows<T, WAVES, TM, TN, true, kSloped, kDirect>
-                           : k_grouped_rows<T, WAVES, TM, TN, true, kSloped, kStaged>;
-    return direct ? k_grouped_rows<T, WAVES, TM, TN, true, kDirect, kDirect>
-                  : k_grouped_rows<T, WAVES, TM, TN, true, kStaged, kStaged>;
+    GroupedKernel k;
+    if (!dx) k = direct ? k_grouped_rows<T, WAVES, TM, TN, false, kDirect, kDirect>
+                        : k_grouped_rows<T, WAVES, TM, TN, false, kStaged, kStaged>;
+    else if (act) k = k_grouped_rows<T, WAVES, TM, TN, true, kSloped, kStaged>;
+    else k = direct ? k_grouped_rows<T, WAVES, TM, TN, true, kDirect, kDirect>
+                    : k_grouped_rows<T, WAVES, TM, TN, true, kStaged, kStaged>;
+    return {k, WAVES, TM, TN};
 }
 
 template <typename T>
@@ -80,8 +82,8 @@ Variant pick_tile(int64_t n, int wc, bool dx, bool act, bool direct)
     if (wc > 128 && n >= 256 && direct && !act)
         return {dx ? k_grouped_rows<T, 8, 256, 256, true, kDirect, kDirect>
                    : k_grouped_rows<T, 8, 256, 256, false, kDirect, kDirect>, 8, 256, 256};
-    if (wc > 64) return {pick<T, 4, 128, 128>(dx, act, direct), 4, 128, 128};
-    return {pick<T, 4, 128, 64>(dx, act, direct), 4, 128, 64};
+    if (wc > 64) return pick<T, 4, 128, 128>(dx, act, direct);
+    return pick<T, 4, 128, 64>(dx, act, direct);
 }
 
 }  // namespace
@@ -95,10 +97,7 @@ cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl
     const Variant v = dtype == COGDL_BF16 ? pick_tile<bf16_t>(a.n, wc, dx, act, direct)
                                           : pick_tile<f16_t>(a.n, wc, dx, act, direct);
     a.tiles_c = (int32_t)(((int64_t)wc + v.tn - 1) / v.tn);
-    const unsigned grid = piece_tiles(most_pieces(a.n, a.E, v.tm), a.tiles_c);
-    if (grid == 0) return COGDL_ERR_TOO_LARGE;
-    COGDL_LAUNCH_SHM(name, v.kern, grid, v.waves * kWave, (size_t)2 * (v.tm + v.tn) * kX * 2, stream, a);
-    return COGDL_OK;
+    return launch_tiles(name, v.kern, a, most_pieces(a.n, a.E, v.tm), v.waves, v.tm, v.tn, stream);
 }
 
 }  // namespace cogdl

@@ -1,14 +1,19 @@
 // The tile engine of the grouped products (grouped_rows.hip, grouped_weights.hip):
 // C[r, c] = sum_x A(r, x) B(c, x) for one tile of one group's outputs.
 //
-// A workgroup owns TM x TN outputs and walks x in chunks of 64.  Both operands' chunks lie in
-// LDS, twice: while the matrix cores work on one, the next is on its way, so a chunk costs
-// one barrier.  An operand lies in memory with x along its rows ("row" operands: X and W of
-// the forward, dZ of dX) or down its rows ("col" operands: W of dX, both of dW).  A row
-// operand's matrix fragments are 16-byte LDS reads, a col operand's the LDS reads that
-// transpose 4 x 16 elements.  Operands whose rows lie on the 16-byte grid go from memory to
-// LDS directly; the others, and those that are computed on the way (an activation's slope,
-// a decoded checkpoint), pass through registers.
+// A workgroup computes TM x TN outputs at a time and walks x in chunks of 64.  Both operands'
+// chunks lie in LDS, two of them: while the matrix cores work on one, the next is on its way.
+// An operand lies in memory with x along its rows ("row" operands: X and W of the forward, dZ of
+// dX) or down its rows ("col" operands: W of dX, both of dW).  A row operand's matrix fragments
+// are 16-byte LDS reads, a col operand's the LDS reads that transpose 4 x 16 elements.  Operands
+// whose rows all lie on the 16-byte grid go from memory to LDS directly; the others, and those
+// that are computed on the way (an activation's slope, a decoded checkpoint), pass through
+// registers.
+//
+// Workgroups are resident and take tile after tile: a tile's first chunk is loaded under the last
+// products of the tile before, whose stores drain under this one's.  (A workgroup a tile, on one
+// group of 32768 rows, 2048 -> 2048: 280 us, 70 a tile and compute unit, of which 17 were waits
+// for the start, the first chunk and the stores.)
 #pragma once
 
 #include "checkpoint.hpp"
@@ -17,7 +22,6 @@
 namespace cogdl {
 
 constexpr int kX = 64;           // x elements of a chunk
-constexpr int kPieces = kX / 8;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -37,15 +41,6 @@ __device__ __forceinline__ f32x16 mfma_32x32x16(uint4 a, uint4 b, f32x16 c)
 }
 
 // ---------------------------------------------------------------- groups
-// Rows [lo, hi) of group g: piece `local` of the pieces of `per` rows that the groups are
-// cut into, `count` pieces in this group, `slot` pieces of groups with several before it.
-struct Span {
-    int g;
-    int64_t lo, hi;
-    int local, count;
-    int64_t slot;
-};
-
 // Offsets as the kernels use them: inside [0, n], so that no contents of the device array
 // lead outside the operands.
 __device__ __forceinline__ int64_t offset_at(const int32_t *__restrict__ off, int e, int64_t n)
@@ -54,56 +49,148 @@ __device__ __forceinline__ int64_t offset_at(const int32_t *__restrict__ off, in
     return o < 0 ? 0 : (o < n ? o : n);
 }
 
-// Piece t of all pieces (false past the last one), found by one wavefront (uniform).
-__device__ __forceinline__ bool find_span(const int32_t *__restrict__ off, int E, int64_t n, int per, int64_t t,
-                                          Span &s)
-{
-    const int lane = lane_id();
-    int64_t slot = 0;
-    for (int base = 0; base < E; base += kWave) {
-        const int e = base + lane;
-        int64_t lo = 0, hi = 0;
+// A tile of the output: rows [lo, lo + have) of group g, which are piece `local` of the `count`
+// pieces of `per` rows that the group is cut into (`slot`: pieces of groups with several before
+// it), and column tile `tile`.
+struct Span {
+    int g, local, count, tile;
+    int have;
+    int64_t lo, slot;
+};
+
+// This workgroup's tiles, in order.  Tiles are numbered by piece and column tile, and each of
+// the 8 XCDs takes a run of them, its workgroups one after another: a group's pieces share its
+// weights in that XCD's L2, a piece's tiles its rows.  The runs hold equal numbers of tiles or,
+// where the time goes with the rows of a piece (dW), equal weights: a piece weighs its chunks of 64
+// rows and kTileWeight for its start and end.  A window of 64 groups is held, a group a lane;
+// every wavefront does the same.
+constexpr int kTileWeight = 3;
+
+struct Walk {
+    const int32_t *off;
+    int64_t n;
+    int E, per, tiles;
+    int base, total;             // the window's first group and its pieces
+    int64_t first, slots;        // pieces, and those of groups with several, before the window
+    int lo, size, pieces, before;       // a lane's group: place, rows, pieces, pieces up to and with it
+    uint32_t j, step, end;       // this workgroup's next tile, the way to the one after, its XCD's end
+
+    __device__ __forceinline__ int pieces_of(int e, int &at, int &rows) const
+    {
+        at = rows = 0;
         if (e < E) {
-            lo = offset_at(off, e, n);
-            hi = offset_at(off, e + 1, n);
+            const int64_t o = offset_at(off, e, n), next = offset_at(off, e + 1, n);
+            at = (int)o;
+            rows = next > o ? (int)(next - o) : 0;
         }
-        const int size = hi > lo ? (int)(hi - lo) : 0;
-        const int pieces = (int)(((int64_t)size + per - 1) / per);
-        const int before = wave_inclusive_scan(pieces);
-        const int total = __builtin_amdgcn_readlane(before, kWave - 1);
-        const int many = pieces > 1 ? pieces : 0;
-        const int many_before = wave_inclusive_scan(many);
-        if (t < total) {
-            const int l = __builtin_ctzll(__ballot((int64_t)before > t));
-            s.g = base + l;
-            s.count = __builtin_amdgcn_readlane(pieces, l);
-            s.local = (int)t - (__builtin_amdgcn_readlane(before, l) - s.count);
-            const int64_t first = __builtin_amdgcn_readlane((int)lo, l);
-            const int64_t end = first + __builtin_amdgcn_readlane(size, l);
-            s.lo = first + (int64_t)s.local * per;
-            s.hi = s.lo + per < end ? s.lo + per : end;
-            s.slot = slot + __builtin_amdgcn_readlane(many_before - many, l);
-            return true;
-        }
-        t -= total;
-        slot += __builtin_amdgcn_readlane(many_before, kWave - 1);
+        return (int)(((int64_t)rows + per - 1) / per);
     }
-    return false;
-}
+    __device__ __forceinline__ void window(int from)
+    {
+        base = from;
+        pieces = pieces_of(base + lane_id(), lo, size);
+        before = wave_inclusive_scan(pieces);
+        total = __builtin_amdgcn_readlane(before, kWave - 1);
+    }
+    // the first window, anew only where there are others
+    __device__ __forceinline__ void rewind()
+    {
+        first = slots = 0;
+        if (base != 0) window(0);
+    }
+    __device__ __forceinline__ int weight() const { return (size + kX - 1) / kX + kTileWeight * pieces; }
+
+    // The number of the tile at which `target` of the weights before it is reached.
+    __device__ __forceinline__ uint32_t tile_at(int64_t target)
+    {
+        rewind();
+        for (;;) {
+            const int w = weight();
+            const int upto = wave_inclusive_scan(w);
+            const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
+            if (target < all) {
+                const int l = __builtin_ctzll(__ballot((int64_t)upto > target));
+                const int each = (per + kX - 1) / kX + kTileWeight;
+                int rest = (int)target - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(w, l));
+                const int count = __builtin_amdgcn_readlane(pieces, l);
+                int piece = rest / each;
+                piece = piece < count ? piece : count - 1;
+                rest -= piece * each;
+                const int mine = piece < count - 1 ? each : __builtin_amdgcn_readlane(w, l) - piece * each;
+                const int64_t tile = (int64_t)rest * tiles / mine;
+                return (uint32_t)((first + __builtin_amdgcn_readlane(before, l) - count + piece) * tiles + tile);
+            }
+            target -= all;
+            first += total;
+            if (base + kWave >= E) return (uint32_t)(first * tiles);
+            window(base + kWave);
+        }
+    }
+    __device__ __forceinline__ void start(const int32_t *offsets, int groups, int64_t rows, int rows_a_piece, int col_tiles,
+                                          bool weighted)
+    {
+        off = offsets;
+        E = groups;
+        n = rows;
+        per = rows_a_piece;
+        tiles = col_tiles;
+        first = slots = 0;
+        window(0);
+        int64_t all = total, weights = weighted ? __builtin_amdgcn_readlane(wave_inclusive_scan(weight()), kWave - 1) : 0;
+        if (E > kWave) {
+            int more = 0, heavier = 0;
+            for (int e = kWave + lane_id(); e < E; e += kWave) {
+                int at, here;
+                const int p = pieces_of(e, at, here);
+                more += p;
+                heavier += (here + kX - 1) / kX + kTileWeight * p;
+            }
+            all += __builtin_amdgcn_readlane(wave_inclusive_scan(more), kWave - 1);
+            if (weighted) weights += __builtin_amdgcn_readlane(wave_inclusive_scan(heavier), kWave - 1);
+        }
+        const uint32_t xcd = blockIdx.x & 7;
+        if (weighted) {
+            end = xcd < 7 ? tile_at(weights * (xcd + 1) / 8) : (uint32_t)(all * tiles);
+            j = xcd > 0 ? tile_at(weights * xcd / 8) : 0u;
+            rewind();
+        } else {
+            j = (uint32_t)(all * tiles * xcd / 8);
+            end = (uint32_t)(all * tiles * (xcd + 1) / 8);
+        }
+        j += blockIdx.x >> 3;
+        step = gridDim.x >> 3;
+    }
+    // The next tile; false when there is none.
+    __device__ __forceinline__ bool next(Span &s)
+    {
+        if (j >= end) return false;
+        const int64_t t = j / (uint32_t)tiles;
+        s.tile = (int)(j % (uint32_t)tiles);
+        j = end - j > step ? j + step : end;
+        while (t - first >= total) {
+            first += total;
+            slots += __builtin_amdgcn_readlane(wave_inclusive_scan(pieces > 1 ? pieces : 0), kWave - 1);
+            if (base + kWave >= E) return false;
+            window(base + kWave);
+        }
+        const int w = (int)(t - first);
+        const int l = __builtin_ctzll(__ballot(before > w));
+        s.g = base + l;
+        s.count = __builtin_amdgcn_readlane(pieces, l);
+        s.local = w - (__builtin_amdgcn_readlane(before, l) - s.count);
+        const int at = s.local * per, rows = __builtin_amdgcn_readlane(size, l) - at;
+        s.lo = (int64_t)__builtin_amdgcn_readlane(lo, l) + at;
+        s.have = rows < per ? rows : per;
+        s.slot = slots;
+        if (s.count > 1) {
+            const int many = pieces > 1 && lane_id() < l ? pieces : 0;
+            s.slot += __builtin_amdgcn_readlane(wave_inclusive_scan(many), kWave - 1);
+        }
+        return true;
+    }
+};
 
 // -------------------------------------------------------- pieces of memory
-
-__device__ __forceinline__ uint4 load16(const void *p)
-{
-    const u32x4_u v = *reinterpret_cast<const u32x4_u *>(p);
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-
-__device__ __forceinline__ uint2 load8_bytes(const void *p)
-{
-    const u32x2_b v = *reinterpret_cast<const u32x2_b *>(p);
-    return make_uint2(v.x, v.y);
-}
 
 // A whole row of under 8 elements, zeros behind it.
 template <typename T>
@@ -196,8 +283,7 @@ __device__ __forceinline__ float act_grad(float d, float y, int act)
 }
 
 // ------------------------------------------------------------- LDS tiles
-// A row tile holds R rows of 64 x (128 bytes): 16-byte piece p of row r lies at p ^ (r / 2
-// mod 8), so that the 16 rows that a phase of fragment reads takes cover all banks.  A col
+// A row tile holds R rows of 64 x (128 bytes): the 16-byte pieces of a row are permuted by the row, so that the 16 rows that a phase of fragment reads takes cover all banks.  A col
 // tile holds 64 x of C elements: the 32-byte granules of a row are permuted by the row, so
 // that the four rows a transposing read takes lie on different banks.
 
@@ -229,83 +315,100 @@ __device__ __forceinline__ uint4 col_fragment(const char *tile, int idx0, int s)
     return make_uint4(u.x, u.y, v.x, v.y);
 }
 
-// 16 bytes a lane from memory to LDS, the wavefront's 1024 bytes in lane order from `to` on.
-__device__ __forceinline__ void load_to_lds(const void *from, char *to)
+// Buffers: loads past their end give zeros.  Direct loads: 16 bytes a lane from byte `offset` of
+// the buffer to LDS, the wavefront's 1024 bytes in lane order from `to` on.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+
+__device__ __forceinline__ Buffer buffer_of(const void *p, int64_t bytes)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    const int64_t most = (int64_t)kBufferMaxBytes;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)(uint32_t)(bytes < most ? bytes : most),
+                                             kBufferWord3);
 }
 
+__device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, char *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint4 load16(Buffer from, uint32_t offset)
+{
+    const auto w = __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ uint2 load8_bytes(Buffer from, uint32_t offset)
+{
+    const auto w = __builtin_amdgcn_raw_buffer_load_b64(from, (int)offset, 0, 0);
+    return make_uint2(w[0], w[1]);
+}
+
+// An offset past every buffer.
+constexpr uint32_t kNowhere = (uint32_t)kBufferMaxBytes;
+
 // ------------------------------------------------------------- operands
-// An operand's chunk on its way from memory to LDS: issue() starts the loads of the pieces
-// this thread brings (FULL: the chunk's 64 x all exist), finish() writes those that wait in
-// registers.  N threads.  Staged pieces at a row's end are read from its last 8 elements and
-// shifted down, those behind the last row from the last one and zeroed: no load leaves the
-// operand, and none waits for a branch.
+// An operand's chunks on their way from memory to LDS: issue() starts the loads of the pieces
+// this thread brings, finish() writes those that wait in registers.  N threads.  x
+// past the end are zero: loads leave the buffer there, and staged pieces at a row's end are
+// read from its last 8 elements and shifted down, so that every piece lies inside or outside.
 
 enum Source { kDirect, kStaged, kSloped, kCodes };
 
-// R indices (rows of the matrix) x 64 x along the row; indices from `have` on repeat the last
-// (their outputs are not stored).  x from `width` on are zero.
+// R indices (rows of the matrix) by x along the row; indices from `have` on are zero, and so are
+// x from `width` on.
 template <typename T, int R, int N, int SRC>
 struct RowOperand {
     static constexpr bool direct = SRC == kDirect, sloped = SRC == kSloped;
-    static constexpr int Q = R * kPieces / N;
-    static_assert(R * kPieces % N == 0 && N % (2 * kWave) == 0, "whole pieces a thread, whole swizzles a round");
+    static constexpr int P = kX / 8;
+    static constexpr int Q = R * P / N;
+    static constexpr int kBytes = R * kX * 2;
+    static_assert(R * P % N == 0 && N / P % 16 == 0, "whole pieces a thread, whole swizzles a round");
     const T *base, *ybase;       // (uniform)
-    uint32_t off[Q];             // the rows' elements from there
-    int width, act;
-    int gone;                    // elements of this thread's piece past the row's end
+    Buffer rows, yrows;
+    uint32_t off[Q];             // bytes to the rows (direct: to the piece)
+    int have, width, act;
     uint4 v[direct ? 1 : Q], y[sloped ? Q : 1];
 
-    __device__ __forceinline__ static int index(int q) { return ((int)threadIdx.x + q * N) / kPieces; }
+    __device__ __forceinline__ static int index(int q) { return ((int)threadIdx.x + q * N) / P; }
     // the piece this thread brings: in direct loads the one whose place is the thread's
     __device__ __forceinline__ static int piece()
     {
-        const int p = threadIdx.x % kPieces;
-        return direct ? p ^ row_swizzle(index(0)) : p;      // (N / 8 rows a round: a multiple of 16)
+        const int p = threadIdx.x % P;
+        return direct ? p ^ row_swizzle(index(0)) : p;
     }
-    __device__ __forceinline__ void open(const T *p, const T *py, int have, int w, int a)
+    __device__ __forceinline__ void open(const T *p, const T *py, int rows_here, int w, int a)
     {
         base = p;
         ybase = py;
+        have = rows_here;
         width = w;
         act = a;
+        rows = buffer_of(p, (int64_t)have * w * 2);
+        if constexpr (sloped) yrows = buffer_of(py, (int64_t)have * w * 2);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const int r = index(q);
-            off[q] = (uint32_t)(r < have ? r : have - 1) * (uint32_t)w;
-        }
+        for (int q = 0; q < Q; ++q) off[q] = (uint32_t)index(q) * (uint32_t)w * 2u + (direct ? (uint32_t)piece() * 16u : 0u);
     }
-    template <bool FULL>
     __device__ __forceinline__ void issue(int x0, char *tile)
     {
         const int at = x0 + piece() * 8;
-        if constexpr (direct && FULL) {
+        if constexpr (direct) {
             const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) load_to_lds(base + (off[q] + at), tile + (wave * kWave + q * N) * 16);
-        } else if constexpr (direct) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);       // (whole pieces: rows on the grid)
-                if (at < width) w = load16(base + (off[q] + at));
-                *reinterpret_cast<uint4 *>(tile + ((int)threadIdx.x + q * N) * 16) = w;
-            }
+            for (int q = 0; q < Q; ++q)
+                load_to_lds(rows, at < width ? off[q] + (uint32_t)x0 * 2u : kNowhere, tile + (wave * kWave + q * N) * 16);
         } else if (width >= 8) {
-            const int from = at + 8 <= width ? at : width - 8;
-            gone = at - from;
+            const uint32_t add = (uint32_t)(at + 8 <= width ? at : width - 8) * 2u;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                v[q] = load16(base + (off[q] + from));
-                if constexpr (sloped) y[q] = load16(ybase + (off[q] + from));
+                v[q] = load16(rows, off[q] + add);
+                if constexpr (sloped) y[q] = load16(yrows, off[q] + add);
             }
         } else {
-            gone = at;               // (one piece holds the row)
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                v[q] = load_short(base + off[q], width);
-                if constexpr (sloped) y[q] = load_short(ybase + off[q], width);
+                const int n = index(q) < have ? width : 0;
+                v[q] = load_short(base + off[q] / 2u, n);
+                if constexpr (sloped) y[q] = load_short(ybase + off[q] / 2u, n);
             }
         }
     }
@@ -313,6 +416,8 @@ struct RowOperand {
     {
         if constexpr (!direct) {
             const bool tail = x0 + kX > width;
+            const int at = x0 + piece() * 8;        // (of rows under 8 wide the first piece holds all)
+            const int gone = width >= 8 ? at + 8 - width : at;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 uint4 w = v[q];
@@ -332,14 +437,15 @@ struct RowOperand {
     __device__ __forceinline__ static uint4 fragment(const char *tile, int idx0, int s) { return row_fragment(tile, idx0, s); }
 };
 
-// 64 x (rows of the matrix, those from `have` on zero) by C indices along the row, from column c0
+// x (rows of the matrix, those from `have` on zero) by C indices along the row, from column c0
 // (columns past the row's end: zeros, or in direct loads whatever, their outputs are not stored).
-// SUM: keeps this thread's share of the sums over x of its 8 columns.
+// SUM: keeps this thread's share of the sums over x of its 8 columns, where asked to.
 template <typename T, int C, int N, int SRC, bool SUM>
 struct ColOperand {
     static constexpr bool direct = SRC == kDirect, sloped = SRC == kSloped, coded = SRC == kCodes;
     static constexpr int P = C / 8;
     static constexpr int Q = kX * P / N;
+    static constexpr int kBytes = kX * C * 2;
     static_assert(kX * P % N == 0 && N / P % 4 == 0, "whole pieces a thread, whole swizzles a round");
     const T *base, *ybase;       // (uniform)
     const int8_t *codes;
@@ -347,6 +453,7 @@ struct ColOperand {
     int have, width, act, nb;
     int at, from;                // this thread's columns, and where they are read
     bool ragged;                 // the tile reaches past the row's end
+    bool sums;
     uint4 v[direct || coded ? 1 : Q], y[sloped ? Q : 1];
     uint2 c[coded ? Q : 1];
     uint32_t b[coded ? Q : 1];
@@ -359,7 +466,7 @@ struct ColOperand {
         return direct ? p ^ col_swizzle<C>(index(0)) : p;
     }
     __device__ __forceinline__ void open(const T *p, const T *py, const int8_t *pc, const uint8_t *pe, int c0, int w,
-                                         int64_t rows, int a)
+                                         int64_t rows, int a, bool want_sums)
     {
         base = p;
         ybase = py;
@@ -372,51 +479,52 @@ struct ColOperand {
         at = c0 + piece() * 8;
         from = at + 8 <= w ? at : w >= 8 ? w - 8 : 0;
         ragged = c0 + C > w;
+        sums = want_sums;
+    }
+    __device__ __forceinline__ void clear_sums()
+    {
 #pragma unroll
         for (int e = 0; e < (SUM ? 8 : 1); ++e) sum[e] = 0.f;
     }
-    template <bool FULL>
     __device__ __forceinline__ void issue(int x0, char *tile)
     {
-        if constexpr (direct && FULL) {
+        const int64_t first = (int64_t)x0 * width, left = (int64_t)(have - x0) * width;
+        const uint32_t off = (uint32_t)index(0) * (uint32_t)width + (uint32_t)from, step = (uint32_t)(N / P) * (uint32_t)width;
+        if constexpr (direct) {
             const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-            const uint32_t off = (uint32_t)index(0) * (uint32_t)width + (uint32_t)from;
+            const Buffer rows = buffer_of(base + first, left * 2);
 #pragma unroll
-            for (int q = 0; q < Q; ++q)
-                load_to_lds(base + (int64_t)(x0 + q * (N / P)) * width + off, tile + (wave * kWave + q * N) * 16);
-        } else if constexpr (direct) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int64_t x = x0 + index(q);
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (x < have) w = load16(base + x * width + from);
-                *reinterpret_cast<uint4 *>(tile + ((int)threadIdx.x + q * N) * 16) = w;
-            }
+            for (int q = 0; q < Q; ++q) load_to_lds(rows, (off + q * step) * 2u, tile + (wave * kWave + q * N) * 16);
         } else if (width >= 8) {
-            const int last = have - 1 - x0;
+            if constexpr (coded) {
+                const Buffer rows = buffer_of(codes + first, left), bytes = buffer_of(exps + (int64_t)x0 * nb, (int64_t)(have - x0) * nb);
+                const uint32_t boff = (uint32_t)index(0) * (uint32_t)nb + (uint32_t)((at < width ? at : width - 1) / kCkptBlock);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int i = index(q) < last ? index(q) : last;
-                const uint32_t off = (uint32_t)i * (uint32_t)width + (uint32_t)from;
-                if constexpr (coded) {
-                    c[q] = load8_bytes(codes + (int64_t)x0 * width + off);
-                    b[q] = exps[(int64_t)x0 * nb + (uint32_t)(i * nb + (at < width ? at : width - 1) / kCkptBlock)];
-                } else {
-                    v[q] = load16(base + (int64_t)x0 * width + off);
-                    if constexpr (sloped) y[q] = load16(ybase + (int64_t)x0 * width + off);
+                for (int q = 0; q < Q; ++q) {
+                    c[q] = load8_bytes(rows, off + q * step);
+                    b[q] = __builtin_amdgcn_raw_buffer_load_b8(bytes, (int)(boff + (uint32_t)(q * (N / P)) * (uint32_t)nb), 0, 0);
+                }
+            } else {
+                const Buffer rows = buffer_of(base + first, left * 2);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) v[q] = load16(rows, (off + q * step) * 2u);
+                if constexpr (sloped) {
+                    const Buffer yrows = buffer_of(ybase + first, left * 2);
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) y[q] = load16(yrows, (off + q * step) * 2u);
                 }
             }
         } else {
-            const int last = have - 1 - x0;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                const int64_t x = x0 + (index(q) < last ? index(q) : last);
+                const int64_t x = x0 + index(q);
+                const int n = x < have ? width : 0;
                 if constexpr (coded) {
-                    c[q] = load_short(codes + x * width, width);
-                    b[q] = exps[x];
+                    c[q] = load_short(codes + x * width, n);
+                    b[q] = n > 0 ? exps[x] : 0u;
                 } else {
-                    v[q] = load_short(base + x * width, width);
-                    if constexpr (sloped) y[q] = load_short(ybase + x * width, width);
+                    v[q] = load_short(base + x * width, n);
+                    if constexpr (sloped) y[q] = load_short(ybase + x * width, n);
                 }
             }
         }
@@ -425,7 +533,6 @@ struct ColOperand {
     {
         if constexpr (!direct) {
             const int gone = at - from;
-            const bool tail = x0 + kX > have;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 uint4 w;
@@ -435,24 +542,24 @@ struct ColOperand {
                     w = ragged ? shift_down(v[q], gone) : v[q];
                 }
                 if constexpr (sloped || SUM) {
-                    float d[8];
-                    unpack8<T>(w, d);
-                    if constexpr (sloped) {
-                        float o[8];
-                        unpack8<T>(ragged ? shift_down(y[q], gone) : y[q], o);
+                    if (sloped || sums) {
+                        float d[8];
+                        unpack8<T>(w, d);
+                        if constexpr (sloped) {
+                            float o[8];
+                            unpack8<T>(ragged ? shift_down(y[q], gone) : y[q], o);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) d[e] = act_grad(d[e], o[e], act);
-                        w = pack8<T>(d);    // the matrix cores take 16 bits; the sums do not round
-                    }
-                    if constexpr (SUM) {
-                        if (!tail || x0 + index(q) < have) {
+                            for (int e = 0; e < 8; ++e) d[e] = act_grad(d[e], o[e], act);
+                            w = pack8<T>(d);    // the matrix cores take 16 bits; the sums do not round
+                        }
+                        if constexpr (SUM) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e) sum[e] += d[e];
                         }
                     }
                 }
-                if (tail && x0 + index(q) >= have) w = make_uint4(0u, 0u, 0u, 0u);
-                *reinterpret_cast<uint4 *>(tile + col_tile_at<C>(index(q), (threadIdx.x % P) * 16)) = w;
+                const int x = index(q);
+                *reinterpret_cast<uint4 *>(tile + col_tile_at<C>(x, (threadIdx.x % P) * 16)) = w;
             }
         }
     }
@@ -477,58 +584,53 @@ struct Acc {
     }
 };
 
-// A wavefront's own part of the LDS for its outputs: 32 rows of 32 WC fp32, rows 16 bytes apart
-// in the banks.
-template <int WC>
-struct OutTile {
-    static constexpr int kRow = 32 * WC * 4 + 16;
-    static constexpr int kBytes = 32 * kRow;
-};
+// A wavefront's own part of the LDS for its outputs: 32 x 32 fp32, the 16-byte pieces of a row
+// permuted by the row.
+constexpr int kOutBytes = 4096;
 
 // Calls out(row in the block, column in the block, 8 consecutive outputs) for each 8 outputs of a
 // wavefront, through its part of the LDS: neighbouring lanes then hold neighbouring columns of
-// a row, and a store instruction fills whole lines.  The LDS is free of other use.
+// a row.
 template <int WR, int WC, typename Out>
-__device__ __forceinline__ void for_outputs(char *lds, int wave, const Acc<WR, WC> &acc, Out out)
+__device__ __forceinline__ void for_outputs(char *mine, const Acc<WR, WC> &acc, Out out)
 {
-    constexpr int kLanes = 4 * WC, kRows = kWave / kLanes;      // lanes of a row, rows of a round
     const int lane = lane_id(), i = lane & 31, kq = lane >> 5;
-    char *const mine = lds + wave * OutTile<WC>::kBytes;
-    const int row = lane / kLanes, col = lane % kLanes * 8;
+    const int row = lane >> 2, piece = lane & 3;
 #pragma unroll
-    for (int br = 0; br < WR; ++br) {
+    for (int br = 0; br < WR; ++br)
 #pragma unroll
-        for (int bc = 0; bc < WC; ++bc)
+        for (int bc = 0; bc < WC; ++bc) {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4 *>(mine + i * OutTile<WC>::kRow + (32 * bc + 8 * g + 4 * kq) * 4) =
+                *reinterpret_cast<float4 *>(mine + i * 128 + (((2 * g + kq) ^ (i & 7)) << 4)) =
                     make_float4(acc.a[br][bc][4 * g], acc.a[br][bc][4 * g + 1], acc.a[br][bc][4 * g + 2],
                                 acc.a[br][bc][4 * g + 3]);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int r = row; r < 32; r += kRows) {
-            const float4 lo = *reinterpret_cast<const float4 *>(mine + r * OutTile<WC>::kRow + col * 4);
-            const float4 hi = *reinterpret_cast<const float4 *>(mine + r * OutTile<WC>::kRow + col * 4 + 16);
-            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            out(32 * br + r, col, v);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = row + 16 * h;
+                const float4 lo = *reinterpret_cast<const float4 *>(mine + r * 128 + (((2 * piece) ^ (r & 7)) << 4));
+                const float4 hi = *reinterpret_cast<const float4 *>(mine + r * 128 + (((2 * piece + 1) ^ (r & 7)) << 4));
+                float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                out(32 * br + r, 32 * bc + 8 * piece, v);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
 }
 
 // A step's fragments of both operands.
 template <int WR, int WC>
 struct Fragments {
     uint4 a[WR], b[WC];
-    template <int TM, typename A, typename B>
+    template <typename A, typename B>
     __device__ __forceinline__ void read(const char *tiles, int r0, int c0, int s)
     {
 #pragma unroll
         for (int i = 0; i < WR; ++i) a[i] = A::fragment(tiles, r0 + 32 * i, s);
 #pragma unroll
-        for (int j = 0; j < WC; ++j) b[j] = B::fragment(tiles + TM * kX * 2, c0 + 32 * j, s);
+        for (int j = 0; j < WC; ++j) b[j] = B::fragment(tiles + A::kBytes, c0 + 32 * j, s);
     }
 };
 
@@ -541,78 +643,114 @@ __device__ __forceinline__ void step(const Fragments<WR, WC> &f, Acc<WR, WC> &ac
         for (int j = 0; j < WC; ++j) acc.a[i][j] = mfma_32x32x16<T>(f.b[j], f.a[i], acc.a[i][j]);
 }
 
-// Every wavefront's loads to LDS have landed (the compiler does not wait for them) and its reads are done.
-__device__ __forceinline__ void chunk_done()
+// Starts the chunk from x0 on.
+template <typename A, typename B>
+__device__ __forceinline__ void issue(int x0, char *to, A &a, B &b)
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
+    a.issue(x0, to);
+    b.issue(x0, to + A::kBytes);
 }
 
-// acc += A B over one chunk of 64 x in `now`, whose first step's fragments are in f[0]; the next
-// one's loads go to `next` meanwhile (from x1 on: kFullNext its 64 x all exist, kTailNext some,
-// kNoNext there is none).  The two never overlap, which the compiler has to know to keep loads in
-// flight under the reads.  A step's fragments are read while the matrix cores work on the step
-// before, those of the next chunk's first step behind the barrier under this one's last.
-enum Next { kNoNext, kFullNext, kTailNext };
-
-template <typename T, int TM, typename A, typename B, int WR, int WC, typename Each>
-__device__ __forceinline__ void chunk(const char *__restrict__ now, char *__restrict__ next, A &a, B &b, int x1, Next more,
-                                      int r0, int c0, Fragments<WR, WC> (&f)[2], Acc<WR, WC> &acc, Each each)
+// This wavefront's chunk is in LDS: what waits in registers is written, direct loads have landed.
+// (The compiler does not wait for loads to LDS on behalf of other wavefronts.)
+template <typename A, typename B>
+__device__ __forceinline__ void landed(int x0, char *to, A &a, B &b)
 {
-    constexpr int kB = TM * kX * 2, S = kX / 16;
-    if (more == kFullNext) {
-        a.template issue<true>(x1, next);
-        b.template issue<true>(x1, next + kB);
-    } else if (more == kTailNext) {
-        a.template issue<false>(x1, next);
-        b.template issue<false>(x1, next + kB);
+    static_assert(A::direct == B::direct, "either both operands pass through registers or none");
+    if constexpr (A::direct) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+        asm volatile("" ::: "memory");
+    } else {
+        a.finish(x0, to);
+        b.finish(x0, to + A::kBytes);
     }
+}
+
+// This wavefront's LDS accesses are done, and so are every other wavefront's.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// acc += A B over one chunk, which lies in `now` and whose first step's fragments are in f[0].
+// `start` starts the loads of what goes to `next`: this tile's chunk x1, if x1 > 0, which is
+// finished here, or the next tile's first.  `next` and `now` never overlap, which the compiler has
+// to know to keep loads in flight under the reads.  A step's fragments are read while the matrix
+// cores work on the step before, those of the next chunk's first step behind the barrier under
+// this one's last.
+template <typename T, typename A, typename B, int WR, int WC, typename Start, typename Each>
+__device__ __forceinline__ void chunk(const char *__restrict__ now, char *__restrict__ next, A &a, B &b, int x1, int r0, int c0,
+                                      Fragments<WR, WC> (&f)[2], Acc<WR, WC> &acc, Start start, Each each)
+{
+    constexpr int S = kX / 16;
+    start(next);
 #pragma unroll
     for (int s = 0; s + 1 < S; ++s) {
-        f[(s + 1) & 1].template read<TM, A, B>(now, r0, c0, s + 1);
+        f[(s + 1) & 1].template read<A, B>(now, r0, c0, s + 1);
         __builtin_amdgcn_sched_barrier(0);       // (the reads start before the step's products, not among the last)
         each(f[s & 1].a);
         step<T>(f[s & 1], acc);
     }
-    if (more != kNoNext) {
-        a.finish(x1, next);
-        b.finish(x1, next + kB);
-        chunk_done();
-        f[0].template read<TM, A, B>(next, r0, c0, 0);
+    // lgkmcnt(0), for f[1]: behind the branch the compiler would wait for the next chunk's reads with it
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    if (x1 > 0) {
+        landed(x1, next, a, b);
+        meet();
+        f[0].template read<A, B>(next, r0, c0, 0);
         __builtin_amdgcn_sched_barrier(0);
     }
     each(f[1].a);
     step<T>(f[1], acc);
 }
 
-// acc += A B over x in [0, width): lds holds two pairs of tiles.
-template <typename T, int TM, int TN, typename A, typename B, int WR, int WC, typename Each>
-__device__ __forceinline__ void multiply(char *lds, A &a, B &b, int width, int r0, int c0, Acc<WR, WC> &acc, Each each)
+// The tiles of a workgroup.  open(span) makes the operands a and b those of a tile; each(span, fa)
+// sees the first operand's fragments; done(span, acc) takes the products of the tile (its own
+// wavefront's, no barrier needed).  lds: two pairs of chunks.  settle() runs between a tile's last
+// product and the next tile's first chunk being finished.
+template <typename T, typename A, typename B, int WR, int WC, typename Open, typename Each, typename Settle, typename Done>
+__device__ __forceinline__ void run_tiles(char *lds, Walk &walk, A &a, B &b, int r0, int c0, Open open, Each each,
+                                          Settle settle, Done done)
 {
-    constexpr int kB = TM * kX * 2, kPair = (TM + TN) * kX * 2;
-    if (width <= 0) return;
-    if (width >= kX) {
-        a.template issue<true>(0, lds);
-        b.template issue<true>(0, lds + kB);
-    } else {
-        a.template issue<false>(0, lds);
-        b.template issue<false>(0, lds + kB);
-    }
-    a.finish(0, lds);
-    b.finish(0, lds + kB);
-    chunk_done();
+    constexpr int kPair = A::kBytes + B::kBytes;
+    Span s, ahead;
+    if (!walk.next(s)) return;
     char *now = lds, *next = lds + kPair;
+    int width = open(s);
+    issue(0, now, a, b);
+    landed(0, now, a, b);
+    Acc<WR, WC> acc;
     Fragments<WR, WC> f[2];
-    f[0].template read<TM, A, B>(now, r0, c0, 0);
+    for (;;) {
+        const bool more = walk.next(ahead);
+        acc.clear();
+        meet();
+        f[0].template read<A, B>(now, r0, c0, 0);
+        int x1 = kX, width1 = 0;
 #pragma unroll 1
-    for (int x1 = kX; x1 < width + kX; x1 += kX) {
-        const Next more = x1 + kX <= width ? kFullNext : x1 < width ? kTailNext : kNoNext;
-        chunk<T, TM>(now, next, a, b, x1, more, r0, c0, f, acc, each);
-        char *const t = now;
-        now = next;
-        next = t;
+        do {
+            const bool last = x1 >= width;
+            chunk<T>(now, next, a, b, last ? 0 : x1, r0, c0, f, acc,
+                     [&](char *to) {
+                         if (last && more) width1 = open(ahead);
+                         if (!last || more) issue(last ? 0 : x1, to, a, b);
+                     },
+                     [&](const uint4 (&fa)[WR]) { each(s, fa); });
+            char *const t = now;
+            now = next;
+            next = t;
+            x1 += kX;
+        } while (x1 < width + kX);
+        settle(s);
+        if (more) landed(0, now, a, b);      // (before this tile's stores: waits are in order)
+        done(s, acc);
+        if (!more) return;
+        s = ahead;
+        width = width1;
     }
-    __syncthreads();
 }
 
 // Stores those of 8 consecutive outputs from column c on that lie below width.
@@ -659,15 +797,6 @@ struct GroupedArgs {
     float *part_db;
 };
 
-// Pieces of rows are dealt round the 8 XCDs, the column tiles of a piece one after another on
-// one of them: they share the piece's rows in its L2.
-__device__ __forceinline__ void tile_of(int tiles_c, int64_t &piece, int &tile)
-{
-    const int64_t j = blockIdx.x >> 3;
-    piece = j / tiles_c * 8 + (blockIdx.x & 7);
-    tile = (int)(j % tiles_c);
-}
-
 // Most pieces of `per` rows that n rows in E groups can have.
 inline int64_t most_pieces(int64_t n, int32_t E, int64_t per) { return n / per + (n < E ? n : E); }
 
@@ -678,14 +807,26 @@ inline unsigned piece_tiles(int64_t pieces, int64_t tiles)
     return b <= INT32_MAX ? (unsigned)b : 0u;
 }
 
-// Rows a tile spans at most; a row operand's offsets are 32 bits (kMaxTile rows of kMaxWidth).
-constexpr int kMaxTile = 256;
-constexpr int kMaxWidth = 1 << 23;
+// Widths: the byte offsets inside a tile of 256 rows (or a chunk of 64) are 32 bits.
+constexpr int kMaxWidth = 1 << 22;
 
-// Whether rows of `width` 16-bit elements from p on lie on the 16-byte grid.
+// Whether direct loads take rows of `width` 16-bit elements from p on.
 inline bool on_grid(const void *p, int width) { return width % 8 == 0 && (uintptr_t)p % 16 == 0; }
 
 using GroupedKernel = void (*)(GroupedArgs);
+
+// A kernel over tiles: resident workgroups, as many on each XCD, no more than the tiles that
+// `pieces` pieces can make.
+inline cogdl_status launch_tiles(const char *name, GroupedKernel kern, const GroupedArgs &a, int64_t pieces, int waves, int tm,
+                                 int tn, hipStream_t stream)
+{
+    const size_t lds = (size_t)2 * (tm + tn) * kX * 2 + (size_t)waves * kOutBytes;
+    const int64_t resident = resident_blocks(reinterpret_cast<const void *>(kern), waves * kWave, lds) / 8;
+    if (resident < 1) return COGDL_ERR_LAUNCH;
+    const int64_t need = (pieces + 7) / 8 * a.tiles_c;
+    COGDL_LAUNCH_SHM(name, kern, dim3((unsigned)(8 * (need < resident ? need : resident))), waves * kWave, lds, stream, a);
+    return COGDL_OK;
+}
 
 // The products over rows: the forward, and dX of dY (and Y, with an activation).
 cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl_dtype dtype, hipStream_t s);

@@ -9,7 +9,7 @@
 namespace cogdl {
 namespace {
 
-// dW and db of one chunk of a group's rows: TM x TN outputs (c by j) of its matrix.
+// dW and db of chunks of a group's rows: TM x TN outputs (c by j) of its matrix at a time.
 template <typename T, int WAVES, int TM, int TN, int SRC, int SRCB>
 __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a)
 {
@@ -17,37 +17,34 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
     constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
     constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
     extern __shared__ __align__(16) char lds[];
-    int64_t piece;
-    int tile;
-    tile_of(a.tiles_c, piece, tile);
-    Span s;
-    if (!find_span(a.off, a.E, a.n, a.per, piece, s)) return;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
-    const int tiles_k = a.k > 0 ? (a.k + TN - 1) / TN : 1;
-    const int row0 = tile / tiles_k * TM, col0 = tile % tiles_k * TN;
-    const int64_t have = s.hi - s.lo;
+    const int tiles_k = a.k > 0 ? (a.k + TN - 1) / TN : 1, nb = (a.k + kCkptBlock - 1) / kCkptBlock;
+    const int64_t mk = (int64_t)a.m * a.k;
     // db: staged operands sum their own columns on the way; direct ones are summed from the
     // fragments of the wavefronts that hold the first columns
     constexpr bool STAGED_SUM = SRC != kDirect;
+    Walk walk;
+    walk.start(a.off, a.E, a.n, a.per, a.tiles_c, true);
     ColOperand<T, TM, N, SRC, STAGED_SUM> A;
-    A.open(static_cast<const T *>(a.dY) + s.lo * a.m, SRC == kSloped ? static_cast<const T *>(a.Y) + s.lo * a.m : nullptr,
-           nullptr, nullptr, row0, a.m, have, a.act);
     ColOperand<T, TN, N, SRCB, false> B;
-    const int nb = (a.k + kCkptBlock - 1) / kCkptBlock;
-    B.open(static_cast<const T *>(a.X) + (SRCB == kCodes ? 0 : s.lo * a.k), nullptr,
-           SRCB == kCodes ? a.codes + s.lo * a.k : nullptr, SRCB == kCodes ? a.exps + s.lo * nb : nullptr, col0, a.k, have, 0);
-    Acc<WR, WC> acc;
-    acc.clear();
-    const bool sums = a.db && col0 == 0;
-    float fsum[WR];
+    A.clear_sums();
+    const auto sums = [&](const Span &s) { return a.db && s.tile % tiles_k == 0; };
+    const auto open = [&](const Span &s) {
+        A.open(static_cast<const T *>(a.dY) + s.lo * a.m, SRC == kSloped ? static_cast<const T *>(a.Y) + s.lo * a.m : nullptr,
+               nullptr, nullptr, s.tile / tiles_k * TM, a.m, s.have, a.act, sums(s));
+        B.open(static_cast<const T *>(a.X) + (SRCB == kCodes ? 0 : s.lo * a.k), nullptr,
+               SRCB == kCodes ? a.codes + s.lo * a.k : nullptr, SRCB == kCodes ? a.exps + s.lo * nb : nullptr,
+               s.tile % tiles_k * TN, a.k, s.have, 0, false);
+        return s.have;
+    };
+    float fsum[STAGED_SUM ? 1 : WR], colsum[STAGED_SUM ? 8 : 1];
 #pragma unroll
-    for (int i = 0; i < WR; ++i) fsum[i] = 0.f;
-    const bool wave_sums = !STAGED_SUM && sums && c0 == 0;
+    for (int i = 0; i < (STAGED_SUM ? 1 : WR); ++i) fsum[i] = 0.f;
     constexpr uint32_t kOnes = Fmt<T>::code == COGDL_BF16 ? 0x3f803f80u : 0x3c003c00u;
-    multiply<T, TM, TN>(lds, A, B, (int)have, r0, c0, acc, [&](const uint4 (&fa)[WR]) {
+    const auto each = [&](const Span &s, const uint4 (&fa)[WR]) {
         if constexpr (!STAGED_SUM) {
-            if (!wave_sums) return;
+            if (c0 != 0 || !sums(s)) return;
 #pragma unroll
             for (int i = 0; i < WR; ++i) {
                 fsum[i] = dot2_acc<T>(fa[i].x, kOnes, fsum[i]);
@@ -56,52 +53,65 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
                 fsum[i] = dot2_acc<T>(fa[i].w, kOnes, fsum[i]);
             }
         }
+    };
+    const auto settle = [&](const Span &) {
+        if constexpr (STAGED_SUM) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) colsum[e] = A.sum[e];
+            A.clear_sums();
+        }
+    };
+    char *const outs = lds + 2 * (TM + TN) * kX * 2;
+    run_tiles<T, decltype(A), decltype(B), WR, WC>(lds, walk, A, B, r0, c0, open, each, settle, [&](const Span &s,
+                                                                                             const Acc<WR, WC> &acc) {
+        const int row0 = s.tile / tiles_k * TM, col0 = s.tile % tiles_k * TN;
+        if (a.out) {
+            float *__restrict__ part = a.part + (s.slot + s.local) * mk;
+            for_outputs<WR, WC>(outs + wave * kOutBytes, acc, [&](int r, int c, float (&v)[8]) {
+                r += row0 + r0;
+                c += col0 + c0;
+                if (r >= a.m || c >= a.k) return;
+                if (s.count == 1) store8(a.out, a.out_dtype, s.g * mk + (int64_t)r * a.k, c, a.k, v);
+                else store8(part + (int64_t)r * a.k, c, a.k, v);
+            });
+        }
+        if (!sums(s)) return;
+        float *__restrict__ db = s.count == 1 ? a.db + (int64_t)s.g * a.m : a.part_db + (s.slot + s.local) * a.m;
+        if constexpr (STAGED_SUM) {
+            // the threads that share 8 columns add up in order
+            constexpr int P = TM / 8, S = N / P;
+            static_assert(S * TM * (int)sizeof(float) <= WAVES * kOutBytes, "the sums fit the outputs' part");
+            float *const shared = reinterpret_cast<float *>(outs);
+            meet();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) shared[(threadIdx.x / P) * TM + (threadIdx.x % P) * 8 + e] = colsum[e];
+            meet();
+            const int c = row0 + (int)threadIdx.x;
+            if ((int)threadIdx.x < TM && c < a.m) {
+                float t = 0.f;
+#pragma unroll
+                for (int q = 0; q < S; ++q) t += shared[q * TM + threadIdx.x];
+                db[c] = t;
+            }
+            meet();
+        } else if (c0 == 0) {
+            const int lane = lane_id();
+#pragma unroll
+            for (int i = 0; i < WR; ++i) {
+                const float t = fsum[i] + bfly_partner<32>(fsum[i]);
+                const int c = row0 + r0 + 32 * i + (lane & 31);
+                if (lane < 32 && c < a.m) db[c] = t;
+                fsum[i] = 0.f;
+            }
+        }
     });
-    const int64_t mk = (int64_t)a.m * a.k;
-    if (a.out) {
-        float *__restrict__ part = a.part + (s.slot + s.local) * mk;
-        for_outputs<WR, WC>(lds, wave, acc, [&](int r, int c, float (&v)[8]) {
-            r += row0 + r0;
-            c += col0 + c0;
-            if (r >= a.m || c >= a.k) return;
-            if (s.count == 1) store8(a.out, a.out_dtype, s.g * mk + (int64_t)r * a.k, c, a.k, v);
-            else store8(part + (int64_t)r * a.k, c, a.k, v);
-        });
-    }
-    if (!sums) return;
-    float *__restrict__ db = s.count == 1 ? a.db + (int64_t)s.g * a.m : a.part_db + (s.slot + s.local) * a.m;
-    if constexpr (STAGED_SUM) {
-        // the threads that share 8 columns add up in order
-        constexpr int P = TM / 8, S = N / P;
-        static_assert(S * TM * (int)sizeof(float) <= 2 * (TM + TN) * kX * 2, "the sums fit the tiles");
-        float *const shared = reinterpret_cast<float *>(lds);
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) shared[(threadIdx.x / P) * TM + (threadIdx.x % P) * 8 + e] = A.sum[e];
-        __syncthreads();
-        const int c = row0 + (int)threadIdx.x;
-        if ((int)threadIdx.x < TM && c < a.m) {
-            float t = 0.f;
-#pragma unroll
-            for (int q = 0; q < S; ++q) t += shared[q * TM + threadIdx.x];
-            db[c] = t;
-        }
-    } else if (wave_sums) {
-        const int lane = lane_id();
-#pragma unroll
-        for (int i = 0; i < WR; ++i) {
-            const float t = fsum[i] + bfly_partner<32>(fsum[i]);
-            const int c = row0 + r0 + 32 * i + (lane & 31);
-            if (lane < 32 && c < a.m) db[c] = t;
-        }
-    }
 }
 
 // Sums over a group's partial sums.  Four quarters of the slots, each added up in order by a
-// thread of its own with kAhead loads in flight, then the quarters in order.
+// thread of its own with kBatch loads in flight, then the quarters in order.
 constexpr int kBlock = 256;
 constexpr int kQuarters = 4;
-constexpr int kAhead = 8;
+constexpr int kBatch = 8;
 
 // V values from p on in each of the slots [0, count), `stride` floats apart.
 template <int V>
@@ -109,16 +119,16 @@ __device__ __forceinline__ void sum_slots(const float *__restrict__ p, int64_t s
 {
 #pragma unroll
     for (int e = 0; e < V; ++e) t[e] = 0.f;
-    for (int c = 0; c < count; c += kAhead) {
-        float v[kAhead][V];
+    for (int c = 0; c < count; c += kBatch) {
+        float v[kBatch][V];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kBatch; ++u) {
             const int at = c + u < count ? c + u : count - 1;
             if constexpr (V == 4) load_vec<float, 4>(p, at * stride, v[u]);
             else v[u][0] = p[at * stride];
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kBatch; ++u)
 #pragma unroll
             for (int e = 0; e < V; ++e) t[e] += c + u < count ? v[u][e] : 0.f;
     }
@@ -178,48 +188,39 @@ struct Tiles {
     int tm, tn;
 };
 
-template <typename T, int WAVES, int TM, int TN, int SRC>
-GroupedKernel pick_x(bool codes, bool direct_x)
-{
-    if (codes) return k_grouped_weights<T, WAVES, TM, TN, SRC, kCodes>;
-    return direct_x ? k_grouped_weights<T, WAVES, TM, TN, SRC, kDirect> : k_grouped_weights<T, WAVES, TM, TN, SRC, kStaged>;
-}
-
 template <typename T, int WAVES, int TM, int TN>
-GroupedKernel pick(bool act, bool direct_dy, bool codes, bool direct_x)
+GroupedKernel pick(bool act, bool codes, bool direct)
 {
-    if (act) return pick_x<T, WAVES, TM, TN, kSloped>(codes, direct_x);
-    return direct_dy ? pick_x<T, WAVES, TM, TN, kDirect>(codes, direct_x) : pick_x<T, WAVES, TM, TN, kStaged>(codes, direct_x);
+    if (act) return codes ? k_grouped_weights<T, WAVES, TM, TN, kSloped, kCodes> : k_grouped_weights<T, WAVES, TM, TN, kSloped, kStaged>;
+    if (codes) return k_grouped_weights<T, WAVES, TM, TN, kStaged, kCodes>;
+    return direct ? k_grouped_weights<T, WAVES, TM, TN, kDirect, kDirect> : k_grouped_weights<T, WAVES, TM, TN, kStaged, kStaged>;
 }
 
 template <typename T>
-GroupedKernel pick_tile(const Tiles &c, bool act, bool direct_dy, bool codes, bool direct_x)
+GroupedKernel pick_tile(const Tiles &c, bool act, bool codes, bool direct)
 {
-    if (c.tm == 256) return codes ? k_grouped_weights<T, 8, 256, 256, kDirect, kCodes>
+    if (c.tm == 256) return codes ? k_grouped_weights<T, 8, 256, 256, kStaged, kCodes>
                                   : k_grouped_weights<T, 8, 256, 256, kDirect, kDirect>;
-    if (c.tm == 128) return c.tn == 128 ? pick<T, 4, 128, 128>(act, direct_dy, codes, direct_x)
-                                        : pick<T, 4, 128, 64>(act, direct_dy, codes, direct_x);
-    return c.tn == 128 ? pick<T, 4, 64, 128>(act, direct_dy, codes, direct_x)
-                       : pick<T, 4, 64, 64>(act, direct_dy, codes, direct_x);
+    if (c.tm == 128) return c.tn == 128 ? pick<T, 4, 128, 128>(act, codes, direct) : pick<T, 4, 128, 64>(act, codes, direct);
+    return c.tn == 128 ? pick<T, 4, 64, 128>(act, codes, direct) : pick<T, 4, 64, 64>(act, codes, direct);
 }
 
 int64_t tiles_of(int64_t m, int64_t k, int tm, int tn) { return (m + tm - 1) / tm * (k > 0 ? (k + tn - 1) / tn : 1); }
 
 }  // namespace
 
-// Rows of a chunk: a partial sum is written and read once for each, so chunks are as long as two
-// workgroups a compute unit allow (counted in tiles of 128 x 128, 64 where a side has no
-// more), E groups ending in a short one each; 512 rows at least.  A group of several chunks has
-// under 2 n_g / per of them.
+// Rows of a piece: a partial sum is written and read once for each, so there are no more pieces
+// than make two tiles of 128 x 128 (one of 256 x 256) for each resident workgroup, E groups ending
+// in a short one each; 512 rows at least.  A group of several pieces has under 2 n_g / per.
 Chunks chunks_of(int64_t n, int32_t E, int32_t k, int32_t m)
 {
     Chunks c;
     const int64_t tiles = tiles_of(m, k, m > 64 ? 128 : 64, k > 64 ? 128 : 64);
-    const int64_t want = 512 / (tiles < 1 ? 1 : tiles < 512 ? tiles : 512);
+    const int64_t want = 1024 / (tiles < 1 ? 1 : tiles < 1024 ? tiles : 1024);
     int64_t pieces = want - E > want / 2 ? want - E : want / 2;
     if (pieces < 1) pieces = 1;
     int64_t per = (n + pieces - 1) / pieces;
-    per = (per + kX - 1) / kX * kX;
+    per = (per + 63) / 64 * 64;
     if (per < 512) per = 512;
     if (per > (1 << 30)) per = 1 << 30;
     c.per = per;
@@ -237,17 +238,16 @@ cogdl_status grouped_weights_launch(GroupedArgs a, const Chunks &c, cogdl_dtype 
     a.part_db = a.part + (size_t)c.slots * a.m * a.k;
     const bool act = a.act != COGDL_ACT_NONE, codes = a.codes != nullptr;
     if (a.n > 0) {
-        const bool direct_dy = on_grid(a.dY, a.m), direct_x = a.out && !codes && on_grid(a.X, a.k);
+        const bool direct = a.out && !codes && on_grid(a.dY, a.m) && on_grid(a.X, a.k);
         Tiles t{a.m > 64 ? 128 : 64, a.k > 64 ? 128 : 64};
-        if (a.m > 128 && a.k > 128 && !act && direct_dy && (codes || direct_x)) t = {256, 256};
+        if (a.m > 128 && a.k > 128 && !act && (codes || direct)) t = {256, 256};
         const int64_t tiles = tiles_of(a.m, a.k, t.tm, t.tn);
-        const unsigned grid = tiles <= INT32_MAX ? piece_tiles(most_pieces(a.n, a.E, c.per), tiles) : 0;
-        if (grid == 0) return COGDL_ERR_TOO_LARGE;
         a.tiles_c = (int32_t)tiles;
-        const GroupedKernel kern = dtype == COGDL_BF16 ? pick_tile<bf16_t>(t, act, direct_dy, codes, direct_x)
-                                                       : pick_tile<f16_t>(t, act, direct_dy, codes, direct_x);
-        const int waves = t.tm == 256 ? 8 : 4;
-        COGDL_LAUNCH_SHM("grouped_linear_dw", kern, grid, waves * kWave, (size_t)2 * (t.tm + t.tn) * kX * 2, stream, a);
+        const GroupedKernel kern = dtype == COGDL_BF16 ? pick_tile<bf16_t>(t, act, codes, direct)
+                                                       : pick_tile<f16_t>(t, act, codes, direct);
+        const cogdl_status st = launch_tiles("grouped_linear_dw", kern, a, most_pieces(a.n, a.E, c.per), t.tm == 256 ? 8 : 4, t.tm,
+                                             t.tn, stream);
+        if (st != COGDL_OK) return st;
     }
     // whole vectors of 4 where the matrices and rows of db are
     const int64_t values = (a.out ? (int64_t)a.m * a.k : 0) + (a.db ? a.m : 0);
