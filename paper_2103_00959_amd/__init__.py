@@ -22,7 +22,9 @@ fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -143,7 +145,8 @@ def _ptr(t):
 
 def _stream():
     import torch
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # (the handle itself: a Stream object around it takes 3 us)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev(t, name, dtype=None):
@@ -894,13 +897,21 @@ CKPT_BLOCK = 32        # COGDL_CKPT_BLOCK: features that share an exponent byte
 MAX_GROUPS = 4096      # COGDL_MAX_GROUPS
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on_device(*tensors):
     """A context with the tensors' device current (they must share one)."""
     import torch
-    devices = {t.device for t in tensors if t is not None}
+    devices = {t.get_device() for t in tensors if t is not None}
     if len(devices) != 1:
-        raise CogdlError(f"the tensors lie on several devices: {sorted(map(str, devices))}")
-    return torch.cuda.device(devices.pop())
+        raise CogdlError(f"the tensors lie on several devices: {sorted(devices)}")
+    device = devices.pop()
+    return _HERE if device == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _ckpt_blocks(F):
@@ -921,12 +932,12 @@ def act_checkpoint(A, codes=None, exps=None):
     _dev(A, "A")
     dt = _dtype_code(A)
     if codes is None:
-        codes = torch.empty((n, F), dtype=torch.int8, device=A.device)
+        codes = A.new_empty((n, F), dtype=torch.int8)
     if exps is None:
-        exps = torch.empty((n, nb), dtype=torch.uint8, device=A.device)
+        exps = A.new_empty((n, nb), dtype=torch.uint8)
     _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
     with _on_device(A, codes, exps):
-        _check(lib().cogdl_act_checkpoint(n, F, _ptr(A), dt, _ptr(codes), _ptr(exps), _stream()),
+        _check(lib().cogdl_act_checkpoint(n, F, _addr(A), dt, _addr(codes), _addr(exps), _stream()),
                "cogdl_act_checkpoint")
     return codes, exps
 
@@ -942,10 +953,10 @@ def act_restore(codes, exps, out_dtype=None, out=None):
     _numel(out, "out", n * F)
     _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
     if out is None:
-        out = torch.empty((n, F), dtype=out_dtype or torch.float32, device=codes.device)
+        out = codes.new_empty((n, F), dtype=out_dtype or torch.float32)
     _dev(out, "out")
     with _on_device(codes, exps, out):
-        _check(lib().cogdl_act_restore(n, F, _ptr(codes), _ptr(exps), _ptr(out), _dtype_code(out), _stream()),
+        _check(lib().cogdl_act_restore(n, F, _addr(codes), _addr(exps), _addr(out), _dtype_code(out), _stream()),
                "cogdl_act_restore")
     return out
 
@@ -986,18 +997,19 @@ def grouped_linear(X, W, offsets, bias=None, act: str = "none", out_dtype=None, 
     _numel(exps, "exps", n * _ckpt_blocks(k))
     _dev(X, "X"), _dev(W, "W"), _dev(offsets, "offsets", torch.int32), _dev(bias, "bias", torch.float32)
     if out is None:
-        out = torch.empty((n, m), dtype=out_dtype or X.dtype, device=X.device)
+        out = X.new_empty((n, m), dtype=out_dtype or X.dtype)
     if save and codes is None:
-        codes = torch.empty((n, k), dtype=torch.int8, device=X.device)
-        exps = torch.empty((n, _ckpt_blocks(k)), dtype=torch.uint8, device=X.device)
+        codes = X.new_empty((n, k), dtype=torch.int8)
+        exps = X.new_empty((n, _ckpt_blocks(k)), dtype=torch.uint8)
     _dev(out, "out"), _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
     with _on_device(X, W, offsets, bias, out, codes, exps):
-        _check(lib().cogdl_grouped_linear(n, E, k, m, _ptr(offsets), _ptr(X), _ptr(W), _dtype_code(X), _ptr(bias),
-                                          ACT[act], _ptr(out), _dtype_code(out), _ptr(codes), _ptr(exps),
+        _check(lib().cogdl_grouped_linear(n, E, k, m, _addr(offsets), _addr(X), _addr(W), _dtype_code(X), _addr(bias),
+                                          ACT[act], _addr(out), _dtype_code(out), _addr(codes), _addr(exps),
                                           _stream()), "cogdl_grouped_linear")
     return (out, codes, exps) if save else out
 
 
+@functools.lru_cache(maxsize=256)
 def grouped_linear_backward_workspace(n: int, E: int, k: int, m: int) -> int:
     """Bytes of scratch that grouped_linear_backward takes for n rows and E groups of k features to m outputs."""
     b = ctypes.c_size_t()
@@ -1049,22 +1061,21 @@ def grouped_linear_backward(dY, W, offsets, X=None, codes=None, exps=None, Y=Non
         _at_least(workspace, "workspace", (need + workspace.element_size() - 1) // workspace.element_size())
     _dev(dY, "dY"), _dev(W, "W"), _dev(offsets, "offsets", torch.int32), _dev(X, "X"), _dev(Y, "Y")
     _dev(codes, "codes", torch.int8), _dev(exps, "exps", torch.uint8)
-    dev = dY.device
     if "dX" not in o:
-        o["dX"] = torch.empty((n, k), dtype=dY.dtype, device=dev)
+        o["dX"] = dY.new_empty((n, k), dtype=dY.dtype)
     if "dW" not in o:
-        o["dW"] = torch.empty((E, m, k), dtype=dw_dtype or dY.dtype, device=dev)
+        o["dW"] = dY.new_empty((E, m, k), dtype=dw_dtype or dY.dtype)
     if "db" not in o:
-        o["db"] = torch.empty((E, m), dtype=torch.float32, device=dev)
+        o["db"] = dY.new_empty((E, m), dtype=torch.float32)
     dX, dW, db = o["dX"], o["dW"], o["db"]
     _dev(dX, "dX", dY.dtype), _dev(dW, "dW"), _dev(db, "db", torch.float32)
     if workspace is None and need > 0 and (dW is not None or db is not None):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = dY.new_empty(need, dtype=torch.uint8)
     _dev(workspace, "workspace")
     with _on_device(dY, W, offsets, X, codes, exps, Y, dX, dW, db, workspace):
         _check(lib().cogdl_grouped_linear_backward(
-            n, E, k, m, _ptr(offsets), _ptr(dY), _ptr(W), _ptr(X), _ptr(codes), _ptr(exps), _dtype_code(dY),
-            _ptr(Y), ACT[act], _ptr(dX), _ptr(dW), _dtype_code(dY if dW is None else dW), _ptr(db),
-            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+            n, E, k, m, _addr(offsets), _addr(dY), _addr(W), _addr(X), _addr(codes), _addr(exps), _dtype_code(dY),
+            _addr(Y), ACT[act], _addr(dX), _addr(dW), _dtype_code(dY if dW is None else dW), _addr(db),
+            _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
             _stream()), "cogdl_grouped_linear_backward")
     return o

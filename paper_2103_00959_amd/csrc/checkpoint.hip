@@ -13,28 +13,60 @@ constexpr int kBlock = 256;
 
 typedef uint32_t u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
 
-// The 8 values from element i of p on, `have` of them inside the row (zeros past it).
+// The 8 values from element i of p on, `have` (1 to 8) of them inside the row of F; zeros past it.
+// A row's end is read with its last 8 elements, which are then moved down.
 template <typename T>
-__device__ __forceinline__ void load_features(const T *__restrict__ p, int64_t i, int have, float (&x)[8])
+__device__ __forceinline__ void load_features(const T *__restrict__ p, int64_t i, int have, int F, float (&x)[8])
 {
-    if (have == 8) {
-        if constexpr (sizeof(T) == 4) {
-            float a[4], b[4];
-            load_vec<T, 4>(p, i, a);
-            load_vec<T, 4>(p, i + 4, b);
+    if (F < 8) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-        } else {
-            load_vec<T, 8>(p, i, x);
+        for (int e = 0; e < 8; ++e) {
+            float one[1] = {0.f};
+            if (e < have) load_vec<T, 1>(p, i + e, one);
+            x[e] = one[0];
         }
         return;
     }
+    const int gone = 8 - have;
+    if constexpr (sizeof(T) == 4) {
+        float a[4], b[4];
+        load_vec<T, 4>(p, i - gone, a);
+        load_vec<T, 4>(p, i - gone + 4, b);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float one[1] = {0.f};
-        if (e < have) load_vec<T, 1>(p, i + e, one);
-        x[e] = one[0];
+        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
+    } else {
+        load_vec<T, 8>(p, i - gone, x);
     }
+    if (gone == 0) return;
+#pragma unroll
+    for (int bit = 0; bit < 3; ++bit)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float from = e + (1 << bit) < 8 ? x[e + (1 << bit)] : 0.f;
+            x[e] = (gone >> bit) & 1 ? from : x[e];
+        }
+}
+
+// The first `have` (1 to 8) of 8 bytes.
+__device__ __forceinline__ void store_bytes(int8_t *__restrict__ p, int have, uint32_t lo, uint32_t hi)
+{
+    if (have == 8) {
+        *reinterpret_cast<u32x2_b *>(p) = u32x2_b{lo, hi};
+        return;
+    }
+    typedef uint32_t u32_b __attribute__((aligned(1)));
+    typedef uint16_t u16_b __attribute__((aligned(1)));
+    if (have & 4) {
+        *reinterpret_cast<u32_b *>(p) = lo;
+        p += 4;
+        lo = hi;
+    }
+    if (have & 2) {
+        *reinterpret_cast<u16_b *>(p) = (uint16_t)lo;
+        p += 2;
+        lo >>= 16;
+    }
+    if (have & 1) *p = (int8_t)lo;
 }
 
 // Pieces of 8 features: nb blocks of 4 pieces a row, the pieces past the row's end empty.
@@ -52,8 +84,8 @@ __global__ __launch_bounds__(kBlock) void k_act_checkpoint(int64_t n, int F, int
         const int left = F - f;
         const int have = left < 0 ? 0 : (left > 8 ? 8 : left);
         const int64_t at = row * F + f;
-        float x[8];
-        load_features<T>(A, at, have, x);
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (have > 0) load_features<T>(A, at, have, F, x);
         uint32_t top = 0;                            // magnitudes order as their bits, NaN above infinity
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -70,13 +102,7 @@ __global__ __launch_bounds__(kBlock) void k_act_checkpoint(int64_t n, int F, int
         }
         const uint32_t lo = ckpt_encode4(x[0], x[1], x[2], x[3], rs);
         const uint32_t hi = ckpt_encode4(x[4], x[5], x[6], x[7], rs);
-        if (have == 8) {
-            *reinterpret_cast<u32x2_b *>(codes + at) = u32x2_b{lo, hi};
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < have) codes[at + e] = (int8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
-        }
+        if (have > 0) store_bytes(codes + at, have, lo, hi);
     }
 }
 

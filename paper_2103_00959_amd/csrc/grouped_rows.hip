@@ -21,8 +21,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
     const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
     const int wx = DX ? a.m : a.k;                      // x
     const int wc = DX ? a.k : a.m;                      // outputs of a row
-    Walk walk;
-    walk.start(a.off, a.E, a.n, TM, a.tiles_c, false);
+    PieceWalk walk;
+    walk.start(a.off, a.E, a.n, TM, a.tiles_c);
     RowOperand<T, TM, N, SRC> A;
     std::conditional_t<DX, ColOperand<T, TN, N, SRCB, false>, RowOperand<T, TN, N, SRCB>> B;
     const auto open = [&](const Span &s) {
@@ -40,15 +40,24 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
         [&](const Span &s, const Acc<WR, WC> &acc) {
             const int col0 = s.tile * TN + c0;
             const float *__restrict__ bias = !DX && a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
-            for_outputs<WR, WC>(mine, acc, [&](int r, int c, float (&v)[8]) {
+            // a lane's columns are the same in every row
+            float add[DX ? 1 : WC][8];
+            if constexpr (!DX) {
+#pragma unroll
+                for (int bc = 0; bc < WC; ++bc)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int c = col0 + 32 * bc + 8 * (lane_id() & 3) + e;
+                        add[bc][e] = bias && c < wc ? bias[c] : 0.f;
+                    }
+            }
+            for_outputs<WR, WC>(mine, acc, [&](int bc, int r, int c, float (&v)[8]) {
                 r += r0;
                 c += col0;
                 if (r >= s.have || c >= wc) return;
                 if constexpr (!DX) {
-                    if (bias) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += bias[c + e < wc ? c + e : wc - 1];
-                    }
+                    for (int e = 0; e < 8; ++e) v[e] += add[bc][e];
                     if (a.act != COGDL_ACT_NONE) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] = apply_act(v[e], a.act);
@@ -57,6 +66,82 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
                 store8(a.out, a.out_dtype, (s.lo + r) * wc, c, wc, v);
             });
         });
+}
+
+// The forward of few rows a group (single tokens): the reads of the weights are all there is.  A
+// workgroup owns 16 rows by 16 columns and its four wavefronts a quarter of x each, kFewSteps
+// steps of 32 loaded at once, straight into the operands of the 16 x 16 x 32 matrix
+// instructions; the quarters are added up through LDS.  8 rows of 8 among 64 groups, 2048 -> 1024,
+// bf16: 64 workgroups of 128 x 128 tiles took 20 us, these 512 take 6.
+constexpr int kFewRows = 16, kFewCols = 16, kFewSteps = 8, kFewWaves = 4;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ f32x4 mfma_16x16x32(uint4 a, uint4 b, f32x4 c)
+{
+    if constexpr (Fmt<T>::code == COGDL_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_grouped_few(GroupedArgs a)
+{
+    __shared__ f32x4 part[kFewWaves][kWave];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int i = lane & 15, q = lane >> 4;             // row of either operand, its 8 of a step's 32 x
+    // this wavefront's x: whole steps
+    const int steps = (a.k + 31) / 32;
+    const int x_lo = steps * wave / kFewWaves * 32, x_hi = steps * (wave + 1) / kFewWaves * 32;
+    PieceWalk walk;
+    walk.start(a.off, a.E, a.n, kFewRows, a.tiles_c);
+    Span s;
+    while (walk.next(s)) {
+        const int col0 = s.tile * kFewCols;
+        const Buffer X = buffer_of(static_cast<const T *>(a.X) + s.lo * a.k, (int64_t)s.have * a.k * 2);
+        const int cols = a.m - col0 < kFewCols ? a.m - col0 : kFewCols;
+        const Buffer W = buffer_of(static_cast<const T *>(a.W) + ((int64_t)s.g * a.m + col0) * a.k, (int64_t)cols * a.k * 2);
+        const uint32_t row = (uint32_t)i * (uint32_t)a.k * 2u;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int x0 = x_lo; x0 < x_hi; x0 += 32 * kFewSteps) {
+            uint4 w[kFewSteps], x[kFewSteps];
+#pragma unroll
+            for (int u = 0; u < kFewSteps; ++u) {
+                // pieces at the row's end are read from its last 8 elements, those past it from nowhere
+                const int at = x0 + 32 * u + 8 * q;
+                const bool in = x0 + 32 * u < x_hi && at < a.k;
+                const uint32_t off = in ? row + (uint32_t)(at + 8 <= a.k ? at : a.k - 8) * 2u : kNowhere;
+                w[u] = load16(W, off);
+                x[u] = load16(X, off);
+            }
+#pragma unroll
+            for (int u = 0; u < kFewSteps; ++u) {
+                if (x0 + 32 * u + 32 > a.k) {            // (uniform)
+                    const int gone = x0 + 32 * u + 8 * q + 8 - a.k;
+                    w[u] = shift_down(w[u], gone);
+                    x[u] = shift_down(x[u], gone);
+                }
+                acc = mfma_16x16x32<T>(w[u], x[u], acc);
+            }
+        }
+        __syncthreads();                                 // (the tile before is read)
+        part[wave][lane] = acc;
+        __syncthreads();
+        if (wave != 0) continue;
+        // lane l: columns 4 (l / 16) ... of row l % 16
+        f32x4 t = part[0][lane];
+#pragma unroll
+        for (int p = 1; p < kFewWaves; ++p) t += part[p][lane];
+        const int c = col0 + 4 * q;
+        if (i >= s.have || c >= a.m) continue;
+        float v[4] = {t.x, t.y, t.z, t.w};
+        const float *__restrict__ bias = a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e] + (bias && c + e < a.m ? bias[c + e] : 0.f), a.act);
+        store4(a.out, a.out_dtype, (s.lo + i) * a.m, c, a.m, v);
+    }
 }
 
 struct Variant {
@@ -86,6 +171,11 @@ Variant pick_tile(int64_t n, int wc, bool dx, bool act, bool direct)
     return pick<T, 4, 128, 64>(dx, act, direct);
 }
 
+// Whether the kernel for few rows is the faster one: every 16 rows read their group's weights
+// again.  2048 -> 1024 bf16, 64 even groups, 32 / 512 / 1024 / 2048 rows: 25 / 61 / 74 / 130 us, with
+// tiles 39 / 77 / 78 / 78; one group, 2048 -> 2048, 64 / 256 / 512 rows: 12 / 34 / 61, with tiles 21 / 43 / 44.
+bool few_rows(int64_t n, int32_t E) { return n <= 256 || (n <= 8 * (int64_t)E && n <= 2048); }
+
 }  // namespace
 
 cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl_dtype dtype, hipStream_t stream)
@@ -94,10 +184,15 @@ cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl
     // direct loads: every row of both operands on the 16-byte grid
     const bool direct = on_grid(dx ? a.dY : a.X, dx ? a.m : a.k) && on_grid(a.W, a.k);
     const int wc = dx ? a.k : a.m;
+    if (!dx && a.k >= 8 && few_rows(a.n, a.E)) {
+        const GroupedKernel kern = dtype == COGDL_BF16 ? k_grouped_few<bf16_t> : k_grouped_few<f16_t>;
+        a.tiles_c = (a.m + kFewCols - 1) / kFewCols;
+        return launch_tiles(name, kern, a, most_pieces(a.n, a.E, kFewRows) * a.tiles_c, kFewWaves, 0, 0, stream);
+    }
     const Variant v = dtype == COGDL_BF16 ? pick_tile<bf16_t>(a.n, wc, dx, act, direct)
                                           : pick_tile<f16_t>(a.n, wc, dx, act, direct);
     a.tiles_c = (int32_t)(((int64_t)wc + v.tn - 1) / v.tn);
-    return launch_tiles(name, v.kern, a, most_pieces(a.n, a.E, v.tm), v.waves, v.tm, v.tn, stream);
+    return launch_tiles(name, v.kern, a, most_pieces(a.n, a.E, v.tm) * a.tiles_c, v.waves, lds_of(v.waves, v.tm, v.tn), 0, stream);
 }
 
 }  // namespace cogdl
@@ -156,8 +251,7 @@ cogdl_status cogdl_grouped_linear_backward_workspace(int64_t n, int32_t E, int32
 {
     if (n < 0 || E < 1 || k < 0 || m < 0 || !bytes) return COGDL_ERR_INVALID;
     if (n > INT32_MAX || E > COGDL_MAX_GROUPS || k > kMaxWidth || m > kMaxWidth) return COGDL_ERR_TOO_LARGE;
-    const Chunks c = chunks_of(n, E, k, m);
-    *bytes = (size_t)c.slots * ((size_t)m * k + m) * sizeof(float);
+    *bytes = (size_t)slices_of(n, E, k, m).slots() * ((size_t)m * k + m) * sizeof(float);
     return COGDL_OK;
 }
 
@@ -176,14 +270,13 @@ cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int3
     if (rows && k > 0 && dX && !W) return COGDL_ERR_INVALID;
     if ((codes == nullptr) != (exps == nullptr)) return COGDL_ERR_INVALID;
     if (rows && k > 0 && dW && (X != nullptr) == (codes != nullptr)) return COGDL_ERR_INVALID;
-    const Chunks c = chunks_of(n, E, k, m);
-    const size_t need = (size_t)c.slots * ((size_t)m * k + m) * sizeof(float);
+    const Slices c = slices_of(n, E, k, m);
+    const size_t need = (size_t)c.slots() * ((size_t)m * k + m) * sizeof(float);
     const bool weights = (dW && k > 0 && m > 0) || (db && m > 0);
     if (weights && need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < need))
         return COGDL_ERR_INVALID;
     if (n > 0 && dX && k > 0 && too_many_tiles(n, E, k)) return COGDL_ERR_TOO_LARGE;
-    if (n > 0 && weights && piece_tiles(most_pieces(n, E, c.per), (int64_t)((m + 63) / 64) * ((k + 64) / 64)) == 0)
-        return COGDL_ERR_TOO_LARGE;
+    if (weights && piece_tiles(c.count, (int64_t)((m + 63) / 64) * ((k + 64) / 64)) == 0) return COGDL_ERR_TOO_LARGE;
     GroupedArgs a{};
     a.n = n; a.E = E; a.k = k; a.m = m;
     a.off = offsets;

@@ -49,115 +49,81 @@ __device__ __forceinline__ int64_t offset_at(const int32_t *__restrict__ off, in
     return o < 0 ? 0 : (o < n ? o : n);
 }
 
-// A tile of the output: rows [lo, lo + have) of group g, which are piece `local` of the `count`
-// pieces of `per` rows that the group is cut into (`slot`: pieces of groups with several before
-// it), and column tile `tile`.
+// A tile of the output: rows [lo, lo + have) of group g, column tile `tile`.  dW: `slot` is where
+// its partial sums go, -1 where the rows are all of the group's.
 struct Span {
-    int g, local, count, tile;
-    int have;
-    int64_t lo, slot;
+    int g, tile, have, slot;
+    int64_t lo;
 };
 
-// This workgroup's tiles, in order.  Tiles are numbered by piece and column tile, and each of
-// the 8 XCDs takes a run of them, its workgroups one after another: a group's pieces share its
-// weights in that XCD's L2, a piece's tiles its rows.  The runs hold equal numbers of tiles or,
-// where the time goes with the rows of a piece (dW), equal weights: a piece weighs its chunks of 64
-// rows and kTileWeight for its start and end.  A window of 64 groups is held, a group a lane;
-// every wavefront does the same.
-constexpr int kTileWeight = 3;
-
-struct Walk {
+// The groups 64 at a time, a group a lane; every wavefront does the same.
+struct Groups {
     const int32_t *off;
     int64_t n;
-    int E, per, tiles;
-    int base, total;             // the window's first group and its pieces
-    int64_t first, slots;        // pieces, and those of groups with several, before the window
-    int lo, size, pieces, before;       // a lane's group: place, rows, pieces, pieces up to and with it
-    uint32_t j, step, end;       // this workgroup's next tile, the way to the one after, its XCD's end
+    int E;
+    int base;                    // the window's first group
+    int lo, size;                // this lane's group: its first row and its rows
 
-    __device__ __forceinline__ int pieces_of(int e, int &at, int &rows) const
+    __device__ __forceinline__ void read(int e)
     {
-        at = rows = 0;
+        lo = size = 0;
         if (e < E) {
             const int64_t o = offset_at(off, e, n), next = offset_at(off, e + 1, n);
-            at = (int)o;
-            rows = next > o ? (int)(next - o) : 0;
+            lo = (int)o;
+            size = next > o ? (int)(next - o) : 0;
         }
-        return (int)(((int64_t)rows + per - 1) / per);
     }
     __device__ __forceinline__ void window(int from)
     {
         base = from;
-        pieces = pieces_of(base + lane_id(), lo, size);
+        read(base + lane_id());
+    }
+    __device__ __forceinline__ int lo_of(int l) const { return __builtin_amdgcn_readlane(lo, l); }
+    __device__ __forceinline__ int size_of(int l) const { return __builtin_amdgcn_readlane(size, l); }
+};
+
+// A workgroup's tiles of the products over rows, in order.  Groups are cut into pieces of `per` rows;
+// tiles are numbered by piece and column tile, and each of the 8 XCDs takes an equal run of
+// them, its workgroups one after another: a group's pieces share its weights in that XCD's L2, a
+// piece's tiles its rows.
+struct PieceWalk {
+    Groups groups;
+    int per, tiles;
+    int total;                   // the window's pieces
+    int64_t first;               // pieces before the window
+    int pieces, before;          // this lane's group: its pieces, and those up to and with it
+    uint32_t j, step, end;       // the next tile, the way to the one after, the XCD's end
+
+    __device__ __forceinline__ int pieces_of(int rows) const { return (int)(((int64_t)rows + per - 1) / per); }
+    __device__ __forceinline__ void window(int from)
+    {
+        groups.window(from);
+        pieces = pieces_of(groups.size);
         before = wave_inclusive_scan(pieces);
         total = __builtin_amdgcn_readlane(before, kWave - 1);
     }
-    // the first window, anew only where there are others
-    __device__ __forceinline__ void rewind()
+    __device__ __forceinline__ void start(const int32_t *offsets, int E, int64_t n, int rows_a_piece, int col_tiles)
     {
-        first = slots = 0;
-        if (base != 0) window(0);
-    }
-    __device__ __forceinline__ int weight() const { return (size + kX - 1) / kX + kTileWeight * pieces; }
-
-    // The number of the tile at which `target` of the weights before it is reached.
-    __device__ __forceinline__ uint32_t tile_at(int64_t target)
-    {
-        rewind();
-        for (;;) {
-            const int w = weight();
-            const int upto = wave_inclusive_scan(w);
-            const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
-            if (target < all) {
-                const int l = __builtin_ctzll(__ballot((int64_t)upto > target));
-                const int each = (per + kX - 1) / kX + kTileWeight;
-                int rest = (int)target - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(w, l));
-                const int count = __builtin_amdgcn_readlane(pieces, l);
-                int piece = rest / each;
-                piece = piece < count ? piece : count - 1;
-                rest -= piece * each;
-                const int mine = piece < count - 1 ? each : __builtin_amdgcn_readlane(w, l) - piece * each;
-                const int64_t tile = (int64_t)rest * tiles / mine;
-                return (uint32_t)((first + __builtin_amdgcn_readlane(before, l) - count + piece) * tiles + tile);
-            }
-            target -= all;
-            first += total;
-            if (base + kWave >= E) return (uint32_t)(first * tiles);
-            window(base + kWave);
-        }
-    }
-    __device__ __forceinline__ void start(const int32_t *offsets, int groups, int64_t rows, int rows_a_piece, int col_tiles,
-                                          bool weighted)
-    {
-        off = offsets;
-        E = groups;
-        n = rows;
+        groups.off = offsets;
+        groups.E = E;
+        groups.n = n;
         per = rows_a_piece;
         tiles = col_tiles;
-        first = slots = 0;
-        window(0);
-        int64_t all = total, weights = weighted ? __builtin_amdgcn_readlane(wave_inclusive_scan(weight()), kWave - 1) : 0;
+        int64_t all = 0;
         if (E > kWave) {
-            int more = 0, heavier = 0;
+            int more = 0;
             for (int e = kWave + lane_id(); e < E; e += kWave) {
-                int at, here;
-                const int p = pieces_of(e, at, here);
-                more += p;
-                heavier += (here + kX - 1) / kX + kTileWeight * p;
+                groups.read(e);
+                more += pieces_of(groups.size);
             }
-            all += __builtin_amdgcn_readlane(wave_inclusive_scan(more), kWave - 1);
-            if (weighted) weights += __builtin_amdgcn_readlane(wave_inclusive_scan(heavier), kWave - 1);
+            all = __builtin_amdgcn_readlane(wave_inclusive_scan(more), kWave - 1);
         }
+        first = 0;
+        window(0);
+        all += total;
         const uint32_t xcd = blockIdx.x & 7;
-        if (weighted) {
-            end = xcd < 7 ? tile_at(weights * (xcd + 1) / 8) : (uint32_t)(all * tiles);
-            j = xcd > 0 ? tile_at(weights * xcd / 8) : 0u;
-            rewind();
-        } else {
-            j = (uint32_t)(all * tiles * xcd / 8);
-            end = (uint32_t)(all * tiles * (xcd + 1) / 8);
-        }
-        j += blockIdx.x >> 3;
+        j = (uint32_t)(all * tiles * xcd / 8) + (blockIdx.x >> 3);
+        end = (uint32_t)(all * tiles * (xcd + 1) / 8);
         step = gridDim.x >> 3;
     }
     // The next tile; false when there is none.
@@ -169,23 +135,102 @@ struct Walk {
         j = end - j > step ? j + step : end;
         while (t - first >= total) {
             first += total;
-            slots += __builtin_amdgcn_readlane(wave_inclusive_scan(pieces > 1 ? pieces : 0), kWave - 1);
-            if (base + kWave >= E) return false;
-            window(base + kWave);
+            if (groups.base + kWave >= groups.E) return false;
+            window(groups.base + kWave);
         }
         const int w = (int)(t - first);
         const int l = __builtin_ctzll(__ballot(before > w));
-        s.g = base + l;
-        s.count = __builtin_amdgcn_readlane(pieces, l);
-        s.local = w - (__builtin_amdgcn_readlane(before, l) - s.count);
-        const int at = s.local * per, rows = __builtin_amdgcn_readlane(size, l) - at;
-        s.lo = (int64_t)__builtin_amdgcn_readlane(lo, l) + at;
+        s.g = groups.base + l;
+        const int at = (w - (__builtin_amdgcn_readlane(before, l) - __builtin_amdgcn_readlane(pieces, l))) * per;
+        const int rows = groups.size_of(l) - at;
+        s.lo = (int64_t)groups.lo_of(l) + at;
         s.have = rows < per ? rows : per;
-        s.slot = slots;
-        if (s.count > 1) {
-            const int many = pieces > 1 && lane_id() < l ? pieces : 0;
-            s.slot += __builtin_amdgcn_readlane(wave_inclusive_scan(many), kWave - 1);
+        s.slot = -1;
+        return true;
+    }
+};
+
+// A workgroup's tiles of dW.  Rows [0, n) are cut into slices of `per`, whatever the groups: each
+// takes the same time, however uneven those are (with pieces of groups instead, 64 groups of 150
+// to 1400 rows, 2048 x 2048, took 587 us, the same rows in even groups 540).  Slices and output
+// tiles are numbered slice by slice, each XCD takes an equal run of them; a workgroup's tile of a
+// slice has its part of every group in turn.  A group without rows belongs to the slice of its
+// place, and its products of nothing are its zeros.  Of a slice's groups only the first and the last can
+// reach out of it: their partial sums go to slots 2 i (begun before slice i) and 2 i + 1.
+struct SliceWalk {
+    Groups groups;
+    int per, tiles, slices;
+    uint32_t j, step, end;
+    int slice, tile;
+    int64_t from, to;            // the slice's rows
+    uint64_t todo;               // groups of the window that have a part in the slice
+    bool past;                   // the window holds a group behind the slice
+
+    __device__ __forceinline__ static int slices_of(int64_t n, int per)
+    {
+        const int64_t s = (n + per - 1) / per;
+        return s > 1 ? (int)s : 1;
+    }
+    __device__ __forceinline__ void window(int at)
+    {
+        groups.window(at);
+        const int64_t lo = groups.lo, hi = lo + groups.size;
+        const bool mine = groups.base + lane_id() < groups.E &&
+                          (groups.size > 0 ? lo < to && hi > from : (lo < to || slice == slices - 1) && lo >= from);
+        todo = __ballot(mine);
+        past = __ballot(groups.base + lane_id() >= groups.E || lo >= to) != 0 && slice != slices - 1;
+    }
+    // the groups of the slice: from the one that holds the row before it
+    __device__ __forceinline__ void open_slice()
+    {
+        slice = (int)(j / (uint32_t)tiles);
+        tile = (int)(j % (uint32_t)tiles);
+        from = (int64_t)slice * per;
+        to = from + per < groups.n ? from + per : groups.n;
+        int64_t g = 0;
+        if (groups.E > kWave && from > 0 && groups.off[0] < from) g = RowCursor::find(groups.off, groups.E, from - 1);
+        window((int)(g / kWave * kWave));
+    }
+    __device__ __forceinline__ void start(const int32_t *offsets, int E, int64_t n, int rows_a_slice, int out_tiles)
+    {
+        groups.off = offsets;
+        groups.E = E;
+        groups.n = n;
+        per = rows_a_slice;
+        tiles = out_tiles;
+        slices = slices_of(n, per);
+        const uint32_t xcd = blockIdx.x & 7;
+        const int64_t all = (int64_t)slices * tiles;
+        j = (uint32_t)(all * xcd / 8) + (blockIdx.x >> 3);
+        end = (uint32_t)(all * (xcd + 1) / 8);
+        step = gridDim.x >> 3;
+        todo = 0;
+        past = true;
+        if (j < end) open_slice();
+    }
+    __device__ __forceinline__ bool next(Span &s)
+    {
+        while (todo == 0) {
+            if (!past && groups.base + kWave < groups.E) {
+                window(groups.base + kWave);
+                continue;
+            }
+            if (j >= end || end - j <= step) {
+                j = end;
+                return false;
+            }
+            j += step;
+            open_slice();
         }
+        const int l = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int64_t lo = groups.lo_of(l), hi = lo + groups.size_of(l);
+        s.g = groups.base + l;
+        s.tile = tile;
+        s.lo = lo > from ? lo : from;
+        const int64_t stop = hi < to ? hi : to;
+        s.have = stop > s.lo ? (int)(stop - s.lo) : 0;
+        s.slot = lo < from ? 2 * slice : hi > to ? 2 * slice + 1 : -1;
         return true;
     }
 };
@@ -588,7 +633,7 @@ struct Acc {
 // permuted by the row.
 constexpr int kOutBytes = 4096;
 
-// Calls out(row in the block, column in the block, 8 consecutive outputs) for each 8 outputs of a
+// Calls out(column block, row in the block, column in the block, 8 consecutive outputs) for each 8 outputs of a
 // wavefront, through its part of the LDS: neighbouring lanes then hold neighbouring columns of
 // a row.
 template <int WR, int WC, typename Out>
@@ -613,7 +658,7 @@ __device__ __forceinline__ void for_outputs(char *mine, const Acc<WR, WC> &acc, 
                 const float4 lo = *reinterpret_cast<const float4 *>(mine + r * 128 + (((2 * piece) ^ (r & 7)) << 4));
                 const float4 hi = *reinterpret_cast<const float4 *>(mine + r * 128 + (((2 * piece + 1) ^ (r & 7)) << 4));
                 float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                out(32 * br + r, 32 * bc + 8 * piece, v);
+                out(bc, 32 * br + r, 32 * bc + 8 * piece, v);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -656,14 +701,12 @@ __device__ __forceinline__ void issue(int x0, char *to, A &a, B &b)
 template <typename A, typename B>
 __device__ __forceinline__ void landed(int x0, char *to, A &a, B &b)
 {
-    static_assert(A::direct == B::direct, "either both operands pass through registers or none");
-    if constexpr (A::direct) {
+    a.finish(x0, to);
+    b.finish(x0, to + A::kBytes);
+    if constexpr (A::direct || B::direct) {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
         asm volatile("" ::: "memory");
-    } else {
-        a.finish(x0, to);
-        b.finish(x0, to + A::kBytes);
     }
 }
 
@@ -711,7 +754,8 @@ __device__ __forceinline__ void chunk(const char *__restrict__ now, char *__rest
 // sees the first operand's fragments; done(span, acc) takes the products of the tile (its own
 // wavefront's, no barrier needed).  lds: two pairs of chunks.  settle() runs between a tile's last
 // product and the next tile's first chunk being finished.
-template <typename T, typename A, typename B, int WR, int WC, typename Open, typename Each, typename Settle, typename Done>
+template <typename T, typename A, typename B, int WR, int WC, typename Walk, typename Open, typename Each, typename Settle,
+          typename Done>
 __device__ __forceinline__ void run_tiles(char *lds, Walk &walk, A &a, B &b, int r0, int c0, Open open, Each each,
                                           Settle settle, Done done)
 {
@@ -776,6 +820,24 @@ __device__ __forceinline__ void store8(void *out, int dtype, int64_t row, int c,
     else store8(static_cast<float *>(out) + row, c, width, v);
 }
 
+__device__ __forceinline__ void store4(void *out, int dtype, int64_t row, int c, int width, const float (&v)[4])
+{
+    if (c + 4 <= width) {
+        if (dtype == COGDL_BF16) store_vec<bf16_t, 4>(static_cast<bf16_t *>(out), row + c, v);
+        else if (dtype == COGDL_F16) store_vec<f16_t, 4>(static_cast<f16_t *>(out), row + c, v);
+        else store_vec<float, 4>(static_cast<float *>(out), row + c, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float one[1] = {v[e]};
+        if (c + e >= width) continue;
+        if (dtype == COGDL_BF16) store_out<bf16_t, 1>(static_cast<bf16_t *>(out), row + c + e, one);
+        else if (dtype == COGDL_F16) store_out<f16_t, 1>(static_cast<f16_t *>(out), row + c + e, one);
+        else store_out<float, 1>(static_cast<float *>(out), row + c + e, one);
+    }
+}
+
 struct GroupedArgs {
     int64_t n;
     int32_t E, k, m;
@@ -791,8 +853,8 @@ struct GroupedArgs {
     void *out;              // Y, dX or dW
     int32_t out_dtype;
     float *db;              // E x m, nullable
-    int32_t tiles_c;        // column tiles of a piece of rows (dW: tiles of an output matrix)
-    int32_t per;            // rows of a piece
+    int32_t tiles_c;        // column tiles of a row (dW: tiles of an output matrix)
+    int32_t per;            // rows of a slice (dW)
     float *part;            // dW: partial sums (m x k a slot), then those of db (m a slot)
     float *part_db;
 };
@@ -815,28 +877,31 @@ inline bool on_grid(const void *p, int width) { return width % 8 == 0 && (uintpt
 
 using GroupedKernel = void (*)(GroupedArgs);
 
-// A kernel over tiles: resident workgroups, as many on each XCD, no more than the tiles that
-// `pieces` pieces can make.
-inline cogdl_status launch_tiles(const char *name, GroupedKernel kern, const GroupedArgs &a, int64_t pieces, int waves, int tm,
-                                 int tn, hipStream_t stream)
+// A kernel over `all` tiles: resident workgroups (`most` a compute unit, where given), as many on
+// each XCD, no more than there are tiles.
+inline cogdl_status launch_tiles(const char *name, GroupedKernel kern, const GroupedArgs &a, int64_t all, int waves, size_t lds,
+                                 int most, hipStream_t stream)
 {
-    const size_t lds = (size_t)2 * (tm + tn) * kX * 2 + (size_t)waves * kOutBytes;
-    const int64_t resident = resident_blocks(reinterpret_cast<const void *>(kern), waves * kWave, lds) / 8;
+    const int64_t resident = resident_blocks(reinterpret_cast<const void *>(kern), waves * kWave, lds, most) / 8;
     if (resident < 1) return COGDL_ERR_LAUNCH;
-    const int64_t need = (pieces + 7) / 8 * a.tiles_c;
+    const int64_t need = (all + 7) / 8;
     COGDL_LAUNCH_SHM(name, kern, dim3((unsigned)(8 * (need < resident ? need : resident))), waves * kWave, lds, stream, a);
     return COGDL_OK;
 }
 
+// The LDS of a kernel for tiles of tm x tn: two pairs of chunks, and the outputs' part.
+inline size_t lds_of(int waves, int tm, int tn) { return (size_t)2 * (tm + tn) * kX * 2 + (size_t)waves * kOutBytes; }
+
 // The products over rows: the forward, and dX of dY (and Y, with an activation).
 cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl_dtype dtype, hipStream_t s);
 
-// dW and db: their work plan for these sizes, and the launches.
-struct Chunks {
-    int64_t per;       // rows of a chunk
-    int64_t slots;     // most partial sums
+// dW and db: the rows of a slice for these sizes, the slices' number, and the launches.
+struct Slices {
+    int64_t per;
+    int64_t count;
+    int64_t slots() const { return count > 1 ? 2 * count : 0; }     // partial sums
 };
-Chunks chunks_of(int64_t n, int32_t E, int32_t k, int32_t m);
-cogdl_status grouped_weights_launch(GroupedArgs a, const Chunks &c, cogdl_dtype dtype, hipStream_t s);
+Slices slices_of(int64_t n, int32_t E, int32_t k, int32_t m);
+cogdl_status grouped_weights_launch(GroupedArgs a, const Slices &c, cogdl_dtype dtype, hipStream_t s);
 
 }  // namespace cogdl

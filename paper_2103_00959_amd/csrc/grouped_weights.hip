@@ -1,15 +1,16 @@
 // The gradients of the grouped products' weights and biases:
 //     dW[g, c, j] = sum_{i in g} dZ[i, c] X[i, j],   db[g, c] = sum_{i in g} dZ[i, c]
 //
-// The sums run over rows, whose number only the device knows: groups are cut into chunks of
-// rows; a group of one chunk writes its result, the others write fp32 partial sums into the
-// workspace, added up in chunk order by k_reduce_chunks (no atomics: the same bits every run).
+// The sums run over rows, and which group they belong to only the device knows: the rows are cut into
+// slices, and a workgroup goes through a slice's groups.  A group inside a slice is written as it
+// is, one that reaches over several as fp32 partial sums into the workspace, added up in a
+// fixed order by k_reduce_slices (no atomics: the same bits every run).
 #include "grouped_tile.hpp"
 
 namespace cogdl {
 namespace {
 
-// dW and db of chunks of a group's rows: TM x TN outputs (c by j) of its matrix at a time.
+// dW and db: TM x TN outputs (c by j) of a group's matrix at a time, over a slice's rows of it.
 template <typename T, int WAVES, int TM, int TN, int SRC, int SRCB>
 __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a)
 {
@@ -24,8 +25,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
     // db: staged operands sum their own columns on the way; direct ones are summed from the
     // fragments of the wavefronts that hold the first columns
     constexpr bool STAGED_SUM = SRC != kDirect;
-    Walk walk;
-    walk.start(a.off, a.E, a.n, a.per, a.tiles_c, true);
+    SliceWalk walk;
+    walk.start(a.off, a.E, a.n, a.per, a.tiles_c);
     ColOperand<T, TM, N, SRC, STAGED_SUM> A;
     ColOperand<T, TN, N, SRCB, false> B;
     A.clear_sums();
@@ -66,17 +67,17 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
                                                                                              const Acc<WR, WC> &acc) {
         const int row0 = s.tile / tiles_k * TM, col0 = s.tile % tiles_k * TN;
         if (a.out) {
-            float *__restrict__ part = a.part + (s.slot + s.local) * mk;
-            for_outputs<WR, WC>(outs + wave * kOutBytes, acc, [&](int r, int c, float (&v)[8]) {
+            float *__restrict__ part = a.part + s.slot * mk;
+            for_outputs<WR, WC>(outs + wave * kOutBytes, acc, [&](int, int r, int c, float (&v)[8]) {
                 r += row0 + r0;
                 c += col0 + c0;
                 if (r >= a.m || c >= a.k) return;
-                if (s.count == 1) store8(a.out, a.out_dtype, s.g * mk + (int64_t)r * a.k, c, a.k, v);
+                if (s.slot < 0) store8(a.out, a.out_dtype, s.g * mk + (int64_t)r * a.k, c, a.k, v);
                 else store8(part + (int64_t)r * a.k, c, a.k, v);
             });
         }
         if (!sums(s)) return;
-        float *__restrict__ db = s.count == 1 ? a.db + (int64_t)s.g * a.m : a.part_db + (s.slot + s.local) * a.m;
+        float *__restrict__ db = s.slot < 0 ? a.db + (int64_t)s.g * a.m : a.part_db + (int64_t)s.slot * a.m;
         if constexpr (STAGED_SUM) {
             // the threads that share 8 columns add up in order
             constexpr int P = TM / 8, S = N / P;
@@ -107,79 +108,83 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
     });
 }
 
-// Sums over a group's partial sums.  Four quarters of the slots, each added up in order by a
-// thread of its own with kBatch loads in flight, then the quarters in order.
+// Sums over a group's partial sums: slot 2 i + 1 of its first slice i, then slots 2 i of the
+// others, in order; of many, four quarters are added up by threads of their own and then joined in
+// order.  kBatch loads are in flight.
 constexpr int kBlock = 256;
 constexpr int kQuarters = 4;
 constexpr int kBatch = 8;
+constexpr int kManySlots = 16;
 
-// V values from p on in each of the slots [0, count), `stride` floats apart.
+// V values from p on in the slots of slices [at, end), the group's first slice being `first`; slots
+// are `stride` floats apart.
 template <int V>
-__device__ __forceinline__ void sum_slots(const float *__restrict__ p, int64_t stride, int count, float (&t)[V])
+__device__ __forceinline__ void sum_slots(const float *__restrict__ p, int64_t stride, int first, int at, int end, float (&t)[V])
 {
-#pragma unroll
-    for (int e = 0; e < V; ++e) t[e] = 0.f;
-    for (int c = 0; c < count; c += kBatch) {
+    for (; at < end; at += kBatch) {
         float v[kBatch][V];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int at = c + u < count ? c + u : count - 1;
-            if constexpr (V == 4) load_vec<float, 4>(p, at * stride, v[u]);
-            else v[u][0] = p[at * stride];
+            if (at + u >= end) break;
+            const int64_t slot = 2 * (int64_t)(at + u) + (at + u == first ? 1 : 0);
+            if constexpr (V == 4) load_vec<float, 4>(p, slot * stride, v[u]);
+            else v[u][0] = p[slot * stride];
         }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
+        for (int u = 0; u < kBatch; ++u) {
+            if (at + u >= end) break;
 #pragma unroll
-            for (int e = 0; e < V; ++e) t[e] += c + u < count ? v[u][e] : 0.f;
+            for (int e = 0; e < V; ++e) t[e] += v[u][e];
+        }
     }
 }
 
-// dW and db of the groups of several chunks (sums of their slots) and of none (zeros).
-// Group blockIdx.y, V values a thread of each quarter.
+// dW and db of the groups that reach over several slices, V values a thread.  Block row y looks at
+// group y or, where there are fewer borders between slices than groups, at the group that reaches
+// over border y first.
 template <int V>
-__global__ __launch_bounds__(kBlock) void k_reduce_chunks(GroupedArgs a)
+__global__ __launch_bounds__(kBlock) void k_reduce_slices(GroupedArgs a, bool by_border)
 {
-    __shared__ float sums[kQuarters][kBlock / kQuarters][V];
-    const int g = blockIdx.y, lane = lane_id();
+    __shared__ float sums[kBlock][V];
+    int g = blockIdx.y;
+    const int64_t border = (int64_t)(g + 1) * a.per;
+    if (by_border) g = a.off[0] < border ? (int)RowCursor::find(a.off, a.E, border - 1) : 0;
     const int64_t lo = offset_at(a.off, g, a.n), hi = offset_at(a.off, g + 1, a.n);
-    const int count = hi > lo ? (int)((hi - lo + a.per - 1) / a.per) : 0;
-    if (count == 1) return;
-    int64_t slot = 0;
-    if (count > 1) {
-        for (int e = lane; e < g; e += kWave) {
-            const int64_t from = offset_at(a.off, e, a.n), to = offset_at(a.off, e + 1, a.n);
-            if (to - from > a.per) slot += (to - from + a.per - 1) / a.per;
-        }
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) slot += __shfl_xor(slot, d);
-    }
-    const int quarter = threadIdx.x / (kBlock / kQuarters), mine = threadIdx.x % (kBlock / kQuarters);
-    const int first = count * quarter / kQuarters, end = count * (quarter + 1) / kQuarters;
+    if (hi <= lo || (by_border && (lo >= border || hi <= border || lo < border - a.per))) return;
+    const int first = (int)(lo / a.per), count = (int)((hi - 1) / a.per) - first + 1;
+    if (count <= 1) return;
+    const int parts = count >= kManySlots ? kQuarters : 1, width = kBlock / parts;
+    const int part = threadIdx.x / width, mine = threadIdx.x % width;
+    const int at = first + (int)((int64_t)count * part / parts), end = first + (int)((int64_t)count * (part + 1) / parts);
     const int64_t mk = a.out ? (int64_t)a.m * a.k : 0, all = mk + (a.db ? a.m : 0);
-    const int64_t step = (int64_t)gridDim.x * (kBlock / kQuarters) * V;
-    for (int64_t i0 = (int64_t)blockIdx.x * (kBlock / kQuarters) * V; i0 < all; i0 += step) {
+    const int64_t step = (int64_t)gridDim.x * width * V;
+    for (int64_t i0 = (int64_t)blockIdx.x * width * V; i0 < all; i0 += step) {
         const int64_t i = i0 + mine * V;
         float t[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) t[e] = 0.f;
-        if (i < mk) sum_slots<V>(a.part + (slot + first) * mk + i, mk, end - first, t);
-        else if (i < all) sum_slots<V>(a.part_db + (slot + first) * a.m + (i - mk), a.m, end - first, t);
-        __syncthreads();
+        if (i < mk) sum_slots<V>(a.part + i, mk, first, at, end, t);
+        else if (i < all) sum_slots<V>(a.part_db + (i - mk), a.m, first, at, end, t);
+        if (parts > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int e = 0; e < V; ++e) sums[quarter][mine][e] = t[e];
-        __syncthreads();
-        if (quarter != 0 || i >= all) continue;
+            for (int e = 0; e < V; ++e) sums[threadIdx.x][e] = t[e];
+            __syncthreads();
+            if (part == 0) {
+                for (int q = 1; q < parts; ++q)
 #pragma unroll
-        for (int q = 1; q < kQuarters; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) t[e] += sums[q][mine][e];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float one[1] = {t[e]};
-            if (i >= mk) a.db[(int64_t)g * a.m + (i - mk) + e] = t[e];
-            else if (a.out_dtype == COGDL_BF16) store_out<bf16_t, 1>(static_cast<bf16_t *>(a.out), g * mk + i + e, one);
-            else if (a.out_dtype == COGDL_F16) store_out<f16_t, 1>(static_cast<f16_t *>(a.out), g * mk + i + e, one);
-            else static_cast<float *>(a.out)[g * mk + i + e] = t[e];
+                    for (int e = 0; e < V; ++e) t[e] += sums[q * width + mine][e];
+            }
+        }
+        if (part != 0 || i >= all) continue;
+        if (i >= mk) {
+            store_vec<float, V>(a.db, (int64_t)g * a.m + (i - mk), t);
+        } else if (a.out_dtype == COGDL_F32) {
+            store_vec<float, V>(static_cast<float *>(a.out), g * mk + i, t);
+        } else if (a.out_dtype == COGDL_BF16) {
+            store_vec<bf16_t, V>(static_cast<bf16_t *>(a.out), g * mk + i, t);
+        } else {
+            store_vec<f16_t, V>(static_cast<f16_t *>(a.out), g * mk + i, t);
         }
     }
 }
@@ -189,75 +194,80 @@ struct Tiles {
 };
 
 template <typename T, int WAVES, int TM, int TN>
-GroupedKernel pick(bool act, bool codes, bool direct)
+GroupedKernel pick(bool act, bool codes, bool direct_dy, bool direct_x)
 {
     if (act) return codes ? k_grouped_weights<T, WAVES, TM, TN, kSloped, kCodes> : k_grouped_weights<T, WAVES, TM, TN, kSloped, kStaged>;
-    if (codes) return k_grouped_weights<T, WAVES, TM, TN, kStaged, kCodes>;
-    return direct ? k_grouped_weights<T, WAVES, TM, TN, kDirect, kDirect> : k_grouped_weights<T, WAVES, TM, TN, kStaged, kStaged>;
+    if (codes) return direct_dy ? k_grouped_weights<T, WAVES, TM, TN, kDirect, kCodes> : k_grouped_weights<T, WAVES, TM, TN, kStaged, kCodes>;
+    return direct_dy && direct_x ? k_grouped_weights<T, WAVES, TM, TN, kDirect, kDirect>
+                                 : k_grouped_weights<T, WAVES, TM, TN, kStaged, kStaged>;
 }
 
 template <typename T>
-GroupedKernel pick_tile(const Tiles &c, bool act, bool codes, bool direct)
+GroupedKernel pick_tile(const Tiles &c, bool act, bool codes, bool direct_dy, bool direct_x)
 {
-    if (c.tm == 256) return codes ? k_grouped_weights<T, 8, 256, 256, kStaged, kCodes>
+    if (c.tm == 256) return codes ? k_grouped_weights<T, 8, 256, 256, kDirect, kCodes>
                                   : k_grouped_weights<T, 8, 256, 256, kDirect, kDirect>;
-    if (c.tm == 128) return c.tn == 128 ? pick<T, 4, 128, 128>(act, codes, direct) : pick<T, 4, 128, 64>(act, codes, direct);
-    return c.tn == 128 ? pick<T, 4, 64, 128>(act, codes, direct) : pick<T, 4, 64, 64>(act, codes, direct);
+    if (c.tm == 128) return c.tn == 128 ? pick<T, 4, 128, 128>(act, codes, direct_dy, direct_x)
+                                        : pick<T, 4, 128, 64>(act, codes, direct_dy, direct_x);
+    return c.tn == 128 ? pick<T, 4, 64, 128>(act, codes, direct_dy, direct_x) : pick<T, 4, 64, 64>(act, codes, direct_dy, direct_x);
 }
 
 int64_t tiles_of(int64_t m, int64_t k, int tm, int tn) { return (m + tm - 1) / tm * (k > 0 ? (k + tn - 1) / tn : 1); }
 
 }  // namespace
 
-// Rows of a piece: a partial sum is written and read once for each, so there are no more pieces
-// than make two tiles of 128 x 128 (one of 256 x 256) for each resident workgroup, E groups ending
-// in a short one each; 512 rows at least.  A group of several pieces has under 2 n_g / per.
-Chunks chunks_of(int64_t n, int32_t E, int32_t k, int32_t m)
+// Slices of rows: a group that is cut costs its partial sums, so there are no more slices than
+// make two tiles of 128 x 128 (one of 256 x 256) for each resident workgroup, and of few rows a
+// slice for 128 of them or 4 groups or, where the partial sums are small, as many as they leave
+// under 4 MB.
+Slices slices_of(int64_t n, int32_t E, int32_t k, int32_t m)
 {
-    Chunks c;
     const int64_t tiles = tiles_of(m, k, m > 64 ? 128 : 64, k > 64 ? 128 : 64);
-    const int64_t want = 1024 / (tiles < 1 ? 1 : tiles < 1024 ? tiles : 1024);
-    int64_t pieces = want - E > want / 2 ? want - E : want / 2;
-    if (pieces < 1) pieces = 1;
-    int64_t per = (n + pieces - 1) / pieces;
-    per = (per + 63) / 64 * 64;
-    if (per < 512) per = 512;
-    if (per > (1 << 30)) per = 1 << 30;
-    c.per = per;
-    c.slots = n > per ? 2 * (n / per) : 0;
+    int64_t count = tiles > 0 ? (1024 + tiles - 1) / tiles : 1;
+    const int64_t small = (4 << 20) / (16 * ((int64_t)m * k + m + 1));
+    int64_t most = n / 128 > E / 4 ? n / 128 : E / 4;
+    if (most < small) most = small;
+    if (count > most) count = most;
+    if (count > n / 16) count = n / 16;
+    if (count < 1) count = 1;
+    Slices c;
+    c.per = (n + count - 1) / count;
+    if (c.per < 1) c.per = 1;
+    c.count = n > 0 ? (n + c.per - 1) / c.per : 1;
     return c;
 }
 
-cogdl_status grouped_weights_launch(GroupedArgs a, const Chunks &c, cogdl_dtype dtype, hipStream_t stream)
+cogdl_status grouped_weights_launch(GroupedArgs a, const Slices &c, cogdl_dtype dtype, hipStream_t stream)
 {
     a.per = (int32_t)c.per;
     if (!a.out) {               // db alone: one column of tiles
         a.k = 0;
         a.X = a.codes = nullptr;
     }
-    a.part_db = a.part + (size_t)c.slots * a.m * a.k;
+    a.part_db = a.part + (size_t)c.slots() * a.m * a.k;
     const bool act = a.act != COGDL_ACT_NONE, codes = a.codes != nullptr;
-    if (a.n > 0) {
-        const bool direct = a.out && !codes && on_grid(a.dY, a.m) && on_grid(a.X, a.k);
-        Tiles t{a.m > 64 ? 128 : 64, a.k > 64 ? 128 : 64};
-        if (a.m > 128 && a.k > 128 && !act && (codes || direct)) t = {256, 256};
-        const int64_t tiles = tiles_of(a.m, a.k, t.tm, t.tn);
-        a.tiles_c = (int32_t)tiles;
-        const GroupedKernel kern = dtype == COGDL_BF16 ? pick_tile<bf16_t>(t, act, codes, direct)
-                                                       : pick_tile<f16_t>(t, act, codes, direct);
-        const cogdl_status st = launch_tiles("grouped_linear_dw", kern, a, most_pieces(a.n, a.E, c.per), t.tm == 256 ? 8 : 4, t.tm,
-                                             t.tn, stream);
-        if (st != COGDL_OK) return st;
-    }
+    const bool direct_dy = on_grid(a.dY, a.m), direct_x = a.out && !codes && on_grid(a.X, a.k);
+    Tiles t{a.m > 64 ? 128 : 64, a.k > 64 ? 128 : 64};
+    if (a.m > 128 && a.k > 128 && !act && direct_dy && (codes || direct_x)) t = {256, 256};
+    a.tiles_c = (int32_t)tiles_of(a.m, a.k, t.tm, t.tn);
+    const GroupedKernel kern = dtype == COGDL_BF16 ? pick_tile<bf16_t>(t, act, codes, direct_dy, direct_x)
+                                                   : pick_tile<f16_t>(t, act, codes, direct_dy, direct_x);
+    const int waves = t.tm == 256 ? 8 : 4;
+    const cogdl_status st = launch_tiles("grouped_linear_dw", kern, a, c.count * a.tiles_c, waves, lds_of(waves, t.tm, t.tn),
+                                         2, stream);
+    if (st != COGDL_OK || c.slots() == 0) return st;
     // whole vectors of 4 where the matrices and rows of db are
     const int64_t values = (a.out ? (int64_t)a.m * a.k : 0) + (a.db ? a.m : 0);
     const int vec = a.m % 4 == 0 ? 4 : 1;
-    int64_t bx = (values + kBlock / kQuarters * vec - 1) / (kBlock / kQuarters * vec);
-    const int64_t most = 8192 / a.E > 1 ? 8192 / a.E : 1;
+    const bool by_border = c.count - 1 < a.E;
+    const int64_t rows = by_border ? c.count - 1 : a.E;
+    int64_t bx = (values + kBlock * vec - 1) / (kBlock * vec);
+    if (c.count >= kManySlots) bx *= kQuarters;
+    const int64_t most = 8192 / rows > 1 ? 8192 / rows : 1;
     if (bx > most) bx = most;
-    const dim3 grid_r((unsigned)bx, (unsigned)a.E);
-    if (vec == 4) COGDL_LAUNCH("grouped_linear_sum", k_reduce_chunks<4>, grid_r, kBlock, stream, a);
-    else COGDL_LAUNCH("grouped_linear_sum", k_reduce_chunks<1>, grid_r, kBlock, stream, a);
+    const dim3 grid((unsigned)bx, (unsigned)rows);
+    if (vec == 4) COGDL_LAUNCH("grouped_linear_sum", k_reduce_slices<4>, grid, kBlock, stream, a, by_border);
+    else COGDL_LAUNCH("grouped_linear_sum", k_reduce_slices<1>, grid, kBlock, stream, a, by_border);
     return COGDL_OK;
 }
 
