@@ -36,7 +36,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
     };
     char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
     run_tiles<T, decltype(A), decltype(B), WR, WC>(
-        lds, walk, A, B, r0, c0, open, [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
+        lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < wc; },
+        [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
         [&](const Span &s, const Acc<WR, WC> &acc) {
             const int col0 = s.tile * TN + c0;
             const float *__restrict__ bias = !DX && a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;

@@ -724,40 +724,45 @@ __device__ __forceinline__ void meet()
 // finished here, or the next tile's first.  `next` and `now` never overlap, which the compiler has
 // to know to keep loads in flight under the reads.  A step's fragments are read while the matrix
 // cores work on the step before, those of the next chunk's first step behind the barrier under
-// this one's last.
+// this one's last.  A wavefront whose outputs all lie past the tile's end (not `busy`) leaves the
+// matrix cores to the others.
 template <typename T, typename A, typename B, int WR, int WC, typename Start, typename Each>
-__device__ __forceinline__ void chunk(const char *__restrict__ now, char *__restrict__ next, A &a, B &b, int x1, int r0, int c0,
-                                      Fragments<WR, WC> (&f)[2], Acc<WR, WC> &acc, Start start, Each each)
+__device__ __forceinline__ void chunk(const char *__restrict__ now, char *__restrict__ next, A &a, B &b, int x1, bool busy,
+                                      int r0, int c0, Fragments<WR, WC> (&f)[2], Acc<WR, WC> &acc, Start start, Each each)
 {
     constexpr int S = kX / 16;
     start(next);
+    if (busy) {
 #pragma unroll
-    for (int s = 0; s + 1 < S; ++s) {
-        f[(s + 1) & 1].template read<A, B>(now, r0, c0, s + 1);
-        __builtin_amdgcn_sched_barrier(0);       // (the reads start before the step's products, not among the last)
-        each(f[s & 1].a);
-        step<T>(f[s & 1], acc);
+        for (int s = 0; s + 1 < S; ++s) {
+            f[(s + 1) & 1].template read<A, B>(now, r0, c0, s + 1);
+            __builtin_amdgcn_sched_barrier(0);       // (the reads start before the step's products, not among the last)
+            each(f[s & 1].a);
+            step<T>(f[s & 1], acc);
+        }
     }
     // lgkmcnt(0), for f[1]: behind the branch the compiler would wait for the next chunk's reads with it
     __builtin_amdgcn_s_waitcnt(0xc07f);
     if (x1 > 0) {
         landed(x1, next, a, b);
         meet();
-        f[0].template read<A, B>(next, r0, c0, 0);
+        if (busy) f[0].template read<A, B>(next, r0, c0, 0);
         __builtin_amdgcn_sched_barrier(0);
     }
-    each(f[1].a);
-    step<T>(f[1], acc);
+    if (busy) {
+        each(f[1].a);
+        step<T>(f[1], acc);
+    }
 }
 
 // The tiles of a workgroup.  open(span) makes the operands a and b those of a tile; each(span, fa)
 // sees the first operand's fragments; done(span, acc) takes the products of the tile (its own
 // wavefront's, no barrier needed).  lds: two pairs of chunks.  settle() runs between a tile's last
 // product and the next tile's first chunk being finished.
-template <typename T, typename A, typename B, int WR, int WC, typename Walk, typename Open, typename Each, typename Settle,
-          typename Done>
-__device__ __forceinline__ void run_tiles(char *lds, Walk &walk, A &a, B &b, int r0, int c0, Open open, Each each,
-                                          Settle settle, Done done)
+template <typename T, typename A, typename B, int WR, int WC, typename Walk, typename Open, typename Busy, typename Each,
+          typename Settle, typename Done>
+__device__ __forceinline__ void run_tiles(char *lds, Walk &walk, A &a, B &b, int r0, int c0, Open open, Busy busy,
+                                          Each each, Settle settle, Done done)
 {
     constexpr int kPair = A::kBytes + B::kBytes;
     Span s, ahead;
@@ -773,11 +778,12 @@ __device__ __forceinline__ void run_tiles(char *lds, Walk &walk, A &a, B &b, int
         acc.clear();
         meet();
         f[0].template read<A, B>(now, r0, c0, 0);
+        const bool mine = busy(s);
         int x1 = kX, width1 = 0;
 #pragma unroll 1
         do {
             const bool last = x1 >= width;
-            chunk<T>(now, next, a, b, last ? 0 : x1, r0, c0, f, acc,
+            chunk<T>(now, next, a, b, last ? 0 : x1, mine, r0, c0, f, acc,
                      [&](char *to) {
                          if (last && more) width1 = open(ahead);
                          if (!last || more) issue(last ? 0 : x1, to, a, b);

@@ -39,6 +39,10 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
                s.tile % tiles_k * TN, a.k, s.have, 0, false);
         return s.have;
     };
+    // (db comes from the wavefronts of the first columns, whatever k)
+    const auto busy = [&](const Span &s) {
+        return s.tile / tiles_k * TM + r0 < a.m && (c0 == 0 || s.tile % tiles_k * TN + c0 < a.k);
+    };
     float fsum[STAGED_SUM ? 1 : WR], colsum[STAGED_SUM ? 8 : 1];
 #pragma unroll
     for (int i = 0; i < (STAGED_SUM ? 1 : WR); ++i) fsum[i] = 0.f;
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
         }
     };
     char *const outs = lds + 2 * (TM + TN) * kX * 2;
-    run_tiles<T, decltype(A), decltype(B), WR, WC>(lds, walk, A, B, r0, c0, open, each, settle, [&](const Span &s,
+    run_tiles<T, decltype(A), decltype(B), WR, WC>(lds, walk, A, B, r0, c0, open, busy, each, settle, [&](const Span &s,
                                                                                              const Acc<WR, WC> &acc) {
         const int row0 = s.tile / tiles_k * TM, col0 = s.tile % tiles_k * TN;
         if (a.out) {
