@@ -11,8 +11,6 @@ namespace {
 
 constexpr int kBlock = 256;
 
-typedef uint32_t u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
-
 // The 8 values from element i of p on, `have` (1 to 8) of them inside the row of F; zeros past it.
 // A row's end is read with its last 8 elements, which are then moved down.
 template <typename T>
@@ -47,28 +45,6 @@ __device__ __forceinline__ void load_features(const T *__restrict__ p, int64_t i
         }
 }
 
-// The first `have` (1 to 8) of 8 bytes.
-__device__ __forceinline__ void store_bytes(int8_t *__restrict__ p, int have, uint32_t lo, uint32_t hi)
-{
-    if (have == 8) {
-        *reinterpret_cast<u32x2_b *>(p) = u32x2_b{lo, hi};
-        return;
-    }
-    typedef uint32_t u32_b __attribute__((aligned(1)));
-    typedef uint16_t u16_b __attribute__((aligned(1)));
-    if (have & 4) {
-        *reinterpret_cast<u32_b *>(p) = lo;
-        p += 4;
-        lo = hi;
-    }
-    if (have & 2) {
-        *reinterpret_cast<u16_b *>(p) = (uint16_t)lo;
-        p += 2;
-        lo >>= 16;
-    }
-    if (have & 1) *p = (int8_t)lo;
-}
-
 // Pieces of 8 features: nb blocks of 4 pieces a row, the pieces past the row's end empty.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_act_checkpoint(int64_t n, int F, int nb, const T *__restrict__ A,
@@ -95,13 +71,9 @@ __global__ __launch_bounds__(kBlock) void k_act_checkpoint(int64_t n, int F, int
         top = group_reduce(top, 4, [](uint32_t u, uint32_t v) { return u > v ? u : v; });
         const int b = ckpt_exponent<T>(top);
         if ((t & 3) == 0) exps[blk] = (uint8_t)b;
-        const float rs = b == kCkptBad ? 0.f : __uint_as_float((uint32_t)(254 - b) << 23);
-        if (b == kCkptBad) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        }
-        const uint32_t lo = ckpt_encode4(x[0], x[1], x[2], x[3], rs);
-        const uint32_t hi = ckpt_encode4(x[4], x[5], x[6], x[7], rs);
+        const CkptScale sc = ckpt_encode_scale(b);
+        const uint32_t lo = ckpt_encode4(x[0], x[1], x[2], x[3], sc);
+        const uint32_t hi = ckpt_encode4(x[4], x[5], x[6], x[7], sc);
         if (have > 0) store_bytes(codes + at, have, lo, hi);
     }
 }

@@ -34,15 +34,52 @@ __device__ __forceinline__ int ckpt_exponent(uint32_t max_bits)
     return b < CkptRange<T>::lo ? CkptRange<T>::lo : (b > CkptRange<T>::hi ? CkptRange<T>::hi : b);
 }
 
-// 4 codes of 4 features, the first in the low byte; rs = 2^(127 - b), 0 for a bad block.
-__device__ __forceinline__ uint32_t ckpt_encode4(float a, float b, float c, float d, float rs)
+// A block's way from values to codes: 2^(127 - b), and the value of code 127 (a bad block: zeros).
+struct CkptScale {
+    float inverse, limit;
+};
+
+__device__ __forceinline__ CkptScale ckpt_encode_scale(int b)
+{
+    if (b == kCkptBad) return {0.f, 0.f};
+    return {__uint_as_float((uint32_t)(254 - b) << 23), 127.f * __uint_as_float((uint32_t)b << 23)};
+}
+
+// 4 codes of 4 features, the first in the low byte.  Adding 1.5 2^23 rounds to a whole number
+// (to nearest even), which is then the low bits of the sum; the limit comes first, as a median,
+// which also makes zeros of the infinities and NaN of a bad block.
+__device__ __forceinline__ uint32_t ckpt_encode4(float a, float b, float c, float d, CkptScale s)
 {
     const auto one = [&](float x) {
-        return (uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(x * rs), -127.f, 127.f);
+        return __float_as_uint(fmaf(__builtin_amdgcn_fmed3f(x, -s.limit, s.limit), s.inverse, 12582912.f));
     };
     const uint32_t lo = __builtin_amdgcn_perm(one(b), one(a), 0x0c0c0400u);
     const uint32_t hi = __builtin_amdgcn_perm(one(d), one(c), 0x0c0c0400u);
-    return lo | (hi << 16);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+// The first `have` (1 to 8) of 8 bytes.
+typedef uint32_t u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
+
+__device__ __forceinline__ void store_bytes(int8_t *__restrict__ p, int have, uint32_t lo, uint32_t hi)
+{
+    if (have >= 8) {
+        *reinterpret_cast<u32x2_b *>(p) = u32x2_b{lo, hi};
+        return;
+    }
+    typedef uint32_t u32_b __attribute__((aligned(1)));
+    typedef uint16_t u16_b __attribute__((aligned(1)));
+    if (have & 4) {
+        *reinterpret_cast<u32_b *>(p) = lo;
+        p += 4;
+        lo = hi;
+    }
+    if (have & 2) {
+        *reinterpret_cast<u16_b *>(p) = (uint16_t)lo;
+        p += 2;
+        lo >>= 16;
+    }
+    if (have & 1) *p = (int8_t)lo;
 }
 
 // The 4 values of 4 codes (exact: 7 bits times a power of two).

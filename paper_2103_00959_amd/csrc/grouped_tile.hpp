@@ -6,9 +6,9 @@
 // An operand lies in memory with x along its rows ("row" operands: X and W of the forward, dZ of
 // dX) or down its rows ("col" operands: W of dX, both of dW).  A row operand's matrix fragments
 // are 16-byte LDS reads, a col operand's the LDS reads that transpose 4 x 16 elements.  Operands
-// whose rows all lie on the 16-byte grid go from memory to LDS directly; the others, and those
-// that are computed on the way (an activation's slope, a decoded checkpoint), pass through
-// registers.
+// whose rows all lie on the 4-byte grid (even widths) go from memory to LDS directly; the others,
+// and those that are computed on the way (an activation's slope, a decoded checkpoint), pass
+// through registers.
 //
 // Workgroups are resident and take tile after tile: a tile's first chunk is loaded under the last
 // products of the tile before, whose stores drain under this one's.  (A workgroup a tile, on one
@@ -394,8 +394,9 @@ constexpr uint32_t kNowhere = (uint32_t)kBufferMaxBytes;
 // ------------------------------------------------------------- operands
 // An operand's chunks on their way from memory to LDS: issue() starts the loads of the pieces
 // this thread brings, finish() writes those that wait in registers.  N threads.  x
-// past the end are zero: loads leave the buffer there, and staged pieces at a row's end are
-// read from its last 8 elements and shifted down, so that every piece lies inside or outside.
+// past the end are zero: loads leave the buffer there; a row operand's direct piece that reaches
+// past its row's end is trimmed in LDS by trim(), once it has landed; staged pieces at a row's end
+// are read from its last 8 elements and shifted down, so that each lies inside or outside.
 
 enum Source { kDirect, kStaged, kSloped, kCodes };
 
@@ -479,6 +480,18 @@ struct RowOperand {
             }
         }
     }
+    __device__ __forceinline__ void trim(int x0, char *tile)
+    {
+        if constexpr (direct) {
+            const int keep = width - (x0 + piece() * 8);
+            if (x0 + kX <= width || keep <= 0 || keep >= 8) return;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                uint32_t *const w = reinterpret_cast<uint32_t *>(tile + ((int)threadIdx.x + q * N) * 16);
+                for (int d = keep / 2; d < 4; ++d) w[d] = 0u;       // (even widths)
+            }
+        }
+    }
     __device__ __forceinline__ static uint4 fragment(const char *tile, int idx0, int s) { return row_fragment(tile, idx0, s); }
 };
 
@@ -522,7 +535,8 @@ struct ColOperand {
         act = a;
         nb = (w + kCkptBlock - 1) / kCkptBlock;
         at = c0 + piece() * 8;
-        from = at + 8 <= w ? at : w >= 8 ? w - 8 : 0;
+        // (direct pieces stay in place: what they hold past the row's end is no output's)
+        from = direct || at + 8 <= w ? at : w >= 8 ? w - 8 : 0;
         ragged = c0 + C > w;
         sums = want_sums;
     }
@@ -608,6 +622,7 @@ struct ColOperand {
             }
         }
     }
+    __device__ __forceinline__ void trim(int, char *) {}
     __device__ __forceinline__ static uint4 fragment(const char *tile, int idx0, int s) { return col_fragment<C>(tile, idx0, s); }
 };
 
@@ -707,6 +722,8 @@ __device__ __forceinline__ void landed(int x0, char *to, A &a, B &b)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
         asm volatile("" ::: "memory");
+        a.trim(x0, to);
+        b.trim(x0, to + A::kBytes);
     }
 }
 
@@ -878,8 +895,9 @@ inline unsigned piece_tiles(int64_t pieces, int64_t tiles)
 // Widths: the byte offsets inside a tile of 256 rows (or a chunk of 64) are 32 bits.
 constexpr int kMaxWidth = 1 << 22;
 
-// Whether direct loads take rows of `width` 16-bit elements from p on.
-inline bool on_grid(const void *p, int width) { return width % 8 == 0 && (uintptr_t)p % 16 == 0; }
+// Whether direct loads take rows of `width` 16-bit elements from p on: buffer loads of 16 bytes want
+// 4-byte addresses, and count the buffer's end in 4 bytes.
+inline bool on_grid(const void *p, int width) { return width % 2 == 0 && (uintptr_t)p % 4 == 0; }
 
 using GroupedKernel = void (*)(GroupedArgs);
 
