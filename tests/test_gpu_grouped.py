@@ -497,3 +497,112 @@ def test_elements_past_32_bits():
     p.check_backward({"dX": o["dX"][-tail:], "dW": o["dW"][1:], "db": o["db"][1:]})
     back = cg.act_restore(codes, exps, out_dtype=torch.bfloat16)
     assert torch.equal(back[-tail:].cpu().double(), p.Xk)
+
+
+@pytest.mark.parametrize("codes", [False, True], ids=["input", "8bit"])
+@pytest.mark.parametrize("seed", range(4))
+def test_groups_across_slices(seed, codes):
+    """Uneven groups over several windows of 64, empty ones anywhere, rows of no group at both ends: groups that
+    lie inside a slice of rows, reach over one border or over many."""
+    g = torch.Generator().manual_seed(seed)
+    E = (150, 64, 65, 9)[seed]
+    sizes = (torch.rand(E, generator=g) ** 6 * 2500).int()
+    sizes[torch.rand(E, generator=g) < 0.3] = 0
+    sizes[-1 if seed % 2 else 0] = 0
+    k, m = ((24, 40), (33, 17), (130, 72), (264, 300))[seed]
+    p = Problem(sizes.tolist(), k, m, ("bf16", "f16")[seed % 2], ("relu", "none")[seed % 2], before=7 * seed,
+                behind=300 * seed, codes=codes, seed=seed)
+    p.check_forward(p.forward())
+    o = p.backward(dw_dtype=torch.float32)
+    p.check_backward(o)
+    again = p.backward(dw_dtype=torch.float32)
+    rows = slice(int(p.offsets[0]), int(p.offsets[-1]))
+    assert torch.equal(o["dX"][rows], again["dX"][rows])
+    assert torch.equal(o["dW"], again["dW"]) and torch.equal(o["db"], again["db"])
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "elu"])
+@pytest.mark.parametrize("k,m", [(3, 2), (2, 5), (7, 64), (6, 200), (64, 7), (300, 3), (5, 6)])
+def test_narrow_rows(k, m, act):
+    """Rows of under 8 elements in either operand, through both forms of the input."""
+    for codes in (False, True):
+        for dt in ("bf16", "f16"):
+            p = Problem([700, 0, 90, 1], k, m, dt, act, codes=codes, seed=k)
+            p.check_forward(p.forward())
+            p.check_backward(p.backward(dw_dtype=torch.float32))
+
+
+@pytest.mark.parametrize("shift", [1, 2, 4])
+@pytest.mark.parametrize("k,m", [(64, 72), (130, 300), (47, 33), (256, 264)])
+def test_operands_at_any_alignment(k, m, shift):
+    """Operands that start off the 16-byte, the 4-byte grid, with other values around them."""
+    def off(t):
+        buf = torch.full((t.numel() + 16,), float("nan"), dtype=t.dtype, device="cuda") if t.is_floating_point() else \
+            torch.full((t.numel() + 16,), 99, dtype=t.dtype, device="cuda")
+        v = buf[shift:shift + t.numel()].view(t.shape)
+        v.copy_(t)
+        return v
+
+    for codes in (False, True):
+        p = Problem([400, 3, 0, 300], k, m, "bf16", "none", codes=codes)
+        p.dev = lambda t: None if t is None else off(t) if t.dtype in (torch.bfloat16, torch.int8, torch.uint8) else t.cuda()
+        p.check_forward(p.forward())
+        p.check_backward(p.backward(dw_dtype=torch.float32))
+
+
+def test_no_rows_at_all():
+    W = torch.randn(3, 40, 24, device="cuda").bfloat16()
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    X, dY = W.new_empty((0, 24)), W.new_empty((0, 40))
+    Y, codes, exps = cg.grouped_linear(X, W, off, save=True)
+    assert Y.shape == (0, 40) and codes.shape == (0, 24) and exps.shape == (0, 1)
+    o = cg.grouped_linear_backward(dY, W, off, X=X, out={"dW": torch.full_like(W, 3.0)})
+    assert o["dX"].shape == (0, 24) and (o["dW"] == 0).all() and (o["db"] == 0).all()
+    # rows, but none of a group: the gradients are zero too
+    X, dY = torch.randn(500, 24, device="cuda").bfloat16(), torch.randn(500, 40, device="cuda").bfloat16()
+    o = cg.grouped_linear_backward(dY, W, off, X=X, out={"dW": torch.full_like(W, 3.0), "dX": torch.full_like(X, 2.0)})
+    assert (o["dW"] == 0).all() and (o["db"] == 0).all() and (o["dX"] == 2.0).all()
+
+
+def test_no_features_or_no_outputs():
+    """k = 0: the activation of the bias, and db; m = 0: a gradient of zeros."""
+    off = offsets_of([3, 0, 5]).cuda()
+    bias = torch.randn(3, 20, device="cuda")
+    Y = cg.grouped_linear(torch.empty(8, 0, dtype=torch.bfloat16, device="cuda"),
+                          torch.empty(3, 20, 0, dtype=torch.bfloat16, device="cuda"), off, bias, "relu", out_dtype=torch.float32)
+    assert torch.equal(Y, bias[[0, 0, 0, 2, 2, 2, 2, 2]].relu())
+    dY = torch.randn(8, 20, device="cuda").bfloat16()
+    o = cg.grouped_linear_backward(dY, torch.empty(3, 20, 0, dtype=torch.bfloat16, device="cuda"), off,
+                                   X=torch.empty(8, 0, dtype=torch.bfloat16, device="cuda"))
+    d = dY.cpu().double()
+    for g, (a, b) in enumerate(((0, 3), (3, 3), (3, 8))):
+        close(o["db"][g], d[a:b].sum(0), (b - a) * STEP * d[a:b].abs().sum(0), f"db of group {g}")
+    o = cg.grouped_linear_backward(dY[:, :0].contiguous(), torch.empty(3, 0, 16, dtype=torch.bfloat16, device="cuda"), off,
+                                   X=torch.empty(8, 16, dtype=torch.bfloat16, device="cuda"))
+    assert (o["dX"] == 0).all()
+
+
+def test_two_captured_graphs_with_workspaces_of_their_own():
+    """Two captured backward passes replayed one after another and interleaved, eager work between."""
+    ps = [Problem([4000, 0, 2500], 72, 64, "bf16", seed=s, codes=True) for s in (5, 6)]
+    ins = [[p.dev(t) for t in (p.dY, p.W, p.offsets, p.codes, p.exps)] for p in ps]
+
+    def call(i):
+        dY, W, off, c, e = ins[i]
+        return cg.grouped_linear_backward(dY, W, off, codes=c, exps=e, dw_dtype=torch.float32)
+
+    wanted = [call(0), call(1)]
+    torch.cuda.synchronize()
+    graphs, held = [], []
+    for i in (0, 1):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            held.append(call(i))
+    for order in ((0, 1), (1, 0), (0, 0, 1), (1, 1, 0)):
+        for i in order:
+            graphs[i].replay()
+        call(0)
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            for name in wanted[i]:
+                assert torch.equal(held[i][name], wanted[i][name]), (order, i, name)
