@@ -477,8 +477,10 @@ cogdl_status cogdl_act_restore(int64_t n, int32_t F, const int8_t *codes, const 
  * [offsets[0], offsets[E]) belong to no group: Y keeps what it held there.
  * codes and exps, both or neither: also write the 8-bit checkpoint of X that
  * cogdl_act_checkpoint would (rows of no group: written or not), for the
- * backward pass.  1 <= E <= COGDL_MAX_GROUPS, n < 2^31 (COGDL_ERR_TOO_LARGE
- * past either).
+ * backward pass.  1 <= E <= COGDL_MAX_GROUPS, n < 2^31, k and m at most 2^22
+ * (COGDL_ERR_TOO_LARGE past these, and where n rows of that many columns make
+ * 2^31 tiles of outputs).  Any alignment of the operands and outputs is right;
+ * rows of an even number of elements on the 4-byte grid are fastest.
  * ---------------------------------------------------------------------- */
 #define COGDL_MAX_GROUPS 4096
 
@@ -506,7 +508,7 @@ cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m,
  * fp32 accumulation, in a fixed order.  workspace: device scratch for partial
  * sums, at least the size that cogdl_grouped_linear_backward_workspace reports
  * (0 for few rows: NULL is then accepted), 16-byte aligned; its contents are
- * clobbered, and calls in flight together need one each.
+ * clobbered, and calls in flight together need one each.  Limits as above.
  * ---------------------------------------------------------------------- */
 cogdl_status cogdl_grouped_linear_backward_workspace(int64_t n, int32_t E, int32_t k, int32_t m,
                                                      size_t *bytes);

@@ -606,3 +606,69 @@ def test_two_captured_graphs_with_workspaces_of_their_own():
         for i in (0, 1):
             for name in wanted[i]:
                 assert torch.equal(held[i][name], wanted[i][name]), (order, i, name)
+
+
+@pytest.mark.parametrize("codes", [False, True], ids=["input", "8bit"])
+def test_the_widest_rows(codes):
+    """2^22 features: byte offsets inside a tile reach 2^31.  Whole numbers, so that every sum is exact."""
+    n, k, m = 300, 2 ** 22, 136
+    g = torch.Generator(device="cuda").manual_seed(2)
+
+    def digits(*s):
+        return torch.randint(-1, 2, s, generator=g, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+
+    X, W, off = digits(n, k), digits(1, m, k), offsets_of([n]).cuda()
+    kept = {"X": X}
+    if codes:
+        Y, c, e = cg.grouped_linear(X, W, off, out_dtype=torch.float32, save=True)
+        kept = {"codes": c, "exps": e}
+    else:
+        Y = cg.grouped_linear(X, W, off, out_dtype=torch.float32)
+    ref = torch.zeros(n, m, device="cuda")
+    for a in range(0, k, 2 ** 18):
+        ref += X[:, a:a + 2 ** 18].float() @ W[0, :, a:a + 2 ** 18].float().t()
+    assert torch.equal(Y, ref)
+    dY = digits(n, m)
+    o = cg.grouped_linear_backward(dY, W, off, **kept, dw_dtype=torch.float32)
+    for a in range(0, k, 2 ** 18):
+        assert torch.equal(o["dX"][:, a:a + 2 ** 18].float(), dY.float() @ W[0, :, a:a + 2 ** 18].float())
+        assert torch.equal(o["dW"][0, :, a:a + 2 ** 18], dY.float().t() @ X[:, a:a + 2 ** 18].float())
+    # and as outputs: 2^22 of them a row
+    V = W.view(1, k, m)
+    Z = cg.grouped_linear(dY, V, off)
+    for a in range(0, k, 2 ** 18):
+        assert torch.equal(Z[:, a:a + 2 ** 18].float(), dY.float() @ V[0, a:a + 2 ** 18].float().t())
+    o = cg.grouped_linear_backward(X, V, off, X=dY, dw_dtype=torch.float32)
+    ref = torch.zeros(n, m, device="cuda")
+    for a in range(0, k, 2 ** 18):
+        ref += X[:, a:a + 2 ** 18].float() @ V[0, a:a + 2 ** 18].float()
+        assert torch.equal(o["dW"][0, a:a + 2 ** 18], X[:, a:a + 2 ** 18].float().t() @ dY.float())
+    assert torch.equal(o["dX"].float(), ref.to(torch.bfloat16).float())
+    assert torch.equal(o["db"][0], X.float().sum(0))
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+@pytest.mark.parametrize("k,m", [(64, 72), (130, 300), (47, 33), (260, 4), (4, 264)])
+def test_outputs_at_any_alignment(k, m, shift):
+    """Outputs off the 16-byte grid, in storage that holds other values before and behind them."""
+    p = Problem([400, 3, 0, 300, 5000], k, m, "bf16", "none")
+    held = {}
+
+    def off(name, shape, dt):
+        size = int(np.prod(shape))
+        buf = held[name] = torch.full((size + 8,), 77.0, dtype=dt, device="cuda")
+        return buf[shift:shift + size].view(shape)
+
+    for y in ("bf16", "f16", "f32"):
+        out = off("Y", (p.n, m), DT[y])
+        p.check_forward(p.forward(out=out))
+        few = Problem([20, 0, 1], k, m, "bf16", "none")
+        few.check_forward(few.forward(out=off("few", (few.n, m), DT[y])))
+        for name in ("Y", "few"):
+            assert (held[name][:shift] == 77).all() and (held[name][shift - 8:] == 77).all()
+    for dt in (torch.bfloat16, torch.float32):
+        o = {"dX": off("dX", (p.n, k), torch.bfloat16), "dW": off("dW", (p.E, m, k), dt),
+             "db": off("db", (p.E, m), torch.float32)}
+        p.check_backward(p.backward(out=o))
+        for name in o:
+            assert (held[name][:shift] == 77).all() and (held[name][shift - 8:] == 77).all()

@@ -161,3 +161,13 @@ def test_grouped_backward_sizes():
                       workspace=torch.zeros(need - 1, dtype=torch.uint8)), "workspace has")
     with pytest.raises(ValueError):
         B(dY, W, off, X=X, act="gelu")
+
+
+def test_widths_past_the_largest(L):
+    wide, size = 2 ** 22 + 1, ctypes.c_size_t()
+    for k, m in ((wide, 8), (8, wide)):
+        assert L.cogdl_grouped_linear(8, 2, k, m, FAKE, FAKE, FAKE, BF16, None, 0, FAKE, BF16, None, None,
+                                      None) == TOO_LARGE
+        assert L.cogdl_grouped_linear_backward_workspace(8, 2, k, m, ctypes.byref(size)) == TOO_LARGE
+        assert L.cogdl_grouped_linear_backward(8, 2, k, m, FAKE, FAKE, FAKE, FAKE, None, None, BF16, None, 0, FAKE,
+                                               FAKE, BF16, FAKE, None, 0, None) == TOO_LARGE
