@@ -182,7 +182,7 @@ bool few_rows(int64_t n, int32_t E) { return n <= 256 || (n <= 8 * (int64_t)E &&
 cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl_dtype dtype, hipStream_t stream)
 {
     const bool act = dx && a.act != COGDL_ACT_NONE;
-    // direct loads: every row of both operands on the 16-byte grid
+    // direct loads: every row of both operands on the 4-byte grid
     const bool direct = on_grid(dx ? a.dY : a.X, dx ? a.m : a.k) && on_grid(a.W, a.k);
     const int wc = dx ? a.k : a.m;
     if (!dx && a.k >= 8 && few_rows(a.n, a.E)) {
