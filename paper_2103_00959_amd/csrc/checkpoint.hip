@@ -2,7 +2,9 @@
 //
 // A lane holds 8 consecutive features, a block of 32 four adjacent lanes: the block's
 // maximum is two DPP steps, and a wavefront reads 64 x 16 (fp32: 32) bytes and writes 64 x 8
-// of codes.  Both ways are bound by memory.
+// of codes.  Both ways are bound by memory: 2.4M x 256 bf16 351 us there and 361 back (1.86 GB each, 5.3
+// and 5.2 TB/s; a large copy 4.9), 169343 x 300 fp32 55 and 49 us (256 MB, 4.6 and 5.2 TB/s).  Small calls
+// by their launch: 2708 x 1433 bf16 5 us each.
 #include "checkpoint.hpp"
 #include "internal.hpp"
 

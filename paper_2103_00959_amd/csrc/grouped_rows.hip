@@ -10,6 +10,12 @@ namespace cogdl {
 namespace {
 
 // WAVES wavefronts, tiles of TM rows by TN columns; DX: the gradient.  The operands from SRC, SRCB.
+// Bound by the matrix cores' clock where both widths are large: one group of 32768 rows, 2048 ->
+// 2048 bf16, 263 us (1.05 PFLOP/s; a large library product reaches 1.43), 229 without the loads
+// from memory and 211 without the reads of LDS too.  64 groups of 280 to 2244 rows there: 375, a quarter of
+// the tiles' rows are no group's.  Bound by memory elsewhere: 2.5M rows of 90 groups, 64 -> 64, fp16
+// to fp32, 183 us (5.2 TB/s); dX of 2.4M rows, 128 -> 256, 378 us (4.9 TB/s); rows of 602 bf16 start
+// off the cache lines: 232965 of them to 128 outputs 120 us (2.8 TB/s).
 template <typename T, int WAVES, int TM, int TN, bool DX, int SRC, int SRCB>
 __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
 {
@@ -162,10 +168,20 @@ Variant pick(bool dx, bool act, bool direct)
     return {k, WAVES, TM, TN};
 }
 
-template <typename T>
-Variant pick_tile(int64_t n, int wc, bool dx, bool act, bool direct)
+// Tiles of 256 x 256 read each operand from the L2s half as often as those of 128 x 128, and hold a whole
+// compute unit: for groups that fill them, and where there are enough for half of the chip.  2048 -> 2048
+// bf16, dX with 256 and with 128: one group of 32768 rows 265 and 340 us, of 300 rows 48 and 32; 64
+// groups, 8192 rows 212 and 172, 16384 rows 216 and 231, 32768 rows 377 and 410 (forward 376 and 417);
+// 8 groups of 2.4M rows, 128 -> 256: 381 and 434.
+bool wide_tiles(int64_t n, int32_t E, int wc)
 {
-    if (wc > 128 && n >= 256 && direct && !act)
+    return wc > 128 && n >= 256 * (int64_t)E && n / 256 * ((wc + 255) / 256) > 128;
+}
+
+template <typename T>
+Variant pick_tile(int64_t n, int32_t E, int wc, bool dx, bool act, bool direct)
+{
+    if (direct && !act && wide_tiles(n, E, wc))
         return {dx ? k_grouped_rows<T, 8, 256, 256, true, kDirect, kDirect>
                    : k_grouped_rows<T, 8, 256, 256, false, kDirect, kDirect>, 8, 256, 256};
     if (wc > 64) return pick<T, 4, 128, 128>(dx, act, direct);
@@ -190,8 +206,8 @@ cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl
         a.tiles_c = (a.m + kFewCols - 1) / kFewCols;
         return launch_tiles(name, kern, a, most_pieces(a.n, a.E, kFewRows) * a.tiles_c, kFewWaves, 0, 0, stream);
     }
-    const Variant v = dtype == COGDL_BF16 ? pick_tile<bf16_t>(a.n, wc, dx, act, direct)
-                                          : pick_tile<f16_t>(a.n, wc, dx, act, direct);
+    const Variant v = dtype == COGDL_BF16 ? pick_tile<bf16_t>(a.n, a.E, wc, dx, act, direct)
+                                          : pick_tile<f16_t>(a.n, a.E, wc, dx, act, direct);
     a.tiles_c = (int32_t)(((int64_t)wc + v.tn - 1) / v.tn);
     return launch_tiles(name, v.kern, a, most_pieces(a.n, a.E, v.tm) * a.tiles_c, v.waves, lds_of(v.waves, v.tm, v.tn), 0, stream);
 }

@@ -672,3 +672,26 @@ def test_outputs_at_any_alignment(k, m, shift):
         p.check_backward(p.backward(out=o))
         for name in o:
             assert (held[name][:shift] == 77).all() and (held[name][shift - 8:] == 77).all()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "elu"])
+@pytest.mark.parametrize("k,m", [(40, 264), (264, 40), (130, 300), (520, 258), (33, 1000)])
+def test_many_rows_of_wide_outputs(k, m, act):
+    """Enough rows for the widest tiles, in groups that fill them, miss them by one, or have none."""
+    sizes = [300, 0, 1, 255, 257, 33500, 0, 128, 129]
+    for dt in ("bf16", "f16"):
+        p = Problem(sizes, k, m, dt, act, before=3, behind=5)
+        p.check_forward(p.forward())
+        o = p.backward(dw_dtype=torch.float32)
+        p.check_backward(o)
+        again = p.backward(dw_dtype=torch.float32)
+        rows = slice(3, 3 + sum(sizes))
+        assert torch.equal(o["dX"][rows], again["dX"][rows]) and torch.equal(o["dW"], again["dW"])
+
+
+@pytest.mark.parametrize("E,rows", [(1, 255), (1, 256), (1, 257), (30, 8), (30, 9), (3, 20000)])
+def test_borders_of_the_kernels_for_few_and_many_rows(E, rows):
+    for k, m in ((64, 520), (520, 64), (7, 300), (8, 300)):
+        p = Problem([rows] * E, k, m, "bf16", "none")
+        p.check_forward(p.forward(out_dtype=torch.float32))
+        p.check_backward(p.backward())
