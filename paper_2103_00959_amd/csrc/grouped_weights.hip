@@ -117,13 +117,14 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
 }
 
 // Sums over a group's partial sums: slot 2 i + 1 of its first slice i, then slots 2 i of the
-// others, in order; of many, four quarters are added up by threads of their own and then joined in
-// order.  kBatch loads are in flight.  Bound by memory where the partial sums are many: 64 groups over 4
+// others, in order; of many, 4 or 16 parts are added up by threads of their own and then joined in
+// order (one group of 1024 slices, 19 x 19: 50 us with 4 parts, 16 with 16).  kBatch loads are in flight.  Bound by memory where the partial sums are many: 64 groups over 4
 // slices, 2048 x 2048, 28 us (100 MB read).
 constexpr int kBlock = 256;
-constexpr int kQuarters = 4;
 constexpr int kBatch = 8;
-constexpr int kManySlots = 16;
+
+// Parts of so many slots.
+__host__ __device__ inline int parts_of(int64_t slots) { return slots >= 64 ? 16 : slots >= 16 ? 4 : 1; }
 
 // V values from p on in the slots of slices [at, end), the group's first slice being `first`; slots
 // are `stride` floats apart.
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void k_reduce_slices(GroupedArgs a, bool by
     if (hi <= lo || (by_border && (lo >= border || hi <= border || lo < border - a.per))) return;
     const int first = (int)(lo / a.per), count = (int)((hi - 1) / a.per) - first + 1;
     if (count <= 1) return;
-    const int parts = count >= kManySlots ? kQuarters : 1, width = kBlock / parts;
+    const int parts = parts_of(count), width = kBlock / parts;
     const int part = threadIdx.x / width, mine = threadIdx.x % width;
     const int at = first + (int)((int64_t)count * part / parts), end = first + (int)((int64_t)count * (part + 1) / parts);
     const int64_t mk = a.out ? (int64_t)a.m * a.k : 0, all = mk + (a.db ? a.m : 0);
@@ -228,7 +229,8 @@ int64_t tiles_of(int64_t m, int64_t k, int tm, int tn) { return (m + tm - 1) / t
 // Slices of rows: a group that is cut costs its partial sums, so there are no more slices than
 // make two tiles of 128 x 128 (one of 256 x 256) for each resident workgroup, and of few rows a
 // slice for 128 of them or 4 groups or, where the partial sums are small, as many as they leave
-// under 4 MB.
+// under 4 MB.  Slices have 16 rows or more, or 4 groups each: groups without rows take their turn too (46 rows
+// in 253 groups, 104 x 28: 487 us in 2 slices, 85 in 46).
 Slices slices_of(int64_t n, int32_t E, int32_t k, int32_t m)
 {
     const int64_t tiles = tiles_of(m, k, m > 64 ? 128 : 64, k > 64 ? 128 : 64);
@@ -237,7 +239,9 @@ Slices slices_of(int64_t n, int32_t E, int32_t k, int32_t m)
     int64_t most = n / 128 > E / 4 ? n / 128 : E / 4;
     if (most < small) most = small;
     if (count > most) count = most;
-    if (count > n / 16) count = n / 16;
+    const int64_t rows = n / 16 > E / 4 ? n / 16 : E / 4;
+    if (count > rows) count = rows;
+    if (count > n) count = n;
     if (count < 1) count = 1;
     Slices c;
     c.per = (n + count - 1) / count;
@@ -273,7 +277,7 @@ cogdl_status grouped_weights_launch(GroupedArgs a, const Slices &c, cogdl_dtype 
     const bool by_border = c.count - 1 < a.E;
     const int64_t rows = by_border ? c.count - 1 : a.E;
     int64_t bx = (values + kBlock * vec - 1) / (kBlock * vec);
-    if (c.count >= kManySlots) bx *= kQuarters;
+    bx *= parts_of(c.count);
     const int64_t most = 8192 / rows > 1 ? 8192 / rows : 1;
     if (bx > most) bx = most;
     const dim3 grid((unsigned)bx, (unsigned)rows);

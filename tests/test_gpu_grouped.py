@@ -695,3 +695,17 @@ def test_borders_of_the_kernels_for_few_and_many_rows(E, rows):
         p = Problem([rows] * E, k, m, "bf16", "none")
         p.check_forward(p.forward(out_dtype=torch.float32))
         p.check_backward(p.backward())
+
+
+@pytest.mark.parametrize("n,E,k,m", [(46, 253, 104, 28), (40, 47, 664, 888), (1, 5, 144, 280), (9, 4096, 8, 8),
+                                     (5000, 4096, 24, 16), (141671, 1, 19, 19), (141671, 3, 20, 20)])
+def test_slices_of_few_rows_and_of_many(n, E, k, m):
+    """More groups than rows, so that most have none; and sums over a thousand slices."""
+    g = torch.Generator().manual_seed(n)
+    sizes = torch.bincount(torch.randint(0, E, (n,), generator=g) ** 2 // E, minlength=E)
+    for codes in (False, True):
+        p = Problem(sizes.tolist(), k, m, "bf16", "none", codes=codes)
+        dW = torch.full((E, m, k), float("nan"), device="cuda")
+        o = p.backward(out={"dW": dW})
+        p.check_backward(o)
+        assert torch.equal(o["dW"], p.backward(dw_dtype=torch.float32)["dW"])
