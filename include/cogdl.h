@@ -473,8 +473,10 @@ cogdl_status cogdl_act_restore(int64_t n, int32_t F, const int8_t *codes, const 
  * offsets: device int32, E + 1 entries, 0 <= offsets[0] <= ... <= offsets[E]
  * <= n (read on the device; entries outside [0, n] count as its ends).  X: n x k,
  * W: E x m x k, both bf16 or both fp16 (dtype); bias: fp32 E x m or NULL;
- * Y: n x m of y_dtype.  fp32 accumulation on the matrix cores.  Rows outside
- * [offsets[0], offsets[E]) belong to no group: Y keeps what it held there.
+ * Y: n x m of y_dtype.  fp32 accumulation on the matrix cores.  NaN stays NaN
+ * under every act, under ReLU too (the epilogues of cogdl_linear and of the
+ * aggregations make it 0).  Rows outside [offsets[0], offsets[E]) belong to no
+ * group: Y keeps what it held there.
  * codes and exps, both or neither: also write the 8-bit checkpoint of X that
  * cogdl_act_checkpoint would (rows of no group: written or not), for the
  * backward pass.  1 <= E <= COGDL_MAX_GROUPS, n < 2^31, k and m at most 2^22

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
                     for (int e = 0; e < 8; ++e) v[e] += add[bc][e];
                     if (a.act != COGDL_ACT_NONE) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = apply_act(v[e], a.act);
+                        for (int e = 0; e < 8; ++e) v[e] = output_act(v[e], a.act);
                     }
                 }
                 store8(a.out, a.out_dtype, (s.lo + r) * wc, c, wc, v);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_grouped_few(GroupedArgs a
         float v[4] = {t.x, t.y, t.z, t.w};
         const float *__restrict__ bias = a.bias ? a.bias + (int64_t)s.g * a.m : nullptr;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e] + (bias && c + e < a.m ? bias[c + e] : 0.f), a.act);
+        for (int e = 0; e < 4; ++e) v[e] = output_act(v[e] + (bias && c + e < a.m ? bias[c + e] : 0.f), a.act);
         store4(a.out, a.out_dtype, (s.lo + i) * a.m, c, a.m, v);
     }
 }

@@ -318,6 +318,14 @@ __device__ __forceinline__ uint4 decode8(uint2 codes, uint32_t b)
                       pack2<T>(hi[2], hi[3]));
 }
 
+// The activation of the outputs: apply_act's, but that ReLU leaves NaN as it is (there it becomes 0), so
+// that a row gone wrong stays visible, as it does under ELU and in a decoded checkpoint.
+__device__ __forceinline__ float output_act(float v, int act)
+{
+    if (act == COGDL_ACT_RELU) return v <= 0.f ? 0.f : v;
+    return apply_act(v, act);
+}
+
 // d act'(y) from the activation's output y: relu 1 where y > 0 and 0 elsewhere, ELU 1 where
 // y > 0 and y + 1 = exp(v) elsewhere.
 __device__ __forceinline__ float act_grad(float d, float y, int act)

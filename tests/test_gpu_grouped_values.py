@@ -1,0 +1,40 @@
+"""GPU tests of the grouped products on values that an epilogue or a number format could lose.  No tolerances: an
+output is compared bit for bit."""
+import pytest
+import torch
+
+import paper_2103_00959_amd as cg
+from test_gpu_grouped import Problem
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+# (group sizes, k, m): the kernel for few rows; tiles of 64 and 128 columns, loaded directly and through registers;
+# rows of under 8 features; tiles of 256 x 256
+FORWARDS = [([9, 0, 30], 64, 40), ([300, 0, 41], 64, 40), ([300, 0, 41], 72, 200), ([300, 0, 41], 45, 130),
+            ([300, 0, 41], 5, 33), ([17000, 0, 16500], 64, 264)]
+
+
+def same(a, b):
+    """Equal bit for bit, any NaN like any other."""
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a[~torch.isnan(a)], b[~torch.isnan(b)])
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "elu"])
+@pytest.mark.parametrize("sizes,k,m", FORWARDS)
+def test_nan_stays_under_an_activation(sizes, k, m, act):
+    """A NaN feature makes its row of Y NaN, a NaN weight or bias its column of the group's rows; the others keep
+    their bits."""
+    for dt, out in (("bf16", torch.float32), ("f16", torch.float16)):
+        p = Problem(sizes, k, m, dt, act)
+        want = p.forward(out_dtype=out)
+        last, r, c = p.E - 1, sizes[0] - 1, m // 2
+        first = int(p.offsets[last])
+        p.X[r, k - 1] = NAN
+        want[r] = NAN
+        p.W[last, c, 0] = NAN
+        want[first:, c] = NAN
+        p.bias[last, m - 1] = NAN
+        want[first:, m - 1] = NAN
+        assert same(p.forward(out_dtype=out), want)
