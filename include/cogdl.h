@@ -495,8 +495,9 @@ cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m,
 /* ------------------------------------------------------------------------
  * Gradients of cogdl_grouped_linear (with one group, of cogdl_linear) for
  * dY = dL/dY, n x m of dtype.  With dZ = dY * act'(Y), where the activation's
- * slope follows from its output Y (n x m of dtype; ReLU Y > 0, ELU 1 where
- * Y > 0 and Y + 1 elsewhere; NULL for COGDL_ACT_NONE):
+ * slope follows from its output Y (n x m of dtype; ReLU 0 where Y <= 0 and 1
+ * elsewhere, where Y is NaN too; ELU 1 where Y > 0 and Y + 1 elsewhere; NULL for
+ * COGDL_ACT_NONE):
  *   dX[i, j]    = sum_c dZ[i, c] * W[g, c, j]            (n x k of dtype)
  *   dW[g, c, j] = sum_{i in group g} dZ[i, c] * X[i, j]  (E x m x k, fp32 or dtype)
  *   db[g, c]    = sum_{i in group g} dZ[i, c]            (E x m fp32)

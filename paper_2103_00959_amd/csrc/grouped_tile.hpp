@@ -326,11 +326,11 @@ __device__ __forceinline__ float output_act(float v, int act)
     return apply_act(v, act);
 }
 
-// d act'(y) from the activation's output y: relu 1 where y > 0 and 0 elsewhere, ELU 1 where
-// y > 0 and y + 1 = exp(v) elsewhere.
+// d act'(y) from the activation's output y: ReLU 0 where y <= 0 and 1 elsewhere (NaN among it: a NaN
+// of d stays), ELU 1 where y > 0 and y + 1 = exp(v) elsewhere.
 __device__ __forceinline__ float act_grad(float d, float y, int act)
 {
-    if (act == COGDL_ACT_RELU) return y > 0.f ? d : 0.f;
+    if (act == COGDL_ACT_RELU) return y <= 0.f ? 0.f : d;
     return y > 0.f ? d : d * (y + 1.f);
 }
 

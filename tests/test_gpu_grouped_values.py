@@ -38,3 +38,40 @@ def test_nan_stays_under_an_activation(sizes, k, m, act):
         p.bias[last, m - 1] = NAN
         want[first:, m - 1] = NAN
         assert same(p.forward(out_dtype=out), want)
+
+
+@pytest.mark.parametrize("codes", [False, True], ids=["input", "8bit"])
+@pytest.mark.parametrize("sizes,k,m", FORWARDS)
+def test_slope_of_nan(sizes, k, m, codes):
+    """ReLU's slope is 0 where Y <= 0 and 1 elsewhere: a NaN of Y lets dY through, a NaN of dY stays where Y > 0 or
+    is NaN, and goes where Y <= 0.  ELU's slope of NaN is NaN."""
+    for dt in ("bf16", "f16"):
+        p = Problem(sizes, k, m, dt, "relu", codes=codes)
+        g, r = p.E - 1, int(p.offsets[p.E - 1]) + 7
+        cols = torch.tensor([0, m // 2, m - 1])
+        p.Y[r, cols] = 1.0
+        want = p.backward(dw_dtype=torch.float32)
+        p.Y[r, cols] = NAN
+        got = p.backward(dw_dtype=torch.float32)
+        for name in want:
+            assert same(got[name], want[name]), name
+        p.dY[r, cols] = NAN
+        got = p.backward(dw_dtype=torch.float32)
+        want["dX"][r] = NAN
+        want["dW"][g, cols] = NAN
+        want["db"][g, cols] = NAN
+        for name in want:
+            assert same(got[name], want[name]), name
+        p.Y[r, cols] = 0.0
+        gone = p.backward(dw_dtype=torch.float32)
+        p.dY[r, cols] = 5.0
+        for name, t in p.backward(dw_dtype=torch.float32).items():
+            assert same(gone[name], t), name
+        p.act = "elu"
+        want = p.backward(dw_dtype=torch.float32)
+        p.Y[r, cols] = NAN
+        want["dX"][r] = NAN
+        want["dW"][g, cols] = NAN
+        want["db"][g, cols] = NAN
+        for name, t in p.backward(dw_dtype=torch.float32).items():
+            assert same(t, want[name]), name
