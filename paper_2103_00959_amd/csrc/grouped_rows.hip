@@ -227,10 +227,11 @@ static cogdl_status check_grouped(int64_t n, int32_t E, int32_t k, int32_t m, co
     return COGDL_OK;
 }
 
-// A grid of the smallest tiles would not fit a launch: refused before anything runs.
+// More of the smallest tiles than the walks number: refused before anything runs.  (The kernel for few rows
+// has smaller ones, of 16 x 16: 2176 pieces at most, under 2^30 tiles at any width.)
 static bool too_many_tiles(int64_t n, int32_t E, int64_t wc)
 {
-    return piece_tiles(most_pieces(n, E, 128), (wc + 63) / 64) == 0;
+    return !countable(most_pieces(n, E, 128), (wc + 63) / 64);
 }
 
 cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m, const int32_t *offsets,
@@ -293,7 +294,7 @@ cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int3
     if (weights && need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < need))
         return COGDL_ERR_INVALID;
     if (n > 0 && dX && k > 0 && too_many_tiles(n, E, k)) return COGDL_ERR_TOO_LARGE;
-    if (weights && piece_tiles(c.count, (int64_t)((m + 63) / 64) * ((k + 64) / 64)) == 0) return COGDL_ERR_TOO_LARGE;
+    if (weights && !countable(c.count, (int64_t)((m + 63) / 64) * (k > 0 ? (k + 63) / 64 : 1))) return COGDL_ERR_TOO_LARGE;
     GroupedArgs a{};
     a.n = n; a.E = E; a.k = k; a.m = m;
     a.off = offsets;

@@ -895,12 +895,8 @@ struct GroupedArgs {
 // Most pieces of `per` rows that n rows in E groups can have.
 inline int64_t most_pieces(int64_t n, int32_t E, int64_t per) { return n / per + (n < E ? n : E); }
 
-// The grid of pieces x tiles, pieces rounded up to whole rounds of the XCDs; 0: too large.
-inline unsigned piece_tiles(int64_t pieces, int64_t tiles)
-{
-    const int64_t b = (pieces + 7) / 8 * 8 * tiles;
-    return b <= INT32_MAX ? (unsigned)b : 0u;
-}
+// The walks number tiles in 31 bits.
+inline bool countable(int64_t pieces, int64_t tiles) { return pieces * tiles <= INT32_MAX; }
 
 // Widths: the byte offsets inside a tile of 256 rows (or a chunk of 64) are 32 bits.
 constexpr int kMaxWidth = 1 << 22;
