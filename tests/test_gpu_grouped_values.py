@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2103_00959_amd as cg
+from grouped_exact import Whole, agree
 from test_gpu_grouped import Problem
 
 pytestmark = pytest.mark.gpu
@@ -75,3 +76,45 @@ def test_slope_of_nan(sizes, k, m, codes):
         want["db"][g, cols] = NAN
         for name, t in p.backward(dw_dtype=torch.float32).items():
             assert same(t, want[name]), name
+
+
+# the smallest subnormals; the codes of a checkpoint have steps of 2^-24 (fp16) and 2^-126 (bf16) at least
+TINY = {"f16": 2.0 ** -24, "bf16": 2.0 ** -133}
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu", "elu"])
+@pytest.mark.parametrize("sizes,k,m", FORWARDS)
+def test_subnormal_gradients(sizes, k, m, act, dt):
+    """dY of two subnormal steps, of which ELU's slope of 1/2 leaves one: dW and db are whole numbers of steps, dX and
+    a narrow dW the same rounded once."""
+    p = Whole(sizes, k, m, dt, act)
+    p.dY = (2 * p.dY.double() * TINY[dt]).to(p.dt)
+    for codes in (False, True):
+        X = p.X.cuda()
+        kept = dict(zip(("codes", "exps"), cg.act_checkpoint(X))) if codes else {"X": X}
+        for dw in (torch.float32, p.dt):
+            o = cg.grouped_linear_backward(p.dY.cuda(), p.W.cuda(), p.offsets.cuda(), **kept, act=act,
+                                           Y=p.Y.cuda() if act != "none" else None, dw_dtype=dw)
+            want = p.sums("cuda")
+            assert want["dW"].abs().max() > 0 and (p.dY != 0).any()
+            for name in o:
+                assert agree(o[name], want[name]), (name, codes, dw)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("sizes,k,m", FORWARDS)
+def test_subnormal_features(sizes, k, m, dt):
+    """X of one subnormal step through the forward and dW; fp16 checkpoints hold it as it is."""
+    p = Whole(sizes, k, m, dt)
+    p.X = (p.X.double() * TINY[dt]).to(p.dt)
+    for out in (torch.float32, p.dt):
+        Y = cg.grouped_linear(p.X.cuda(), p.W.cuda(), p.offsets.cuda(), out_dtype=out)
+        assert agree(Y, p.outputs("cuda"))
+    want = p.sums("cuda")
+    for codes in (False, True) if dt == "f16" else (False,):
+        X = p.X.cuda()
+        kept = dict(zip(("codes", "exps"), cg.act_checkpoint(X))) if codes else {"X": X}
+        o = cg.grouped_linear_backward(p.dY.cuda(), p.W.cuda(), p.offsets.cuda(), **kept, dw_dtype=torch.float32)
+        for name in o:
+            assert agree(o[name], want[name]), (name, codes)
