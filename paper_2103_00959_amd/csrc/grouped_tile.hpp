@@ -153,9 +153,9 @@ struct PieceWalk {
 // takes the same time, however uneven those are (with pieces of groups instead, 64 groups of 150
 // to 1400 rows, 2048 x 2048, took 587 us, the same rows in even groups 540).  Slices and output
 // tiles are numbered slice by slice, each XCD takes an equal run of them; a workgroup's tile of a
-// slice has its part of every group in turn.  A group without rows belongs to the slice of its
-// place, and its products of nothing are its zeros.  Of a slice's groups only the first and the last can
-// reach out of it: their partial sums go to slots 2 i (begun before slice i) and 2 i + 1.
+// slice has its part of every group in turn.  Groups without rows are in no slice (deal_empty_groups).
+// Of a slice's groups only the first and the last can reach out of it: their partial sums go to
+// slots 2 i (begun before slice i) and 2 i + 1.
 struct SliceWalk {
     Groups groups;
     int per, tiles, slices;
@@ -174,10 +174,8 @@ struct SliceWalk {
     {
         groups.window(at);
         const int64_t lo = groups.lo, hi = lo + groups.size;
-        const bool mine = groups.base + lane_id() < groups.E &&
-                          (groups.size > 0 ? lo < to && hi > from : (lo < to || slice == slices - 1) && lo >= from);
-        todo = __ballot(mine);
-        past = __ballot(groups.base + lane_id() >= groups.E || lo >= to) != 0 && slice != slices - 1;
+        todo = __ballot(groups.size > 0 && lo < to && hi > from);
+        past = __ballot(groups.base + lane_id() >= groups.E || lo >= to) != 0;
     }
     // the groups of the slice: from the one that holds the row before it
     __device__ __forceinline__ void open_slice()
@@ -228,11 +226,32 @@ struct SliceWalk {
         s.tile = tile;
         s.lo = lo > from ? lo : from;
         const int64_t stop = hi < to ? hi : to;
-        s.have = stop > s.lo ? (int)(stop - s.lo) : 0;
+        s.have = (int)(stop - s.lo);
         s.slot = lo < from ? 2 * slice : hi > to ? 2 * slice + 1 : -1;
         return true;
     }
 };
+
+// Calls zero(g, piece) for every group g without rows and each of `pieces` pieces of its output, dealt over
+// the workgroups one by one whatever the groups' places: E x pieces pairs, a lane looks at one, 64 at a time.
+template <typename Zero>
+__device__ __forceinline__ void deal_empty_groups(const int32_t *__restrict__ off, int E, int64_t n, int64_t pieces, Zero zero)
+{
+    Groups groups{off, n, E};
+    const int64_t all = E * pieces, step = gridDim.x;
+    for (int64_t u0 = blockIdx.x; u0 < all; u0 += kWave * step) {
+        const int64_t u = u0 + lane_id() * step;
+        const int g = u < all ? (int)(u / pieces) : E;
+        groups.read(g);
+        uint64_t todo = __ballot(g < E && groups.size == 0);
+        while (todo != 0) {
+            const int l = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const int mine = __builtin_amdgcn_readlane(g, l);
+            zero(mine, u0 + l * step - mine * pieces);
+        }
+    }
+}
 
 // -------------------------------------------------------- pieces of memory
 

@@ -10,6 +10,14 @@
 namespace cogdl {
 namespace {
 
+// The matrix of a group without rows is zeroed in pieces of so many elements (of size 0 in one: db's zeros are with
+// the first), which all workgroups share evenly: bound by memory.  8 rows in the first 8 of 64 groups, 2048 -> 1024
+// bf16: 48 us (5.6 TB/s); one row among 256 groups of 1024 x 1024 111 (4.8 TB/s); 4096 groups of 64 x 64, two of
+// them with rows, 14.  (As tiles of the slice at their place 354, 1558 and 6459: a workgroup zeroed a run of them one
+// after another.)
+constexpr int kZeroPiece = 16384;
+__host__ __device__ inline int64_t zero_pieces(int64_t size) { return size > 0 ? (size + kZeroPiece - 1) / kZeroPiece : 1; }
+
 // dW and db: TM x TN outputs (c by j) of a group's matrix at a time, over a slice's rows of it.
 // One group of 32768 rows, 2048 x 2048 bf16: 270 us (1.02 PFLOP/s); from 8 bits 365: each of the 8 rows of
 // tiles decodes the codes again, and the matrix cores wait meanwhile.  64 groups of 280 to 2244 rows
@@ -113,6 +121,15 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_weights(GroupedArgs a
                 fsum[i] = 0.f;
             }
         }
+    });
+    const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int64_t size = a.out ? mk : 0;
+    deal_empty_groups(a.off, a.E, a.n, zero_pieces(size), [&](int g, int64_t piece) {
+        const int64_t end = (piece + 1) * kZeroPiece < size ? (piece + 1) * kZeroPiece : size;
+        for (int64_t i = piece * kZeroPiece + threadIdx.x * 8; i < end; i += N * 8)
+            store8(a.out, a.out_dtype, g * mk + i, 0, end - i < 8 ? (int)(end - i) : 8, zeros);
+        if (piece == 0 && a.db)
+            for (int c = threadIdx.x; c < a.m; c += N) a.db[(int64_t)g * a.m + c] = 0.f;
     });
 }
 
@@ -229,8 +246,8 @@ int64_t tiles_of(int64_t m, int64_t k, int tm, int tn) { return (m + tm - 1) / t
 // Slices of rows: a group that is cut costs its partial sums, so there are no more slices than
 // make two tiles of 128 x 128 (one of 256 x 256) for each resident workgroup, and of few rows a
 // slice for 128 of them or 4 groups or, where the partial sums are small, as many as they leave
-// under 4 MB.  Slices have 16 rows or more, or 4 groups each: groups without rows take their turn too (46 rows
-// in 253 groups, 104 x 28: 487 us in 2 slices, 85 in 46).
+// under 4 MB.  Slices have 16 rows or more, or 4 groups each: few rows can be as many groups (46 rows
+// in 253 groups, 104 x 28: 49 us in 2 slices, 9 in 46; 64 groups of one row, 1024 x 1024, 105 and 35).
 Slices slices_of(int64_t n, int32_t E, int32_t k, int32_t m)
 {
     const int64_t tiles = tiles_of(m, k, m > 64 ? 128 : 64, k > 64 ? 128 : 64);
@@ -268,8 +285,10 @@ cogdl_status grouped_weights_launch(GroupedArgs a, const Slices &c, cogdl_dtype 
     const GroupedKernel kern = dtype == COGDL_BF16 ? pick_tile<bf16_t>(t, act, codes, direct_dy, direct_x)
                                                    : pick_tile<f16_t>(t, act, codes, direct_dy, direct_x);
     const int waves = t.tm == 256 ? 8 : 4;
-    const cogdl_status st = launch_tiles("grouped_linear_dw", kern, a, c.count * a.tiles_c, waves, lds_of(waves, t.tm, t.tn),
-                                         2, stream);
+    // (with any number of groups without rows: which, only the device knows)
+    const int64_t zeros = a.E * zero_pieces(a.out ? (int64_t)a.m * a.k : 0);
+    const int64_t all = c.count * a.tiles_c > zeros ? c.count * a.tiles_c : zeros;
+    const cogdl_status st = launch_tiles("grouped_linear_dw", kern, a, all, waves, lds_of(waves, t.tm, t.tn), 2, stream);
     if (st != COGDL_OK || c.slots() == 0) return st;
     // whole vectors of 4 where the matrices and rows of db are
     const int64_t values = (a.out ? (int64_t)a.m * a.k : 0) + (a.db ? a.m : 0);
