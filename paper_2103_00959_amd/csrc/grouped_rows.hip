@@ -188,10 +188,22 @@ Variant pick_tile(int64_t n, int32_t E, int wc, bool dx, bool act, bool direct)
     return pick<T, 4, 128, 64>(dx, act, direct);
 }
 
-// Whether the kernel for few rows is the faster one: every 16 rows read their group's weights
-// again.  2048 -> 1024 bf16, 64 even groups, 32 / 512 / 1024 / 2048 rows: 25 / 61 / 74 / 130 us, with
-// tiles 39 / 77 / 78 / 78; one group, 2048 -> 2048, 64 / 256 / 512 rows: 12 / 34 / 61, with tiles 21 / 43 / 44.
-bool few_rows(int64_t n, int32_t E) { return n <= 256 || (n <= 8 * (int64_t)E && n <= 2048); }
+// Whether the kernel for few rows is the faster one.  It reads a group's weights once for every 16 rows, at 5 TB/s;
+// tiles read them once, at 5.5, but take 9.5 ns for each of k features besides.  With G groups that have rows and
+// P pieces of 16 rows in them (as if they were even) that is in favour of few rows while
+//     2 k m P / 5 TB/s < 9.5 ns k + 2 k m G / 5.5 TB/s,  or  m (11 (P - G) + G) < 2^18,
+// whatever k.  bf16, us, with tiles in brackets: 64 groups, 2048 -> 1024, 32 / 512 rows: 25 (39) / 61 (77); 2048 -> 2048,
+// one group of 16 / 64 / 128 / 256 rows: 9 (23) / 13 (24) / 21 (26) / 35 (26); 64 groups of 1 / 8 rows 96 (125) / 115
+// (126), 256 groups 365 (346) / 446 (352); 4096 -> 4096, one group of 64 / 128 / 256: 35 (52) / 63 (55) / 121 (56), 64 of
+// one row 356 (344); 8192 -> 8192, one of 16 / 64 / 256: 35 (92) / 119 (95) / 453 (105), with odd k three times that
+// (256 rows of 8191: 1556 (169)).  More rows (64 groups, 2048 -> 1024, 1024 / 2048 rows: 74 (78) / 130 (78)) are
+// tiles' whatever the widths.
+bool few_rows(int64_t n, int32_t E, int32_t m)
+{
+    if (n > 256 && (n > 8 * (int64_t)E || n > 2048)) return false;
+    const int64_t G = n < E ? n : E, P = G * (((n + G - 1) / G + kFewRows - 1) / kFewRows);
+    return m * (11 * (P - G) + G) < 1 << 18;
+}
 
 }  // namespace
 
@@ -201,7 +213,7 @@ cogdl_status grouped_rows_launch(const char *name, GroupedArgs a, bool dx, cogdl
     // direct loads: every row of both operands on the 4-byte grid
     const bool direct = on_grid(dx ? a.dY : a.X, dx ? a.m : a.k) && on_grid(a.W, a.k);
     const int wc = dx ? a.k : a.m;
-    if (!dx && a.k >= 8 && few_rows(a.n, a.E)) {
+    if (!dx && a.k >= 8 && few_rows(a.n, a.E, a.m)) {
         const GroupedKernel kern = dtype == COGDL_BF16 ? k_grouped_few<bf16_t> : k_grouped_few<f16_t>;
         a.tiles_c = (a.m + kFewCols - 1) / kFewCols;
         return launch_tiles(name, kern, a, most_pieces(a.n, a.E, kFewRows) * a.tiles_c, kFewWaves, 0, 0, stream);
