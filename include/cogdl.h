@@ -507,7 +507,8 @@ cogdl_status cogdl_grouped_linear(int64_t n, int32_t E, int32_t k, int32_t m,
  * is rounded to it).  dX, dW and db may each be NULL (not computed; W is then
  * not needed for dX, nor X for dW).  Groups of no rows get dW = 0 and db = 0;
  * rows of no group keep what dX held there.  The products take dZ rounded to
- * dtype (exact without an activation and for ReLU); db sums it unrounded.
+ * dtype (exact without an activation and for ReLU; ELU's terms are off by up to
+ * half a step of dtype each, in an fp32 dW too); db sums it unrounded.
  * fp32 accumulation, in a fixed order.  workspace: device scratch for partial
  * sums, at least the size that cogdl_grouped_linear_backward_workspace reports
  * (0 for few rows: NULL is then accepted), 16-byte aligned; its contents are

@@ -978,7 +978,9 @@ def grouped_linear(X, W, offsets, bias=None, act: str = "none", out_dtype=None, 
     none).  X [n, k] and W [E, m, k] both bf16 or both fp16; offsets int32 [E + 1] on the device; bias
     fp32 [E, m] or None.  Rows before offsets[0] and from offsets[E] on belong to no group: ``out`` keeps
     what it held there, a fresh output holds anything.  With ``save`` (or codes and exps given) returns
-    (Y, codes, exps), the 8-bit checkpoint of X for grouped_linear_backward."""
+    (Y, codes, exps), the 8-bit checkpoint of X for grouped_linear_backward.  A given ``out`` has the type
+    it has (out_dtype is for a fresh one).  Not recorded by autograd: the gradients are
+    grouped_linear_backward's."""
     import torch
     if act not in ACT:
         raise ValueError(f"act must be one of {sorted(ACT)}")
@@ -1022,8 +1024,9 @@ def grouped_linear_backward(dY, W, offsets, X=None, codes=None, exps=None, Y=Non
                             dw_dtype=None, out=None, workspace=None):
     """Gradients of grouped_linear for dY = dL/dY [n, m]: returns dict(dX [n, k], dW [E, m, k], db fp32
     [E, m]).  The input comes as X [n, k] or as its 8-bit checkpoint (codes, exps), which the products read
-    as it is.  With an activation, Y is the forward's output in dY's dtype.  dw_dtype: dY's dtype (default)
-    or fp32.  ``out`` may supply the tensors; a None among them leaves that gradient out.  Groups without
+    as it is.  With an activation, Y is the forward's output in dY's dtype (ELU's dZ is rounded to that
+    dtype for dX and dW, an fp32 dW too).  dw_dtype, of a fresh dW: dY's dtype (default) or fp32.  ``out``
+    may supply the tensors, of either type for dW; a None among them leaves that gradient out.  Groups without
     rows get zeros; rows of no group keep what dX held there (anything in a fresh one).  ``workspace``: at
     least grouped_linear_backward_workspace bytes."""
     import torch

@@ -500,7 +500,7 @@ struct RowOperand {
                     unpack8<T>(y[q], o);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[e] = act_grad(d[e], o[e], act);
-                    w = pack8<T>(d);        // the matrix cores take 16 bits
+                    w = pack8<T>(d);        // the matrix cores take 16 bits: ELU's dZ is rounded (see ColOperand)
                 }
                 if (tail) w = shift_down(w, gone);
                 *reinterpret_cast<uint4 *>(tile + row_tile_at(index(q), piece())) = w;
@@ -636,7 +636,11 @@ struct ColOperand {
                             unpack8<T>(ragged ? shift_down(y[q], gone) : y[q], o);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) d[e] = act_grad(d[e], o[e], act);
-                            w = pack8<T>(d);    // the matrix cores take 16 bits; the sums do not round
+                            // The matrix cores take 16 bits.  ReLU's dZ is dY or 0, ELU's is rounded here, by up to
+                            // half a step of T a term, as where a layer below hands dZ on in T; a dW in fp32 has that
+                            // error too (20000 rows: 8e-4 of its size in bf16, 1e-4 in fp16, against 1e-7 of the other
+                            // activations).  The sums do not round.
+                            w = pack8<T>(d);
                         }
                         if constexpr (SUM) {
 #pragma unroll
