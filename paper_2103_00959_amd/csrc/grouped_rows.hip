@@ -2,8 +2,8 @@
 // with a weight matrix of its own, and the gradient of their input:
 //     Y[i, c]  = act(sum_j X[i, j] W[g, c, j] + bias[g, c])        rows i of group g
 //     dX[i, j] = sum_c dZ[i, c] W[g, c, j]                          dZ = dY act'(Y)
-// The offsets stay on the device: the grid covers the most tiles that n rows in E groups can
-// have, and each workgroup finds its group by a scan of the group sizes.
+// The offsets stay on the device: each of the resident workgroups finds its tiles' groups by a scan of
+// the group sizes.
 #include "grouped_tile.hpp"
 
 namespace cogdl {
