@@ -525,6 +525,119 @@ cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int3
                                            size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Rows of a table of learned embeddings (nodes, entities, tokens; H^(0) of a
+ * model without input features):
+ *   Y[i] = scale * table[index[i]]
+ * table: V x k of dtype; index: n int32; Y: n x k of y_dtype; dtypes fp32, bf16
+ * or fp16, the product formed in fp32.  An index outside [0, V) stands for a
+ * padded place and gives a row of zeros.  n up to COGDL_MAX_NNZ, k up to 2^22
+ * (COGDL_ERR_TOO_LARGE past these), V >= 1.
+ * ---------------------------------------------------------------------- */
+cogdl_status cogdl_embedding(int64_t n, int32_t V, int32_t k, const void *table, cogdl_dtype dtype,
+                             const int32_t *index, float scale, void *Y, cogdl_dtype y_dtype,
+                             hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Gradient of cogdl_embedding for dY (n x k of dtype):
+ *   dtable[v] = scale * sum_{i: index[i] = v} dY[i]      (V x k of d_dtype)
+ * With accumulate != 0 that sum is added to what dtable holds (an exception to
+ * "never accumulated into": the other gradient of a tied table), and the rows
+ * of indices that do not occur are neither read nor written; else they become
+ * zeros.  Places whose index lies outside [0, V) count for nothing, whatever dY
+ * holds there.  The sums are fp32, over the places of an index in order, and
+ * rounded once.  workspace: device scratch of at least the size that
+ * cogdl_embedding_backward_workspace reports (0 where n or k is 0: NULL is then
+ * accepted), 256-byte aligned; its contents are clobbered, and calls in flight
+ * together need one each.
+ * ---------------------------------------------------------------------- */
+cogdl_status cogdl_embedding_backward_workspace(int64_t n, int32_t V, int32_t k, size_t *bytes);
+cogdl_status cogdl_embedding_backward(int64_t n, int32_t V, int32_t k, const void *dY,
+                                      cogdl_dtype dtype, const int32_t *index, float scale,
+                                      void *dtable, cogdl_dtype d_dtype, int32_t accumulate,
+                                      void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Softmax cross entropy of a linear layer over a large vocabulary (all
+ * entities, nodes or tokens), without keeping its logits:
+ *   z[i, v] = sum_j X[i, j] * W[v, j] + bias[v],   lse[i] = log sum_v exp(z[i, v])
+ *   loss[i] = lse[i] - z[i, target[i]]
+ * X: n x k, W: V x k, both of dtype (bf16 or fp16), row-major; bias: V fp32,
+ * nullable (-inf takes an answer out); target: n int32; loss and lse: n fp32.
+ * A row whose target lies outside [0, V) is left out: loss and lse are 0, and
+ * neither is computed, whatever X holds there.  Logits, exponentials and sums
+ * are fp32; a loss is off by the rounding of its logits, so one far below
+ * 2^-24 of them (a certain answer) may come out as 0, never below.  A NaN in a
+ * row that counts, or a logit of +inf, makes its loss NaN.
+ * n up to 2^24, k up to 2^22, and n x V up to 2^45 (tiles of 128 x 128 are
+ * counted in 31 bits; COGDL_ERR_TOO_LARGE past these).  Any alignment of X and W
+ * is right; rows of W of an even number of elements on the 4-byte grid are
+ * fastest.  workspace: device scratch of at least the size that
+ * cogdl_linear_loss_workspace reports (K = 0 for cross entropy, the entries
+ * of a row for distillation), 256-byte aligned, one for each call in flight; NULL
+ * where n is 0.
+ * ---------------------------------------------------------------------- */
+cogdl_status cogdl_linear_loss_workspace(int64_t n, int32_t V, int32_t k, int32_t K, size_t *bytes);
+cogdl_status cogdl_linear_cross_entropy(int64_t n, int32_t V, int32_t k, const void *X,
+                                        const void *W, cogdl_dtype dtype, const float *bias,
+                                        const int32_t *target, float *loss, float *lse,
+                                        void *workspace, size_t workspace_bytes,
+                                        hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Gradients of cogdl_linear_cross_entropy for dloss = dL/dloss (n fp32), from
+ * the forward's loss and lse:
+ *   dz[i, v] = dloss[i] * (exp(z[i, v] - lse[i]) - [v = target[i]])
+ *   dX = dz W (n x k of dtype),  dW = dz^T X (V x k of dtype),  db[v] = sum_i dz[i, v] (V fp32)
+ * The logits are computed again, for a piece of the vocabulary at a time; the
+ * products take dz rounded to dtype (each by at most half a step, after a power
+ * of two for the whole call has brought the largest dloss near fp16's top; fp16
+ * keeps what is above 2^-38 of the largest), db sums it unrounded.  dX, dW and db may each be NULL
+ * (not computed).  Rows left out get dX = 0 and enter no sum.  fp32
+ * accumulation in a fixed order.  workspace as above, of the size that
+ * cogdl_linear_loss_backward_workspace reports (nonzero for n = 0 too).
+ * ---------------------------------------------------------------------- */
+cogdl_status cogdl_linear_loss_backward_workspace(int64_t n, int32_t V, int32_t k, int32_t K,
+                                                  size_t *bytes);
+cogdl_status cogdl_linear_cross_entropy_backward(int64_t n, int32_t V, int32_t k,
+                                                 const float *dloss, const void *X, const void *W,
+                                                 cogdl_dtype dtype, const float *bias,
+                                                 const int32_t *target, const float *loss,
+                                                 const float *lse, void *dX, void *dW, float *db,
+                                                 void *workspace, size_t workspace_bytes,
+                                                 hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Distillation from a teacher's top logits: the loss of the same layer against
+ * the K answers that a teacher gives each row.  With temperature T > 0,
+ *   q[i, :]    = softmax over the entries that count of teacher[i, :] / T
+ *   lse[i]     = log sum_v exp(z[i, v] / T)          (over the whole vocabulary)
+ *   logp[i, e] = z[i, index[i, e]] / T - lse[i]
+ *   loss[i]    = T^2 * sum_e q[i, e] * (log q[i, e] - logp[i, e])
+ * index: n x K int32; teacher: n x K fp32; 1 <= K <= COGDL_MAX_TEACHER.  An entry
+ * counts where its index lies inside [0, V) (a padded one has logp 0); a teacher's
+ * logit of -inf has q = 0.  The same index twice in a row is two entries.  A row
+ * without an entry that counts, or with -inf alone, is left out as above (logp 0).
+ * Everything else as cogdl_linear_cross_entropy.  Gradients, from lse and logp:
+ *   dz[i, v] = dloss[i] * T * (exp(z[i, v] / T - lse[i]) - sum_{e: index[i, e] = v} q[i, e])
+ * and the rest as cogdl_linear_cross_entropy_backward (no gradient of the
+ * teacher's logits).
+ * ---------------------------------------------------------------------- */
+#define COGDL_MAX_TEACHER 1024
+
+cogdl_status cogdl_linear_distill(int64_t n, int32_t V, int32_t k, int32_t K, const void *X,
+                                  const void *W, cogdl_dtype dtype, const float *bias,
+                                  const int32_t *index, const float *teacher, float temperature,
+                                  float *loss, float *lse, float *logp, void *workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+cogdl_status cogdl_linear_distill_backward(int64_t n, int32_t V, int32_t k, int32_t K,
+                                           const float *dloss, const void *X, const void *W,
+                                           cogdl_dtype dtype, const float *bias,
+                                           const int32_t *index, const float *teacher,
+                                           float temperature, const float *lse, const float *logp,
+                                           void *dX, void *dW, float *db, void *workspace,
+                                           size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Dot-product SDDMM -- section 2.2, T = A (.) (P Q^T), per head: for every
  * edge k = (i, col[k]) and head h
  *     out[k * H + h] = sum_d P[i, h, d] * Q[col[k], h, d]

@@ -18,6 +18,12 @@ fallback.
     grouped_linear(X, W, offsets, bias, act, save=False)          -> Y, rows of group g by W[g] (, checkpoint of X)
     grouped_linear_backward(dY, W, offsets, X | codes, exps, ...) -> dX, dW, db
     act_checkpoint(A) / act_restore(codes, exps)                  -> activations in 8 bits and back
+    embedding(table, index, scale)                                -> Y = scale table[index]
+    embedding_backward(dY, index, V, scale)                       -> the table's gradient, by sorted tokens
+    linear_cross_entropy(X, W, target, bias)                      -> loss, lse of the logits X W^T + b, never kept
+    linear_cross_entropy_backward(dloss, X, W, target, loss, lse) -> dX, dW, db
+    linear_distill(X, W, index, teacher, bias, temperature)       -> loss, lse, logp against a teacher's top logits
+    linear_distill_backward(dloss, X, W, index, teacher, ...)     -> dX, dW, db
     Plan(rowptr, nnz, max_feat, max_heads, mode, group_size)      -> the workload balancer
 """
 from __future__ import annotations
@@ -93,6 +99,17 @@ def lib():
     L.cogdl_grouped_linear_backward_workspace.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
     L.cogdl_grouped_linear_backward.argtypes = [i64, i32, i32, i32, P, P, P, P, P, P, ctypes.c_int, P,
                                                 ctypes.c_int, P, P, ctypes.c_int, P, P, sz, P]
+    L.cogdl_embedding.argtypes = [i64, i32, i32, P, ctypes.c_int, P, f32, P, ctypes.c_int, P]
+    L.cogdl_embedding_backward_workspace.argtypes = [i64, i32, i32, ctypes.POINTER(sz)]
+    L.cogdl_embedding_backward.argtypes = [i64, i32, i32, P, ctypes.c_int, P, f32, P, ctypes.c_int, i32, P, sz, P]
+    L.cogdl_linear_loss_workspace.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
+    L.cogdl_linear_loss_backward_workspace.argtypes = L.cogdl_linear_loss_workspace.argtypes
+    L.cogdl_linear_cross_entropy.argtypes = [i64, i32, i32, P, P, ctypes.c_int, P, P, P, P, P, sz, P]
+    L.cogdl_linear_cross_entropy_backward.argtypes = [i64, i32, i32, P, P, P, ctypes.c_int, P, P, P, P, P, P, P, P,
+                                                      sz, P]
+    L.cogdl_linear_distill.argtypes = [i64, i32, i32, i32, P, P, ctypes.c_int, P, P, P, f32, P, P, P, P, sz, P]
+    L.cogdl_linear_distill_backward.argtypes = [i64, i32, i32, i32, P, P, P, ctypes.c_int, P, P, P, f32, P, P, P, P,
+                                                P, P, sz, P]
     L.cogdl_spmm_t.argtypes = [i32, i32, i64, P, P, P, i32, P, ctypes.c_int, P, ctypes.c_int, P, P]
     L.cogdl_csr_to_csc_workspace.argtypes = [i32, i32, i64, ctypes.POINTER(sz)]
     L.cogdl_csr_to_csc.argtypes = [i32, i32, i64, P, P, P, P, P, P, P, P, sz, P]
@@ -119,7 +136,10 @@ def lib():
                  "cogdl_linear",
                  "cogdl_head_scores", "cogdl_act_codec_size", "cogdl_act_compress",
                  "cogdl_act_decompress", "cogdl_act_checkpoint", "cogdl_act_restore", "cogdl_grouped_linear",
-                 "cogdl_grouped_linear_backward_workspace", "cogdl_grouped_linear_backward"):
+                 "cogdl_grouped_linear_backward_workspace", "cogdl_grouped_linear_backward", "cogdl_embedding",
+                 "cogdl_embedding_backward_workspace", "cogdl_embedding_backward", "cogdl_linear_loss_workspace",
+                 "cogdl_linear_loss_backward_workspace", "cogdl_linear_cross_entropy",
+                 "cogdl_linear_cross_entropy_backward", "cogdl_linear_distill", "cogdl_linear_distill_backward"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -1081,4 +1101,245 @@ def grouped_linear_backward(dY, W, offsets, X=None, codes=None, exps=None, Y=Non
             _addr(Y), ACT[act], _addr(dX), _addr(dW), _dtype_code(dY if dW is None else dW), _addr(db),
             _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
             _stream()), "cogdl_grouped_linear_backward")
+    return o
+
+
+def _scratch(workspace, need, like):
+    """A workspace of at least `need` bytes (None: a fresh one, or None where nothing is needed)."""
+    import torch
+    if workspace is None:
+        return like.new_empty(need, dtype=torch.uint8) if need > 0 else None
+    _at_least(workspace, "workspace", (need + workspace.element_size() - 1) // workspace.element_size())
+    return _dev(workspace, "workspace")
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
+    """Rows of a table [V, k] (fp32, bf16 or fp16) by an int32 index [n], times ``scale``: Y [n, k] in out_dtype (the
+    table's by default).  An index outside [0, V) stands for a padded place: a row of zeros.  A given ``out``
+    has the type it has.  Not recorded by autograd: the gradient is embedding_backward's."""
+    import torch
+    V, k = _dims(table, "table", 2)
+    if V < 1:
+        raise CogdlError("table needs at least one row")
+    n = _index_array(index, "index")
+    _numel(out, "out", n * k)
+    _dev(table, "table"), _dev(index, "index", torch.int32)
+    if out is None:
+        out = table.new_empty((n, k), dtype=out_dtype or table.dtype)
+    _dev(out, "out")
+    with _on_device(table, index, out):
+        _check(lib().cogdl_embedding(n, V, k, _addr(table), _dtype_code(table), _addr(index), float(scale), _addr(out),
+                                     _dtype_code(out), _stream()), "cogdl_embedding")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def embedding_backward_workspace(n: int, V: int, k: int) -> int:
+    """Bytes of scratch that embedding_backward takes for n places and a table of V rows of k features."""
+    b = ctypes.c_size_t()
+    _check(lib().cogdl_embedding_backward_workspace(n, V, k, ctypes.byref(b)), "cogdl_embedding_backward_workspace")
+    return b.value
+
+
+def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, out=None, accumulate: bool = False,
+                       workspace=None):
+    """Gradient of embedding for dY = dL/dY [n, k]: dtable [V, k] in out_dtype (dY's by default), with
+    dtable[v] = scale * the sum of dY over the places of v, in fp32 and in order (the same bits every run).
+    With ``accumulate``, ``out`` must be given: the sums are added to it, and its other rows are left alone (the
+    other gradient of a tied table, such as linear_cross_entropy_backward's dW); else they become zeros.  Padded
+    places (an index outside [0, V)) count for nothing.  ``workspace``: at least embedding_backward_workspace
+    bytes."""
+    import torch
+    n, k = _dims(dY, "dY", 2)
+    V = int(V)
+    if V < 1:
+        raise CogdlError("the table needs at least one row")
+    _index_array(index, "index")
+    _numel(index, "index", n)
+    _numel(out, "out", V * k)
+    if accumulate and out is None:
+        raise CogdlError("accumulate needs out, the gradient to add to")
+    need = embedding_backward_workspace(n, V, k)
+    _dev(dY, "dY"), _dev(index, "index", torch.int32)
+    if out is None:
+        out = dY.new_empty((V, k), dtype=out_dtype or dY.dtype)
+    _dev(out, "out")
+    workspace = _scratch(workspace, need, dY)
+    with _on_device(dY, index, out, workspace):
+        _check(lib().cogdl_embedding_backward(n, V, k, _addr(dY), _dtype_code(dY), _addr(index), float(scale),
+                                              _addr(out), _dtype_code(out), int(bool(accumulate)), _addr(workspace),
+                                              _bytes(workspace), _stream()), "cogdl_embedding_backward")
+    return out
+
+
+MAX_TEACHER = 1024     # COGDL_MAX_TEACHER: entries of a teacher's row
+
+
+@functools.lru_cache(maxsize=256)
+def linear_loss_workspace(n: int, V: int, k: int, K: int = 0) -> int:
+    """Bytes of scratch that linear_cross_entropy (K = 0) or linear_distill of K entries takes."""
+    b = ctypes.c_size_t()
+    _check(lib().cogdl_linear_loss_workspace(n, V, k, K, ctypes.byref(b)), "cogdl_linear_loss_workspace")
+    return b.value
+
+
+@functools.lru_cache(maxsize=256)
+def linear_loss_backward_workspace(n: int, V: int, k: int, K: int = 0) -> int:
+    """Bytes of scratch that the backward of linear_cross_entropy (K = 0) or linear_distill takes."""
+    b = ctypes.c_size_t()
+    _check(lib().cogdl_linear_loss_backward_workspace(n, V, k, K, ctypes.byref(b)),
+           "cogdl_linear_loss_backward_workspace")
+    return b.value
+
+
+def _head(X, W, bias):
+    """(n, V, k) of a linear layer over a vocabulary, with its sizes checked."""
+    n, k = _dims(X, "X", 2)
+    V, kw = _dims(W, "W", 2)
+    if kw != k or X.dtype != W.dtype:
+        raise CogdlError("X must be [n, k] and W [V, k] of the same dtype")
+    if V < 1:
+        raise CogdlError("W needs at least one row")
+    _numel(bias, "bias", V)
+    return n, V, k
+
+
+def _teacher(index, teacher, n, temperature):
+    """The entries of a teacher's row, with sizes and temperature checked."""
+    if _dims(index, "index", 2)[0] != n or _dims(teacher, "teacher", 2) != tuple(index.shape):
+        raise CogdlError(f"index and teacher must both be [{n}, K]")
+    K = index.shape[1]
+    if K < 1 or K > MAX_TEACHER:
+        raise CogdlError(f"index has {K} entries a row, 1 to {MAX_TEACHER} are supported")
+    if not 0.0 < float(temperature) < float("inf"):
+        raise CogdlError(f"temperature must be positive and finite, got {temperature}")
+    return K
+
+
+def _loss_outputs(X, shapes, given):
+    """The forward's fp32 outputs: those given, checked, or fresh ones."""
+    import torch
+    outs = []
+    for (name, shape), t in zip(shapes.items(), given):
+        size = 1
+        for d in shape:
+            size *= d
+        _numel(t, name, size)
+        outs.append(X.new_empty(shape, dtype=torch.float32) if t is None else _dev(t, name, torch.float32))
+    return outs
+
+
+def linear_cross_entropy(X, W, target, bias=None, loss=None, lse=None, workspace=None):
+    """Softmax cross entropy of the logits z = X W^T + bias over a large vocabulary, which are never kept: returns
+    (loss, lse), fp32 [n] each, with lse = logsumexp(z) and loss = lse - z[target].  X [n, k] and W [V, k] both
+    bf16 or both fp16; target int32 [n], a row whose target lies outside [0, V) is left out (loss and lse 0);
+    bias fp32 [V] or None (-inf takes an answer out).  ``workspace``: at least linear_loss_workspace bytes.  Not
+    recorded by autograd: the gradients are linear_cross_entropy_backward's."""
+    import torch
+    n, V, k = _head(X, W, bias)
+    _index_array(target, "target")
+    _numel(target, "target", n)
+    _numel(loss, "loss", n), _numel(lse, "lse", n)
+    need = linear_loss_workspace(n, V, k)
+    _dev(X, "X"), _dev(W, "W"), _dev(target, "target", torch.int32), _dev(bias, "bias", torch.float32)
+    loss, lse = _loss_outputs(X, {"loss": (n,), "lse": (n,)}, (loss, lse))
+    workspace = _scratch(workspace, need, X)
+    with _on_device(X, W, target, bias, loss, lse, workspace):
+        _check(lib().cogdl_linear_cross_entropy(n, V, k, _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(target),
+                                                _addr(loss), _addr(lse), _addr(workspace), _bytes(workspace),
+                                                _stream()), "cogdl_linear_cross_entropy")
+    return loss, lse
+
+
+def linear_distill(X, W, index, teacher, bias=None, temperature: float = 1.0, loss=None, lse=None, logp=None,
+                   workspace=None):
+    """Distillation from a teacher's top K logits: the loss of the logits z = X W^T + bias, over the whole
+    vocabulary and never kept, against q = softmax(teacher / T) over the K entries of a row.  Returns (loss, lse,
+    logp): loss = T^2 sum q (log q - logp) [n], lse = logsumexp(z / T) [n], logp = z[index] / T - lse [n, K], all
+    fp32.  index int32 [n, K] (outside [0, V): no entry), teacher fp32 [n, K]; a row without entries is left out
+    (zeros).  Everything else as linear_cross_entropy; the gradients are linear_distill_backward's."""
+    import torch
+    n, V, k = _head(X, W, bias)
+    K = _teacher(index, teacher, n, temperature)
+    _numel(loss, "loss", n), _numel(lse, "lse", n), _numel(logp, "logp", n * K)
+    need = linear_loss_workspace(n, V, k, K)
+    _dev(X, "X"), _dev(W, "W"), _dev(index, "index", torch.int32), _dev(teacher, "teacher", torch.float32)
+    _dev(bias, "bias", torch.float32)
+    loss, lse, logp = _loss_outputs(X, {"loss": (n,), "lse": (n,), "logp": (n, K)}, (loss, lse, logp))
+    workspace = _scratch(workspace, need, X)
+    with _on_device(X, W, index, teacher, bias, loss, lse, logp, workspace):
+        _check(lib().cogdl_linear_distill(n, V, k, K, _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(index),
+                                          _addr(teacher), float(temperature), _addr(loss), _addr(lse), _addr(logp),
+                                          _addr(workspace), _bytes(workspace), _stream()), "cogdl_linear_distill")
+    return loss, lse, logp
+
+
+def _head_gradients(X, W, bias, out):
+    """The gradients' outputs: those given, checked, or fresh ones (db where there is a bias)."""
+    import torch
+    n, k = X.shape
+    V = W.shape[0]
+    o = dict(out or {})
+    sizes = {"dX": n * k, "dW": V * k, "db": V}
+    for name, t in o.items():
+        if name not in sizes:
+            raise CogdlError(f"unknown output {name!r}")
+        _numel(t, name, sizes[name])
+    for name, t, dtype in (("dX", X, X.dtype), ("dW", W, X.dtype), ("db", bias, torch.float32)):
+        if name not in o:
+            o[name] = None if t is None else torch.empty_like(t)
+        _dev(o[name], name, dtype)
+    return o
+
+
+def linear_cross_entropy_backward(dloss, X, W, target, loss, lse, bias=None, out=None, workspace=None):
+    """Gradients of linear_cross_entropy for dloss = dL/dloss fp32 [n], from the forward's loss and lse: returns
+    dict(dX [n, k], dW [V, k], db fp32 [V]; db None without a bias).  The logits are computed again by pieces of the
+    vocabulary; the products take dz = dloss (softmax(z) - onehot) rounded to X's dtype, db sums it unrounded.
+    Rows left out get zeros in dX and enter no sum.  ``out`` may supply the tensors; a None among them leaves that
+    gradient out.  ``workspace``: at least linear_loss_backward_workspace bytes."""
+    import torch
+    n, V, k = _head(X, W, bias)
+    _index_array(target, "target")
+    for name, t in (("dloss", dloss), ("target", target), ("loss", loss), ("lse", lse)):
+        _tensor(t, name)
+        _numel(t, name, n)
+    need = linear_loss_backward_workspace(n, V, k)
+    _dev(X, "X"), _dev(W, "W"), _dev(target, "target", torch.int32), _dev(bias, "bias", torch.float32)
+    _dev(dloss, "dloss", torch.float32), _dev(loss, "loss", torch.float32), _dev(lse, "lse", torch.float32)
+    o = _head_gradients(X, W, bias, out)
+    workspace = _scratch(workspace, need, X)
+    with _on_device(X, W, target, bias, dloss, loss, lse, o["dX"], o["dW"], o["db"], workspace):
+        _check(lib().cogdl_linear_cross_entropy_backward(
+            n, V, k, _addr(dloss), _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(target), _addr(loss),
+            _addr(lse), _addr(o["dX"]), _addr(o["dW"]), _addr(o["db"]), _addr(workspace), _bytes(workspace),
+            _stream()), "cogdl_linear_cross_entropy_backward")
+    return o
+
+
+def linear_distill_backward(dloss, X, W, index, teacher, lse, logp, bias=None, temperature: float = 1.0, out=None,
+                            workspace=None):
+    """Gradients of linear_distill for dloss = dL/dloss fp32 [n], from the forward's lse and logp: returns
+    dict(dX, dW, db) as linear_cross_entropy_backward does (none of the teacher's logits)."""
+    import torch
+    n, V, k = _head(X, W, bias)
+    K = _teacher(index, teacher, n, temperature)
+    for name, t, size in (("dloss", dloss, n), ("lse", lse, n), ("logp", logp, n * K)):
+        _tensor(t, name)
+        _numel(t, name, size)
+    need = linear_loss_backward_workspace(n, V, k, K)
+    _dev(X, "X"), _dev(W, "W"), _dev(index, "index", torch.int32), _dev(teacher, "teacher", torch.float32)
+    _dev(bias, "bias", torch.float32), _dev(dloss, "dloss", torch.float32), _dev(lse, "lse", torch.float32)
+    _dev(logp, "logp", torch.float32)
+    o = _head_gradients(X, W, bias, out)
+    workspace = _scratch(workspace, need, X)
+    with _on_device(X, W, index, teacher, bias, dloss, lse, logp, o["dX"], o["dW"], o["db"], workspace):
+        _check(lib().cogdl_linear_distill_backward(
+            n, V, k, K, _addr(dloss), _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(index), _addr(teacher),
+            float(temperature), _addr(lse), _addr(logp), _addr(o["dX"]), _addr(o["dW"]), _addr(o["db"]),
+            _addr(workspace), _bytes(workspace), _stream()), "cogdl_linear_distill_backward")
     return o

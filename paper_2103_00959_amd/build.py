@@ -23,6 +23,7 @@ LIB = os.path.join(HERE, "libcogdl_mi355.so")
 CALIB_LIB = os.path.join(HERE, "libcogdl_calib.so")
 CALIB_SOURCES = ["calib.hip"]
 SOURCES = ["primitives.hip", "plan.hip", "spmm.hip", "gspmm.hip", "gat.hip", "gat_proj.hip", "gat_bwd.hip", "dense.hip", "grouped_rows.hip", "grouped_weights.hip", "codec.hip",
+           "embedding.hip", "vocab.hip", "vocab_grad.hip",
            "checkpoint.hip", "csc.hip", "trace.hip"]
 
 ARCH = "gfx950"

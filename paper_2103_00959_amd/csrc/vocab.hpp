@@ -1,0 +1,131 @@
+// The softmax losses over a large vocabulary (vocab.hip, vocab_grad.hip): what their launches share.
+//
+//     z[i, v] = sum_j X[i, j] W[v, j] + bias[v],   lse[i] = log sum_v exp(z[i, v] / T)
+//     cross entropy:  loss[i] = lse[i] - z[i, t_i]                                   (T = 1)
+//     distillation:   loss[i] = T^2 sum_e q[i, e] (log q[i, e] - logp[i, e])
+//                     logp[i, e] = z[i, v_ie] / T - lse[i],  q[i, :] = softmax(teacher[i, :] / T)
+//     dz[i, v] = g[i] T (exp(z[i, v] / T - lse[i]) - sum_{e: v_ie = v} q[i, e]),  dX = dz W,  dW = dz^T X
+//
+// Logits are never kept.  Rows that count (a target inside the vocabulary, a teacher's entry) are gathered
+// first, so that padded rows cost nothing and what they hold reaches no sum: every product below runs over
+// `live` rows, a number that only the device knows.
+#pragma once
+
+#include "grouped_tile.hpp"
+
+namespace cogdl {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Most entries of a teacher's row.
+constexpr int kMaxEntries = COGDL_MAX_TEACHER;
+// Rows of one call.
+constexpr int64_t kMaxRows = 1 << 24;
+
+// Header of a workspace, written by k_vocab_rows.
+struct RowsHead {
+    int32_t off[2];              // 0, live rows
+    float scale, unscale;        // 2^e and 2^-e: |g T| 2^e < 2^15 for every live row
+};
+
+struct VocabArgs {
+    int64_t n;                   // rows given
+    int32_t V, k, kp;            // kp: k rounded up to 8, the pitch of the gathered rows
+    int32_t entries;             // of a row: 1 (cross entropy), K (distillation)
+    bool distill;
+    float T, per_z;              // per_z = log2(e) / T
+    const void *X, *W;
+    const float *bias;           // V, nullable
+    const int32_t *index;        // n x entries
+    const float *teacher;        // n x entries (distillation)
+    const float *dloss;          // n (backward)
+    const float *loss_in, *lse_in, *logp_in;
+    float *loss, *lse, *logp;
+    void *dX, *dW;
+    float *db;
+    // workspace
+    RowsHead *head;
+    int32_t *live;               // n: >= 0 where the row counts (distillation; else the targets are read)
+    float *tlse;                 // n: log sum_e exp(teacher / T) (distillation)
+    int32_t *rows;               // live: the rows that count
+    float *lse2, *g;             // live: lse log2(e), g T
+    void *Xr;                    // live x kp: their features
+    float2 *part;                // [slot][n]: (max, sum) of a row's logits in a slot of columns, in powers of two
+    int32_t slots;
+    void *dz;                    // live x (piece's columns, rounded up to 8): scaled by head->scale
+    float *dx_part;              // [slice][live][kp]
+    int32_t slices;
+    float *db_part;              // [row tile][V]
+    int32_t row_tiles;
+    unsigned long long *db_q;    // V: the targets' part, in units of 2^-unit_bits
+    int32_t unit_bits;
+    // this launch
+    int32_t v0, width;           // the vocabulary piece [v0, v0 + width)
+    int32_t pitch;               // of dz
+    int32_t tiles_c;
+    bool first;                  // the first piece
+};
+
+using VocabKernel = void (*)(VocabArgs);
+
+// The tiles of one output of R x C tiles (R >= 0, known on the device), S slices of the sum each.  Tiles are
+// numbered slice by slice, then in panels of kPanel row tiles, in a panel column by column; the XCDs take equal runs
+// of them, their workgroups one after another: those that run together on an XCD take kPanel rows of tiles by a
+// few columns, and share both operands in its L2.
+constexpr int kPanel = 8;
+
+struct GridWalk {
+    int R, C, tm;
+    int64_t rows;
+    uint32_t j, step, end;
+
+    __device__ __forceinline__ void start(int64_t n, int rows_a_tile, int col_tiles, int slices)
+    {
+        rows = n;
+        tm = rows_a_tile;
+        R = (int)((n + tm - 1) / tm);
+        C = col_tiles;
+        const int64_t all = (int64_t)R * C * slices;
+        const uint32_t xcd = blockIdx.x & 7;
+        j = (uint32_t)(all * xcd / 8) + (blockIdx.x >> 3);
+        end = (uint32_t)(all * (xcd + 1) / 8);
+        step = gridDim.x >> 3;
+    }
+    __device__ __forceinline__ bool next(Span &s)
+    {
+        if (j >= end) return false;
+        const uint32_t one = (uint32_t)R * (uint32_t)C;
+        const uint32_t slice = j / one, u = j % one;
+        j = end - j > step ? j + step : end;
+        const uint32_t panel = u / (uint32_t)(kPanel * C), w = u % (uint32_t)(kPanel * C);
+        const int left = R - (int)panel * kPanel, tall = left < kPanel ? left : kPanel;
+        s.g = (int)panel * kPanel + (int)(w % (uint32_t)tall);          // row tile
+        s.tile = (int)(w / (uint32_t)tall);
+        s.slot = (int)slice;
+        s.lo = (int64_t)s.g * tm;
+        s.have = rows - s.lo < tm ? (int)(rows - s.lo) : tm;
+        return true;
+    }
+};
+
+// Launches a kernel of resident workgroups over at most `all` tiles.
+inline cogdl_status launch_vocab(const char *name, VocabKernel kern, const VocabArgs &a, int64_t all, int waves, size_t lds,
+                                 hipStream_t stream)
+{
+    const int64_t resident = resident_blocks(reinterpret_cast<const void *>(kern), waves * kWave, lds, 0) / 8;
+    if (resident < 1) return COGDL_ERR_LAUNCH;
+    const int64_t need = (all + 7) / 8;
+    COGDL_LAUNCH_SHM(name, kern, dim3((unsigned)(8 * (need < resident ? need : resident))), waves * kWave, lds, stream, a);
+    return COGDL_OK;
+}
+
+// The rows that count, gathered (and, for a backward pass, the gradients of the others zeroed).
+cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backward, hipStream_t stream);
+// The logits: their (max, sum) by slots of columns, or the piece's dz.
+cogdl_status vocab_logits_launch(VocabArgs a, cogdl_dtype dtype, bool grad, bool wide, hipStream_t stream);
+
+// Whether the logits of n rows by `cols` columns take tiles of 256 x 256 (else 128 x 128).
+bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W);
+
+}  // namespace cogdl

@@ -1,0 +1,397 @@
+// Softmax losses over a large vocabulary, backward (the formulas: vocab.hpp): the vocabulary in pieces, for
+// each of which the logits are computed again, turned into dz in 16 bits, and multiplied with W (into dX's
+// sums) and with X (into the piece's rows of dW).
+#include "vocab.hpp"
+
+namespace cogdl {
+namespace {
+
+constexpr int kBlock = 256;
+
+// The targets' part of dz, in fp32 from the loss itself: dz = g T (p - sum q), where p of a likely target is
+// near sum q and dz of it was rounded as g T p.  Several entries of a row on the same answer all write their
+// common value.  On the first piece also the targets' part of db, in whole numbers (any order gives the same
+// sum).  A wavefront a row, an entry a lane (cross entropy: a row a lane).
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_targets(VocabArgs a)
+{
+    const int64_t live = a.head->off[1];
+    const float scale = a.head->scale;
+    T *__restrict__ dz = static_cast<T *>(a.dz);
+    const int64_t me = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
+    const int64_t group = a.distill ? me / kWave : me, groups = a.distill ? all / kWave : all;
+    const int first = a.distill ? lane_id() : 0, step = a.distill ? kWave : 1;
+    for (int64_t p = group; p < live; p += groups) {
+        const int64_t i = a.rows[p];
+        const int32_t *__restrict__ index = a.index + i * a.entries;
+        const float g = a.g[p] * scale;
+        for (int e = first; e < a.entries; e += step) {
+            const int32_t v = index[e];
+            if ((uint32_t)v >= (uint32_t)a.V) continue;
+            const bool here = v >= a.v0 && v - a.v0 < a.width;
+            float d, mine = 1.f;
+            if (a.distill) {
+                const float *__restrict__ teacher = a.teacher + i * a.entries;
+                const float tlse = a.tlse[i];
+                mine = expf(teacher[e] / a.T - tlse);
+                float q = 0.f;
+                if (here)
+                    for (int o = 0; o < a.entries; ++o)
+                        if (index[o] == v) q += expf(teacher[o] / a.T - tlse);
+                d = expf(a.logp_in[i * a.entries + e]) - q;
+            } else {
+                d = expm1f(-a.loss_in[i]);
+            }
+            if (here) {
+                const float one[1] = {d * g};
+                store_out<T, 1>(dz + p * a.pitch, v - a.v0, one);
+            }
+            if (a.first && a.db_q) {
+                const float w = ldexpf(mine * g, a.unit_bits);
+                // (a row whose gradient is not finite makes all of db NaN by its dz)
+                if (fabsf(w) < 9e18f) atomicAdd(&a.db_q[v], (unsigned long long)(long long)rintf(w));
+            }
+        }
+    }
+}
+
+// dX's sums over the piece: rows by k, a slice of the piece's columns each.
+template <typename T, int WAVES, int TM, int TN, int SRCB>
+__global__ __launch_bounds__(WAVES * kWave) void k_vocab_dx(VocabArgs a)
+{
+    constexpr int N = WAVES * kWave;
+    constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
+    constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
+    extern __shared__ __align__(16) char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
+    const int64_t live = a.head->off[1];
+    const int per = ((a.pitch + a.slices - 1) / a.slices + kX - 1) / kX * kX;
+    GridWalk walk;
+    walk.start(live, TM, a.tiles_c, a.slices);
+    RowOperand<T, TM, N, kDirect> A;
+    ColOperand<T, TN, N, SRCB, false> B;
+    const auto open = [&](const Span &s) {
+        int x0 = s.slot * per;
+        if (x0 > a.pitch) x0 = a.pitch;
+        const int wide = a.pitch - x0 < per ? a.pitch - x0 : per, real = a.width - x0 < 0 ? 0 : a.width - x0 < wide ? a.width - x0 : wide;
+        A.open(static_cast<const T *>(a.dz) + s.lo * a.pitch + x0, nullptr, s.have, a.pitch, 0);
+        A.width = wide;
+        B.open(static_cast<const T *>(a.W) + ((int64_t)a.v0 + x0) * a.k, nullptr, nullptr, nullptr, s.tile * TN, a.k, real, 0, false);
+        return wide;
+    };
+    char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
+    run_tiles<T, decltype(A), decltype(B), WR, WC>(
+        lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; },
+        [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
+        [&](const Span &s, const Acc<WR, WC> &acc) {
+            const int col0 = s.tile * TN + c0;
+            float *__restrict__ part = a.dx_part + (s.slot * a.n + s.lo) * a.kp;
+            for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
+                r += r0;
+                c += col0;
+                if (r >= s.have || c >= a.kp) return;
+                float *__restrict__ to = part + (int64_t)r * a.kp + c;
+                if (!a.first) {
+                    float w[2][4];
+                    load_vec<float, 4>(to, 0, w[0]);
+                    load_vec<float, 4>(to, 4, w[1]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += w[e / 4][e % 4];
+                }
+                store_vec<float, 8>(to, 0, v);
+            });
+        });
+}
+
+// The piece's rows of dW: vocabulary by k, summed over the live rows.
+template <typename T, int WAVES, int TM, int TN>
+__global__ __launch_bounds__(WAVES * kWave) void k_vocab_dw(VocabArgs a)
+{
+    constexpr int N = WAVES * kWave;
+    constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
+    constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
+    extern __shared__ __align__(16) char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
+    const int live = a.head->off[1];
+    const float unscale = a.head->unscale;
+    GridWalk walk;
+    walk.start(a.width, TM, a.tiles_c, 1);
+    ColOperand<T, TM, N, kDirect, false> A;
+    ColOperand<T, TN, N, kDirect, false> B;
+    const auto open = [&](const Span &s) {
+        A.open(static_cast<const T *>(a.dz), nullptr, nullptr, nullptr, (int)s.lo, a.pitch, live, 0, false);
+        B.open(static_cast<const T *>(a.Xr), nullptr, nullptr, nullptr, s.tile * TN, a.kp, live, 0, false);
+        return live;
+    };
+    char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
+    run_tiles<T, decltype(A), decltype(B), WR, WC>(
+        lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; },
+        [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
+        [&](const Span &s, const Acc<WR, WC> &acc) {
+            const int col0 = s.tile * TN + c0;
+            T *__restrict__ dW = static_cast<T *>(a.dW) + (a.v0 + s.lo) * a.k;
+            for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
+                r += r0;
+                c += col0;
+                if (r >= s.have || c >= a.k) return;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= unscale;
+                store8(dW + (int64_t)r * a.k, c, a.k, v);
+            });
+        });
+}
+
+// dX of the live rows from their slices' sums.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_dx_out(VocabArgs a)
+{
+    const int64_t live = a.head->off[1];
+    const float unscale = a.head->unscale;
+    const int vecs = a.kp / 8;
+    const int64_t all = live * vecs;
+    for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < all; u += (int64_t)gridDim.x * kBlock) {
+        const int64_t p = u / vecs;
+        const int c = (int)(u % vecs) * 8;
+        float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < a.slices; ++s) {
+            float w[2][4];
+            const float *__restrict__ from = a.dx_part + (s * a.n + p) * a.kp + c;
+            load_vec<float, 4>(from, 0, w[0]);
+            load_vec<float, 4>(from, 4, w[1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] += w[e / 4][e % 4];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] *= unscale;
+        store8(static_cast<T *>(a.dX) + a.rows[p] * (int64_t)a.k, c, a.k, t);
+    }
+}
+
+// db from the row tiles' sums and the targets' part.
+__global__ __launch_bounds__(kBlock) void k_vocab_db(VocabArgs a, int rows_a_part)
+{
+    const int64_t live = a.head->off[1];
+    const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
+    const int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (v >= a.V) return;
+    float t = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.V + v];
+    const double q = ldexp((double)(long long)a.db_q[v], -a.unit_bits);
+    a.db[v] = (float)((double)t - q) * a.head->unscale;
+}
+
+template <typename T>
+VocabKernel pick_dx(bool wide, bool direct)
+{
+    if (wide) return k_vocab_dx<T, 8, 256, 256, kDirect>;
+    return direct ? k_vocab_dx<T, 4, 128, 128, kDirect> : k_vocab_dx<T, 4, 128, 128, kStaged>;
+}
+
+template <typename T>
+VocabKernel pick_dw(bool wide)
+{
+    if (wide) return k_vocab_dw<T, 8, 256, 256>;
+    return k_vocab_dw<T, 4, 128, 128>;
+}
+
+int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1) / tile * ((cols + tile - 1) / tile); }
+
+// The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).
+constexpr int64_t kPieceBytes = 256ll << 20;
+
+struct Pieces {
+    int32_t width;               // of a piece, the last may be smaller
+    int32_t slices;              // of a piece, in dX's sums
+};
+
+Pieces pieces_of(int64_t n, int32_t V, int32_t k)
+{
+    int64_t cols = kPieceBytes / (2 * (n > 0 ? n : 1)) / 256 * 256;
+    if (cols < 256) cols = 256;
+    if (cols > kMaxWidth) cols = kMaxWidth;
+    const int64_t count = (V + cols - 1) / cols;
+    int64_t width = ((V + count - 1) / count + 255) / 256 * 256;
+    if (width > V) width = V;
+    Pieces p;
+    p.width = (int32_t)width;
+    const int64_t tiles = tiles_of(n, k, 128);
+    int64_t slices = tiles > 0 ? 512 / tiles : 1;
+    const int64_t most = width / 256;
+    if (slices > most) slices = most;
+    p.slices = (int32_t)(slices < 1 ? 1 : slices);
+    return p;
+}
+
+struct Layout {
+    size_t total = 0;
+    size_t take(size_t bytes)
+    {
+        const size_t at = total;
+        total += (bytes + 255) & ~size_t(255);
+        return at;
+    }
+};
+
+size_t lay_backward(VocabArgs &a, char *ws)
+{
+    const Pieces p = pieces_of(a.n, a.V, a.k);
+    a.width = p.width;
+    a.pitch = (p.width + 7) / 8 * 8;
+    a.slices = p.slices;
+    a.row_tiles = (int32_t)((a.n + 127) / 128 * 2);
+    const size_t n = (size_t)a.n;
+    Layout l;
+    a.head = reinterpret_cast<RowsHead *>(ws + l.take(sizeof(RowsHead)));
+    a.live = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 4 * n : 0));
+    a.tlse = reinterpret_cast<float *>(ws + l.take(a.distill ? 4 * n : 0));
+    a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * n));
+    a.lse2 = reinterpret_cast<float *>(ws + l.take(4 * n));
+    a.g = reinterpret_cast<float *>(ws + l.take(4 * n));
+    a.Xr = ws + l.take(2 * n * a.kp);
+    a.dz = ws + l.take(2 * n * a.pitch);
+    a.dx_part = reinterpret_cast<float *>(ws + l.take(4 * n * a.kp * a.slices));
+    a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.V));
+    a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(8 * (size_t)a.V));
+    return l.total;
+}
+
+cogdl_status check_sizes(int64_t n, int32_t V, int32_t k, int32_t K)
+{
+    if (n < 0 || V < 1 || k < 0 || K < 1) return COGDL_ERR_INVALID;
+    if (n > kMaxRows || k > kMaxWidth || K > kMaxEntries) return COGDL_ERR_TOO_LARGE;
+    const int64_t tr = (n + 127) / 128, tv = ((int64_t)V + 127) / 128, tk = ((int64_t)k + 127) / 128;
+    if (!countable(tr, tv) || !countable(tr, tk) || !countable(tv, tk)) return COGDL_ERR_TOO_LARGE;
+    return COGDL_OK;
+}
+
+#define COGDL_TRY(expr)                              \
+    do {                                             \
+        const cogdl_status _s = (expr);              \
+        if (_s != COGDL_OK) return _s;               \
+    } while (0)
+
+cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (dtype != COGDL_BF16 && dtype != COGDL_F16) return COGDL_ERR_DTYPE;
+    COGDL_TRY(check_sizes(a.n, a.V, a.k, a.entries));
+    if (!(a.T > 0.f) || a.T > 3.4e38f) return COGDL_ERR_INVALID;
+    if (a.n > 0 && (!a.index || !a.dloss || !a.lse_in || (a.k > 0 && (!a.X || !a.W)))) return COGDL_ERR_INVALID;
+    if (a.n > 0 && (a.distill ? !a.teacher || !a.logp_in : !a.loss_in)) return COGDL_ERR_INVALID;
+    if (a.k == 0) a.dX = a.dW = nullptr;
+    if (a.n == 0) a.dX = nullptr;
+    if (!a.dX && !a.dW && !a.db) return COGDL_OK;
+    a.kp = (a.k + 7) / 8 * 8;
+    a.per_z = kLog2e / a.T;
+    const size_t need = lay_backward(a, static_cast<char *>(workspace));
+    if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < need) return COGDL_ERR_INVALID;
+    const int piece = a.width;
+    if (!a.db) {
+        a.db_part = nullptr;
+        a.db_q = nullptr;
+    }
+    // n terms below 2^15, in 62 bits
+    a.unit_bits = 46 - bits_for((uint64_t)a.n);
+    const bool bf16 = dtype == COGDL_BF16;
+    COGDL_TRY(vocab_rows_launch(a, dtype, true, stream));
+    const bool wide_logits = vocab_wide(a.n, piece, a.k, a.W);
+    for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
+        a.v0 = (int32_t)v0;
+        a.width = (int32_t)(a.V - v0 < piece ? a.V - v0 : piece);
+        a.pitch = (a.width + 7) / 8 * 8;
+        a.first = v0 == 0;
+        if (a.n > 0) {
+            COGDL_TRY(vocab_logits_launch(a, dtype, true, wide_logits, stream));
+            int64_t blocks = ((a.distill ? a.n * kWave : a.n) + kBlock - 1) / kBlock;
+            if (blocks > 2048) blocks = 2048;
+            if (bf16) COGDL_LAUNCH("vocab_targets", k_vocab_targets<bf16_t>, (unsigned)blocks, kBlock, stream, a);
+            else COGDL_LAUNCH("vocab_targets", k_vocab_targets<f16_t>, (unsigned)blocks, kBlock, stream, a);
+        }
+        if (a.dX) {
+            const bool wide = on_grid(a.W, a.k) && a.k > 128 && tiles_of(a.n, a.k, 256) * a.slices >= 128;
+            const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
+            a.tiles_c = (a.k + tile - 1) / tile;
+            COGDL_TRY(launch_vocab("vocab_dx", bf16 ? pick_dx<bf16_t>(wide, on_grid(a.W, a.k)) : pick_dx<f16_t>(wide, on_grid(a.W, a.k)),
+                                   a, tiles_of(a.n, a.k, tile) * a.slices, waves, lds_of(waves, tile, tile), stream));
+        }
+        if (a.dW) {
+            const bool wide = a.k > 128 && tiles_of(a.width, a.k, 256) >= 128;
+            const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
+            a.tiles_c = (a.k + tile - 1) / tile;
+            COGDL_TRY(launch_vocab("vocab_dw", bf16 ? pick_dw<bf16_t>(wide) : pick_dw<f16_t>(wide), a, tiles_of(a.width, a.k, tile),
+                                   waves, lds_of(waves, tile, tile), stream));
+        }
+    }
+    if (a.dX) {
+        int64_t blocks = (a.n * (a.kp / 8) + kBlock - 1) / kBlock;
+        if (blocks > 4096) blocks = 4096;
+        if (bf16) COGDL_LAUNCH("vocab_dx_out", k_vocab_dx_out<bf16_t>, (unsigned)blocks, kBlock, stream, a);
+        else COGDL_LAUNCH("vocab_dx_out", k_vocab_dx_out<f16_t>, (unsigned)blocks, kBlock, stream, a);
+    }
+    if (a.db) COGDL_LAUNCH("vocab_db", k_vocab_db, (unsigned)((a.V + kBlock - 1) / kBlock), kBlock, stream, a, wide_logits ? 128 : 64);
+    return COGDL_OK;
+}
+
+}  // namespace
+}  // namespace cogdl
+
+using namespace cogdl;
+
+extern "C" {
+
+cogdl_status cogdl_linear_loss_backward_workspace(int64_t n, int32_t V, int32_t k, int32_t K, size_t *bytes)
+{
+    if (!bytes || K < 0) return COGDL_ERR_INVALID;
+    VocabArgs a{};
+    a.n = n; a.V = V; a.k = k;
+    a.entries = K > 0 ? K : 1;
+    a.distill = K > 0;
+    COGDL_TRY(check_sizes(n, V, k, a.entries));
+    a.kp = (k + 7) / 8 * 8;
+    *bytes = lay_backward(a, nullptr);
+    return COGDL_OK;
+}
+
+cogdl_status cogdl_linear_cross_entropy_backward(int64_t n, int32_t V, int32_t k, const float *dloss, const void *X,
+                                                 const void *W, cogdl_dtype dtype, const float *bias,
+                                                 const int32_t *target, const float *loss, const float *lse, void *dX,
+                                                 void *dW, float *db, void *workspace, size_t workspace_bytes,
+                                                 hipStream_t stream)
+{
+    VocabArgs a{};
+    a.n = n; a.V = V; a.k = k;
+    a.entries = 1;
+    a.T = 1.f;
+    a.X = X; a.W = W;
+    a.bias = bias;
+    a.index = target;
+    a.dloss = dloss;
+    a.loss_in = loss; a.lse_in = lse;
+    a.dX = dX; a.dW = dW; a.db = db;
+    return run_backward(a, dtype, workspace, workspace_bytes, stream);
+}
+
+cogdl_status cogdl_linear_distill_backward(int64_t n, int32_t V, int32_t k, int32_t K, const float *dloss, const void *X,
+                                           const void *W, cogdl_dtype dtype, const float *bias, const int32_t *index,
+                                           const float *teacher, float temperature, const float *lse, const float *logp,
+                                           void *dX, void *dW, float *db, void *workspace, size_t workspace_bytes,
+                                           hipStream_t stream)
+{
+    VocabArgs a{};
+    a.n = n; a.V = V; a.k = k;
+    a.entries = K;
+    a.distill = true;
+    a.T = temperature;
+    a.X = X; a.W = W;
+    a.bias = bias;
+    a.index = index;
+    a.teacher = teacher;
+    a.dloss = dloss;
+    a.lse_in = lse; a.logp_in = logp;
+    a.dX = dX; a.dW = dW; a.db = db;
+    return run_backward(a, dtype, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,174 @@
+"""GPU tests of the embedding lookup and its gradient against the formulas in 64 bits.
+
+Tolerances (u = 2^-24): the lookup forms one product in fp32 and rounds it to the output: u |y|, then half a step
+of the output's type.  A sum of c rows in fp32, in any order, is off by at most c u of the sum of their
+magnitudes; the factor adds u, adding to what is there another, and the output's type its half step."""
+import pytest
+import torch
+
+import paper_2103_00959_amd as cg
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+U = 2.0 ** -24
+
+
+def half(dtype):
+    return 0.0 if dtype == torch.float32 else torch.finfo(dtype).eps / 2
+
+
+def tiny(dtype):
+    return torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+
+
+def tokens(n, V, g, skew=1.0, pad=0.1):
+    t = (torch.rand(n, generator=g, dtype=torch.float64) ** skew * V).int()
+    t[torch.rand(n, generator=g) < pad] = -1
+    if n > 5:
+        t[n // 3], t[n // 2] = V, -2 ** 31
+    return t
+
+
+WIDTHS = [1, 2, 3, 5, 8, 16, 33, 64, 100, 300, 602, 2048, 5000]
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k", WIDTHS)
+def test_lookup(k, dt, out):
+    g = torch.Generator().manual_seed(k)
+    for n, V in ((1, 1), (7, 3), (300, 90), (2100, 50)):
+        if n * k > 4_000_000:
+            continue
+        T = torch.randn((V, k), generator=g).to(DT[dt])
+        index = tokens(n, V, g)
+        got = cg.embedding(T.cuda(), index.cuda(), scale=1.7, out_dtype=DT[out]).double().cpu()
+        scale = torch.tensor(1.7, dtype=torch.float32).double()
+        inside = (index >= 0) & (index < V)
+        want = torch.where(inside[:, None], T.double()[index.clamp(0, V - 1).long()] * scale, 0.0)
+        bound = want.abs() * (U + half(DT[out]) * (1 + U)) + tiny(DT[out])
+        assert (got - want).abs().le(bound).all()
+        assert (got[~inside] == 0).all()
+
+
+def test_lookup_without_a_factor_is_a_copy():
+    for dt in DT:
+        T = torch.randn(40, 77).to(DT[dt]).cuda()
+        T[3, 5], T[4, 6] = float("inf"), float("nan")
+        index = torch.randint(0, 40, (500,), dtype=torch.int32).cuda()
+        assert torch.equal(cg.embedding(T, index).nan_to_num(7.0), T[index.long()].nan_to_num(7.0))
+
+
+def test_lookup_past_4_gib():
+    """Rows behind the 4 GiB that 32-bit offsets reach."""
+    V, k = 2_300_000, 1024
+    T = torch.zeros((V, k), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 2_097_151, 2_097_152, V - 1], dtype=torch.int32, device="cuda")
+    T[at.long()] = torch.arange(1, 5, device="cuda", dtype=torch.bfloat16)[:, None]
+    got = cg.embedding(T, at.flip(0).contiguous(), scale=2.0)
+    assert torch.equal(got, torch.tensor([8, 6, 4, 2], dtype=torch.bfloat16, device="cuda")[:, None].expand(4, k))
+    g = cg.embedding_backward(got, at, V, out=T, accumulate=True)
+    assert g[at.long()].float().mean(1).tolist() == [9, 8, 7, 6]
+
+
+def gradient_ref(dY, index, V, scale, base=None):
+    """(value, bound apart from the output's type)."""
+    inside = (index >= 0) & (index < V)
+    d = torch.where(inside[:, None], dY.double(), 0.0)
+    at = torch.where(inside, index, 0).long()
+    zeros = torch.zeros((V, dY.shape[1]), dtype=torch.float64)
+    s = zeros.index_add(0, at, d)
+    mag = zeros.index_add(0, at, d.abs())
+    count = torch.zeros(V, dtype=torch.float64).index_add(0, at, inside.double())[:, None]
+    scale = torch.tensor(scale, dtype=torch.float32).double()
+    value = s * scale
+    bound = (count + 2) * U * mag * scale.abs()
+    if base is not None:
+        value = value + base.double()
+        bound = bound + U * value.abs()
+    return value, bound
+
+
+def check_gradient(n, V, k, dt, out, skew, add, seed, scale=0.75):
+    g = torch.Generator().manual_seed(seed)
+    dY = torch.randn((n, k), generator=g).to(DT[dt])
+    index = tokens(n, V, g, skew)
+    base = torch.randn((V, k), generator=g).to(DT[out]) if add else None
+    value, bound = gradient_ref(dY, index, V, scale, base)
+    dY[(index < 0) | (index >= V)] = float("nan")           # padded places may hold anything
+    got = cg.embedding_backward(dY.cuda(), index.cuda(), V, scale=scale, out_dtype=DT[out],
+                                out=base.cuda() if add else None, accumulate=add)
+    assert got.dtype == DT[out]
+    bound = bound + half(DT[out]) * (value.abs() + bound) + tiny(DT[out])
+    d = (got.double().cpu() - value).abs()
+    assert d.le(bound).all(), f"off by {float((d / bound).max()):.3g} times the bound"
+    if add:
+        untouched = torch.ones(V, dtype=torch.bool)
+        untouched[index[(index >= 0) & (index < V)].long()] = False
+        assert torch.equal(got.cpu()[untouched], base[untouched])
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("dt,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f32", "bf16"), ("bf16", "f16")])
+@pytest.mark.parametrize("k", [1, 3, 8, 12, 33, 64, 300, 1030])
+def test_gradient(k, dt, out, add):
+    for i, (n, V, skew) in enumerate(((1, 1, 1.0), (5, 4, 1.0), (17, 1, 1.0), (100, 1000, 1.0), (3000, 90, 2.0), (5000, 3, 1.5))):
+        check_gradient(n, V, k, dt, out, skew, add, 31 * k + i)
+
+
+def test_gradient_of_many_tokens():
+    """Lists in pieces of 32 and of 64, more than one radix pass, and a token that takes most of them."""
+    check_gradient(70_000, 40_000, 20, "bf16", "bf16", 2.0, False, 1)
+    check_gradient(300_000, 2_000, 9, "f32", "f32", 4.0, False, 2)
+    check_gradient(300_000, 70_000, 9, "f16", "f32", 1.0, True, 3)
+    check_gradient(300_000, 1, 8, "bf16", "f32", 1.0, False, 4)
+
+
+def test_gradient_without_places():
+    out = torch.full((9, 5), 3.0, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    cg.embedding_backward(torch.empty(0, 5, device="cuda"), none, 9, out=out, accumulate=True)
+    assert (out == 3).all()
+    cg.embedding_backward(torch.empty(0, 5, device="cuda"), none, 9, out=out)
+    assert (out == 0).all()
+    pad = torch.full((50,), -1, dtype=torch.int32, device="cuda")
+    out = cg.embedding_backward(torch.full((50, 5), float("nan"), device="cuda"), pad, 9)
+    assert (out == 0).all()
+    assert cg.embedding(out, none).shape == (0, 5)
+
+
+def test_gradient_at_any_alignment():
+    g = torch.Generator().manual_seed(6)
+    for dt, k in (("bf16", 33), ("f32", 7), ("f16", 64)):
+        dY = torch.randn((200, k), generator=g).to(DT[dt])
+        index = tokens(200, 20, g)
+        buf = torch.zeros(200 * k + 1, dtype=DT[dt], device="cuda")
+        buf[1:] = dY.flatten().cuda()
+        out = torch.full((20 * k + 2,), 5.0, dtype=DT[dt], device="cuda")
+        cg.embedding_backward(buf[1:].view(200, k), index.cuda(), 20, out=out[1:-1].view(20, k))
+        value, bound = gradient_ref(dY, index, 20, 1.0)
+        got = out[1:-1].view(20, k).double().cpu()
+        assert (got - value).abs().le(bound + half(DT[dt]) * (value.abs() + bound) + tiny(DT[dt])).all()
+        assert out[0] == 5 and out[-1] == 5
+
+
+def test_gradient_is_that_of_the_lookup():
+    """<dY, lookup(T + tD) - lookup(T)> / t = <gradient, D>: the lookup is linear in the table."""
+    g = torch.Generator().manual_seed(7)
+    T, D = (torch.randn((30, 24), generator=g, dtype=torch.float32).cuda() for _ in range(2))
+    dY = torch.randn((400, 24), generator=g).cuda()
+    index = tokens(400, 30, g).cuda()
+    both = cg.embedding(T + D, index, scale=3.0).double() - cg.embedding(T, index, scale=3.0).double()
+    left = float((both * dY.double()).sum())
+    right = float((cg.embedding_backward(dY, index, 30, scale=3.0).double() * D.double()).sum())
+    size = float((both.abs() * dY.double().abs()).sum())
+    assert abs(left - right) <= 1e-5 * size
+
+
+def test_gradient_has_the_same_bits_again():
+    g = torch.Generator().manual_seed(8)
+    dY = torch.randn((50_000, 40), generator=g).cuda()
+    index = tokens(50_000, 300, g, 3.0).cuda()
+    first = cg.embedding_backward(dY, index, 300)
+    assert all(torch.equal(first, cg.embedding_backward(dY, index, 300)) for _ in range(3))
