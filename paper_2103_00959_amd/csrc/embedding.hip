@@ -11,6 +11,28 @@
 namespace cogdl {
 namespace {
 
+// VEC values (4 or 8, or one) of a row of any type.
+template <typename T, int VEC>
+__device__ __forceinline__ void read_row(const T *__restrict__ row, int at, float (&v)[VEC])
+{
+    if constexpr (VEC == 1 || (int)sizeof(T) * VEC == 16) {
+        load_vec<T, VEC>(row, at, v);
+    } else if constexpr (sizeof(T) == 4) {
+        float h[2][4];
+        load_vec<float, 4>(row, at, h[0]);
+        load_vec<float, 4>(row, at + 4, h[1]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = h[e / 4][e % 4];
+    } else {
+        const u32x2_u w = *reinterpret_cast<const u32x2_u *>(row + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t h = (e < 2 ? w.x : w.y) >> (16 * (e & 1)) & 0xffffu;
+            v[e] = RowGather<T, 1, false>::widen1(h);
+        }
+    }
+}
+
 constexpr int kBlock = 256;
 
 // ---------------------------------------------------------------- lookup
@@ -84,15 +106,9 @@ struct ScatterArgs {
     int32_t lanes, log_lanes, vecs, chunks;
 };
 
-__global__ __launch_bounds__(kBlock) void k_tokens(ScatterArgs a)
+// The gradient of tokens that do not occur: thread `me` of `all`.
+__device__ __forceinline__ void write_zeros(const ScatterArgs &a, int64_t me, int64_t all)
 {
-    const int64_t me = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
-    for (int64_t i = me; i < a.n; i += all) {
-        const uint32_t t = (uint32_t)a.index[i];
-        a.keys[i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
-    }
-    if (a.add) return;
-    // the gradient of tokens that do not occur
     const int64_t halves = (int64_t)a.V * a.k * (a.out_bytes / 2);
     uint16_t *__restrict__ out = static_cast<uint16_t *>(a.out);
     for (int64_t i = me * 8; i < halves; i += all * 8) {
@@ -104,33 +120,146 @@ __global__ __launch_bounds__(kBlock) void k_tokens(ScatterArgs a)
     }
 }
 
-// Columns [at + gone, at + VEC) of a row of the gradient: (out +) scale v.
-template <typename TO, int VEC>
-__device__ __forceinline__ void put(const ScatterArgs &a, uint32_t token, int at, int gone, const float (&v)[VEC])
+__global__ __launch_bounds__(kBlock) void k_tokens(ScatterArgs a)
 {
-    TO *__restrict__ out = static_cast<TO *>(a.out) + (int64_t)token * a.k;
-    if (!a.add && gone == 0) {
-        float w[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] = v[e] * a.scale;
-        store_out<TO, VEC>(out, at, w);
+    const int64_t me = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = me; i < a.n; i += all) {
+        const uint32_t t = (uint32_t)a.index[i];
+        a.keys[i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
+    }
+    if (!a.add) write_zeros(a, me, all);
+}
+
+// Short lists are sorted by one workgroup in LDS, while the others of its launch write the zeros: a stable radix sort
+// of 6 bits a pass.  Each wavefront owns a run of the list and counts its digits, one scan over (digit,
+// wavefront) gives every run's places, and a key's rank in its run is the count of lower lanes with its digit (a
+// ballot a bit) behind the run's keys so far.  4096 tokens of 7 bits FIGURE us, where the sort for any length takes
+// three launches a pass.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr int kSortBits = 6, kSortDigits = 1 << kSortBits;
+constexpr int kShortList = 8192;
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_short(ScatterArgs a, int bits)
+{
+    __shared__ uint32_t keys[2][kShortList];
+    __shared__ uint16_t vals[2][kShortList];
+    __shared__ int counts[kSortDigits][kSortWaves];
+    __shared__ int sums[kSortWaves];
+    if (blockIdx.x > 0) {
+        if (!a.add) write_zeros(a, (int64_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x, (int64_t)(gridDim.x - 1) * kSortThreads);
         return;
     }
+    const int n = (int)a.n, lane = lane_id(), wave = threadIdx.x / kWave;
+    for (int i = threadIdx.x; i < n; i += kSortThreads) {
+        const uint32_t t = (uint32_t)a.index[i];
+        keys[0][i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
+        vals[0][i] = (uint16_t)i;
+    }
+    __syncthreads();
+    const int run = ((n + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
+    const int from = wave * run < n ? wave * run : n, to = from + run < n ? from + run : n;
+    int now = 0;
+    for (int shift = 0; shift < bits; shift += kSortBits, now ^= 1) {
+        for (int d = threadIdx.x; d < kSortDigits * kSortWaves; d += kSortThreads) counts[d / kSortWaves][d % kSortWaves] = 0;
+        __syncthreads();
+        for (int i = from + lane; i < to; i += kWave) atomicAdd(&counts[keys[now][i] >> shift & (kSortDigits - 1)][wave], 1);
+        __syncthreads();
+        // exclusive over (digit, wavefront): a thread an entry
+        static_assert(kSortDigits * kSortWaves == kSortThreads, "a thread an entry");
+        int *const mine = &counts[0][0] + threadIdx.x;
+        const int c = *mine, scan = wave_inclusive_scan(c);
+        if (lane == kWave - 1) sums[wave] = scan;
+        __syncthreads();
+        int before = scan - c;
+        for (int w = 0; w < wave; ++w) before += sums[w];
+        *mine = before;
+        __syncthreads();
+        for (int i0 = from; i0 < to; i0 += kWave) {
+            const int i = i0 + lane;
+            const bool in = i < to;
+            const uint32_t key = in ? keys[now][i] : 0u;
+            const int digit = (int)(key >> shift & (kSortDigits - 1));
+            uint64_t same = __ballot(in);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        if (e < gone) continue;
-        float was[1] = {0.f};
-        if (a.add) load_vec<TO, 1>(out, at + e, was);
-        const float sum[1] = {fmaf(v[e], a.scale, was[0])};
-        store_out<TO, 1>(out, at + e, sum);
+            for (int b = 0; b < kSortBits; ++b) {
+                const uint64_t ones = __ballot(digit >> b & 1);
+                same &= digit >> b & 1 ? ones : ~ones;
+            }
+            if (in) {
+                const int place = counts[digit][wave] + __popcll(same & ((1ull << lane) - 1));
+                keys[now ^ 1][place] = key;
+                vals[now ^ 1][place] = vals[now][i];
+                // the last lane of a digit moves the run's place on (the next round reads it behind this write)
+                if (same >> lane == 1) counts[digit][wave] = place + 1;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += kSortThreads) {
+        const_cast<uint32_t *>(a.sorted)[i] = keys[now][i];
+        const_cast<uint32_t *>(a.order)[i] = vals[now][i];
     }
 }
 
+// Columns [at + gone, at + VEC) of a row of the gradient: scale v, onto `was` where sums are added to it.
+template <typename TO, int VEC>
+__device__ __forceinline__ void put(const ScatterArgs &a, uint32_t token, int at, int gone, const float (&v)[VEC],
+                                    const float (&was)[VEC])
+{
+    TO *__restrict__ out = static_cast<TO *>(a.out) + (int64_t)token * a.k;
+    float w[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = fmaf(v[e], a.scale, was[e]);
+    if (gone == 0) {
+        store_out<TO, VEC>(out, at, w);
+        return;
+    }
+    // (the columns before are the lane's before)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const float one[1] = {w[e]};
+        if (e >= gone) store_out<TO, 1>(out, at + e, one);
+    }
+}
+
+// VEC elements as they lie in memory: 16 bytes, or one.
+template <typename T, int VEC>
+struct Packed {
+    std::conditional_t<VEC == 1, float, uint4> w;
+    __device__ __forceinline__ void load(const T *__restrict__ p, int64_t i)
+    {
+        if constexpr (VEC == 1) {
+            float one[1];
+            load_vec<T, 1>(p, i, one);
+            w = one[0];
+        } else {
+            const u32x4_u u = *reinterpret_cast<const u32x4_u *>(p + i);
+            w = make_uint4(u.x, u.y, u.z, u.w);
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&t)[VEC]) const
+    {
+        if constexpr (VEC == 1) {
+            t[0] += w;
+        } else {
+            float v[VEC];
+            RowGather<T, VEC, false>::unpack16(w.x, w.y, w.z, w.w, v);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) t[e] += v[e];
+        }
+    }
+};
+
+// A group of lanes a piece (and a chunk of its columns), a vector a lane.  Bound by the rows' reads.  ADD: the rows
+// that sums are added to are read with the batch that names them first.
 constexpr int kDeep = 8;         // rows a lane has in flight
 
-template <typename TI, typename TO, int VEC>
+template <typename TI, typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(kBlock) void k_scatter_sums(ScatterArgs a)
 {
+    constexpr int D = ADD && sizeof(TI) == 2 ? kDeep / 2 : kDeep;
     const int lane = lane_id() & (a.lanes - 1);
     const int64_t groups = (int64_t)gridDim.x * kBlock >> a.log_lanes;
     const int64_t all = (int64_t)a.pieces * a.chunks;
@@ -148,83 +277,169 @@ __global__ __launch_bounds__(kBlock) void k_scatter_sums(ScatterArgs a)
         const uint32_t after = to < a.n ? a.sorted[to] : ~0u;
         uint32_t token = a.sorted[from];
         bool begun = token == before;
-        float t[VEC];
+        float t[VEC], was[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) t[e] = 0.f;
+        for (int e = 0; e < VEC; ++e) t[e] = was[e] = 0.f;
+        if (ADD && token < (uint32_t)a.V) read_row<TO, VEC>(static_cast<const TO *>(a.out) + (int64_t)token * a.k, at, was);
         const auto flush = [&](int slot) {
-            if (slot < 0) {
-                put<TO, VEC>(a, token, at, gone, t);
-                return;
-            }
             // (columns of two lanes: both write the same sum)
-            store_vec<float, VEC>(a.slots, (2 * piece + slot) * (int64_t)a.k + at, t);
+            if (slot < 0) put<TO, VEC>(a, token, at, gone, t, was);
+            else store_vec<float, VEC>(a.slots, (2 * piece + slot) * (int64_t)a.k + at, t);
         };
-        for (int64_t i0 = from; i0 < to && token < (uint32_t)a.V; i0 += kDeep) {
-            uint32_t tok[kDeep];
-            float v[kDeep][VEC];
+        for (int64_t i0 = from; i0 < to && token < (uint32_t)a.V; i0 += D) {
+            uint32_t tok[D];
+            Packed<TI, VEC> v[D];
+            float base[ADD ? D : 1][VEC];
 #pragma unroll
-            for (int d = 0; d < kDeep; ++d) {
+            for (int d = 0; d < D; ++d) {
                 const int64_t i = i0 + d < to ? i0 + d : to - 1;
                 tok[d] = i0 + d < to ? a.sorted[i] : (uint32_t)a.V;
-                load_vec<TI, VEC>(dY, (int64_t)a.order[i] * a.k + at, v[d]);
+                v[d].load(dY, (int64_t)a.order[i] * a.k + at);
+                if constexpr (ADD) {
+                    if (tok[d] < (uint32_t)a.V && tok[d] != (d > 0 ? tok[d > 0 ? d - 1 : 0] : token))
+                        read_row<TO, VEC>(static_cast<const TO *>(a.out) + (int64_t)tok[d] * a.k, at, base[d]);
+                }
             }
 #pragma unroll
-            for (int d = 0; d < kDeep; ++d) {
+            for (int d = 0; d < D; ++d) {
                 if (tok[d] != token) {
                     if (i0 + d >= to || token >= (uint32_t)a.V) continue;
                     flush(begun ? 0 : -1);
                     begun = false;
                     token = tok[d];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) t[e] = 0.f;
+                    for (int e = 0; e < VEC; ++e) {
+                        t[e] = 0.f;
+                        if constexpr (ADD) was[e] = base[d][e];
+                    }
                     if (token >= (uint32_t)a.V) continue;
                 }
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) t[e] += v[d][e];
+                v[d].add_to(t);
             }
         }
         if (token < (uint32_t)a.V) flush(begun ? 0 : token == after ? 1 : -1);
     }
 }
 
-// Tokens that reach over pieces: the slot of the piece that begins one, then those of the pieces after.
+// Tokens that reach over pieces: the slot of the piece that begins one, then those of the pieces after.  A
+// wavefront looks at a piece; tokens of more pieces than kShort are summed by the whole workgroup, in 16 parts, or
+// more where rows are short.
+constexpr int kShort = 16;
+
+// The sums of slots [q0, q1) of a token that begins in `piece`, columns [c, c + 4) below k.
+__device__ __forceinline__ void sum_slots(const ScatterArgs &a, int64_t piece, int64_t q0, int64_t q1, int c, float (&t)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = 0.f;
+    const bool whole = c + 4 <= a.k;
+    for (int64_t q = q0; q < q1; q += kDeep) {
+        float v[kDeep][4];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            const int64_t at = q + d < q1 ? q + d : q1 - 1;
+            const float *__restrict__ row = a.slots + (2 * (piece + at) + (at == 0 ? 1 : 0)) * (int64_t)a.k + c;
+            if (whole) {
+                load_vec<float, 4>(row, 0, v[d]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[d][e] = c + e < a.k ? row[e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += q + d < q1 ? v[d][e] : 0.f;
+    }
+}
+
 template <typename TO>
 __global__ __launch_bounds__(kBlock) void k_scatter_join(ScatterArgs a)
 {
-    constexpr int kCols = 16, kParts = kBlock / kCols;
-    __shared__ float sums[kParts][kCols];
-    const int part = threadIdx.x / kCols, col = threadIdx.x % kCols;
-    for (int64_t piece = blockIdx.x; piece + 1 < a.pieces; piece += gridDim.x) {
-        const int64_t from = piece * a.per, next = from + a.per;
-        const uint32_t token = a.sorted[next - 1];
-        if (token >= (uint32_t)a.V || a.sorted[next] != token) continue;
-        if (a.sorted[from] == token && from > 0 && a.sorted[from - 1] == token) continue;      // begun before
-        // the last piece that has it: the first that ends otherwise
-        int64_t lo = piece + 1, hi = a.pieces - 1;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            const int64_t end = (mid + 1) * a.per;         // (of a piece before the last)
-            if (a.sorted[end] == token) lo = mid + 1;
-            else hi = mid;
+    constexpr int W = kBlock / kWave;
+    __shared__ float4 sums[kBlock];
+    __shared__ int64_t long_count[W];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const auto finish = [&](uint32_t token, int c, const float (&t)[4]) {
+        const TO *__restrict__ out = static_cast<const TO *>(a.out) + (int64_t)token * a.k;
+        if (c + 4 <= a.k) {
+            float was[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.add) read_row<TO, 4>(out, c, was);
+            put<TO, 4>(a, token, c, 0, t, was);
+            return;
         }
-        const int64_t count = lo - piece + 1;
-        const int64_t p0 = count * part / kParts, p1 = count * (part + 1) / kParts;
-        for (int c0 = 0; c0 < a.k; c0 += kCols) {
-            const int c = c0 + col;
-            float t = 0.f;
-            if (c < a.k) {
-#pragma unroll 4
-                for (int64_t q = p0; q < p1; ++q) t += a.slots[(2 * (piece + q) + (q == 0 ? 1 : 0)) * (int64_t)a.k + c];
-            }
-            __syncthreads();
-            sums[part][col] = t;
-            __syncthreads();
-            if (part == 0 && c < a.k) {
-                for (int q = 1; q < kParts; ++q) t += sums[q][col];
-                const float one[1] = {t};
-                put<TO, 1>(a, token, c, 0, one);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= a.k) continue;
+            const float one[1] = {t[e]};
+            float was[1] = {0.f};
+            if (a.add) read_row<TO, 1>(out, c + e, was);
+            put<TO, 1>(a, token, c + e, 0, one, was);
+        }
+    };
+    for (int64_t p0 = (int64_t)blockIdx.x * W; p0 + 1 < a.pieces; p0 += (int64_t)gridDim.x * W) {
+        const int64_t piece = p0 + wave;
+        int64_t count = 0;
+        uint32_t token = 0;
+        if (piece + 1 < a.pieces) {
+            const int64_t from = piece * a.per, next = from + a.per;
+            token = a.sorted[next - 1];
+            const uint32_t after = a.sorted[next], first = a.sorted[from], before = from > 0 ? a.sorted[from - 1] : ~0u;
+            if (token < (uint32_t)a.V && after == token && !(first == token && before == token)) {
+                // the last piece that has it: the first that ends otherwise (most often the next one)
+                int64_t lo = piece + 1, hi = a.pieces - 1;
+                for (int64_t step = 1; lo < hi; step *= 2) {
+                    const int64_t mid = lo + step - 1 < hi ? lo + step - 1 : hi - 1;
+                    if (a.sorted[(mid + 1) * a.per] != token) {
+                        hi = mid;
+                        break;
+                    }
+                    lo = mid + 1;
+                }
+                while (lo < hi) {
+                    const int64_t mid = (lo + hi) / 2;
+                    if (a.sorted[(mid + 1) * a.per] == token) lo = mid + 1;
+                    else hi = mid;
+                }
+                count = lo - piece + 1;
             }
         }
+        if (count > 0 && count <= kShort) {
+            for (int c = 4 * lane; c < a.k; c += 4 * kWave) {
+                float t[4];
+                sum_slots(a, piece, 0, count, c, t);
+                finish(token, c, t);
+            }
+        }
+        if (lane == 0) long_count[wave] = count > kShort ? count : 0;
+        __syncthreads();
+        for (int w = 0; w < W; ++w) {
+            const int64_t many = long_count[w];
+            if (many == 0) continue;                     // (uniform)
+            const int64_t mine = p0 + w;
+            const uint32_t its = a.sorted[(mine + 1) * a.per];
+            // lanes by 4 columns: 16, fewer of short rows
+            int lanes = 16;
+            while (lanes > 1 && lanes * 2 >= a.k) lanes /= 2;
+            const int parts = kBlock / lanes, part = threadIdx.x / lanes;
+            for (int c0 = 0; c0 < a.k; c0 += 4 * lanes) {
+                const int c = c0 + 4 * ((int)threadIdx.x % lanes);
+                float t[4];
+                sum_slots(a, mine, many * part / parts, many * (part + 1) / parts, c, t);
+                __syncthreads();
+                sums[threadIdx.x] = make_float4(t[0], t[1], t[2], t[3]);
+                __syncthreads();
+                for (int half = parts / 2; half > 0; half /= 2) {
+                    if (part < half) {
+                        const float4 o = sums[threadIdx.x + half * lanes];
+                        t[0] += o.x; t[1] += o.y; t[2] += o.z; t[3] += o.w;
+                        sums[threadIdx.x] = make_float4(t[0], t[1], t[2], t[3]);
+                    }
+                    __syncthreads();
+                }
+                if (part == 0) finish(its, c, t);
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -246,17 +461,36 @@ cogdl_status check_table(int64_t n, int32_t V, int32_t k)
 
 struct Scatter {
     size_t keys, ping_k, ping_v, sorted, order, radix, slots, total;
-    int32_t per;
-    int64_t pieces;
 };
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
+// The sorted list's pieces: all of them at once on the chip (6 wavefronts a SIMD; FIGURE), 16 tokens or more,
+// and no more than the join takes in a few us.
+int32_t piece_of(int64_t n, int32_t vecs)
+{
+    const int lanes = vecs >= kWave ? kWave : next_pow2(vecs);
+    const int64_t wide = (int64_t)((vecs + lanes - 1) / lanes) * lanes;      // of a piece
+    int64_t per = (n * wide + kWave * 4608 - 1) / (kWave * 4608);
+    if (per < n / 16384) per = n / 16384;
+    if (per > 256) per = 256;
+    per = (per + kDeep - 1) / kDeep * kDeep;
+    return (int32_t)(per < 16 ? 16 : per);
+}
+
+// 16-byte vectors of a row, or its elements where it has under one.
+int32_t vecs_of(int32_t k, int bytes)
+{
+    const int vec = 16 / bytes;
+    return k >= vec ? (k + vec - 1) / vec : k;
+}
+
 Scatter scatter_layout(int64_t n, int32_t k)
 {
     Scatter s;
-    s.per = n < (1 << 16) ? 16 : n < (1 << 18) ? 32 : 64;
-    s.pieces = (n + s.per - 1) / s.per;
+    // (the type is not known here: the more pieces of the two)
+    const int32_t p2 = piece_of(n, vecs_of(k, 2)), p4 = piece_of(n, vecs_of(k, 4));
+    const int64_t pieces = (n + (p2 < p4 ? p2 : p4) - 1) / (p2 < p4 ? p2 : p4);
     size_t off = 0;
     s.keys = off; off += al(4 * (size_t)n);
     s.ping_k = off; off += al(8 * (size_t)n);
@@ -264,7 +498,7 @@ Scatter scatter_layout(int64_t n, int32_t k)
     s.sorted = off; off += al(4 * (size_t)n);
     s.order = off; off += al(4 * (size_t)n);
     s.radix = off; off += al(radix_workspace_bytes(n));
-    s.slots = off; off += al(8 * (size_t)s.pieces * k);
+    s.slots = off; off += al(8 * (size_t)pieces * k);
     s.total = off;
     return s;
 }
@@ -291,10 +525,11 @@ cogdl_status run_scatter(ScatterArgs a, hipStream_t stream)
     const int64_t groups = (int64_t)a.pieces * a.chunks;
     int64_t blocks = ((groups << a.log_lanes) + kBlock - 1) / kBlock;
     if (blocks > (1 << 20)) blocks = 1 << 20;
-    COGDL_LAUNCH("embedding_sums", (k_scatter_sums<TI, TO, VEC>), (unsigned)blocks, kBlock, stream, a);
+    if (a.add) COGDL_LAUNCH("embedding_sums", (k_scatter_sums<TI, TO, VEC, true>), (unsigned)blocks, kBlock, stream, a);
+    else COGDL_LAUNCH("embedding_sums", (k_scatter_sums<TI, TO, VEC, false>), (unsigned)blocks, kBlock, stream, a);
     if (a.pieces > 1) {
-        const unsigned joins = a.pieces < (1 << 16) ? (unsigned)a.pieces : 1u << 16;
-        COGDL_LAUNCH("embedding_join", k_scatter_join<TO>, joins, kBlock, stream, a);
+        const int64_t joins = (a.pieces + kBlock / kWave - 2) / (kBlock / kWave);
+        COGDL_LAUNCH("embedding_join", k_scatter_join<TO>, (unsigned)(joins < (1 << 16) ? joins : 1 << 16), kBlock, stream, a);
     }
     return COGDL_OK;
 }
@@ -365,20 +600,28 @@ cogdl_status cogdl_embedding_backward(int64_t n, int32_t V, int32_t k, const voi
         a.sorted = reinterpret_cast<uint32_t *>(ws + s.sorted);
         a.order = reinterpret_cast<uint32_t *>(ws + s.order);
         a.slots = reinterpret_cast<float *>(ws + s.slots);
-        a.per = s.per;
-        a.pieces = (int32_t)s.pieces;
+        a.per = piece_of(n, vecs_of(k, dtype_bytes(dtype)));
+        a.pieces = (int32_t)((n + a.per - 1) / a.per);
     } else if (a.add) {
         return COGDL_OK;
     }
-    int64_t blocks = a.add ? (n + kBlock - 1) / kBlock : ((int64_t)V * k * a.out_bytes / 16 + n + kBlock - 1) / kBlock + 1;
-    if (blocks > 4096) blocks = 4096;
-    COGDL_LAUNCH("embedding_tokens", k_tokens, (unsigned)blocks, kBlock, stream, a);
-    if (n == 0) return COGDL_OK;
-    char *ws = static_cast<char *>(workspace);
-    const Scatter s = scatter_layout(n, k);
-    COGDL_HIP_TRY(radix_sort_pairs(a.keys, nullptr, const_cast<uint32_t *>(a.sorted), const_cast<uint32_t *>(a.order), n,
-                                   bits_for((uint64_t)V), reinterpret_cast<uint32_t *>(ws + s.ping_k),
-                                   reinterpret_cast<uint32_t *>(ws + s.ping_v), ws + s.radix, stream));
+    const int64_t zeros = a.add ? 0 : ((int64_t)V * k * a.out_bytes + 15) / 16;      // threads for them
+    const int bits = bits_for((uint64_t)V);
+    if (n > 0 && n <= kShortList) {
+        int64_t blocks = (zeros + kSortThreads - 1) / kSortThreads;
+        if (blocks > 1024) blocks = 1024;
+        COGDL_LAUNCH("embedding_sort", k_sort_short, (unsigned)(blocks + 1), kSortThreads, stream, a, bits);
+    } else {
+        int64_t blocks = ((n > zeros ? n : zeros) + kBlock - 1) / kBlock;
+        if (blocks > 4096) blocks = 4096;
+        COGDL_LAUNCH("embedding_tokens", k_tokens, (unsigned)blocks, kBlock, stream, a);
+        if (n == 0) return COGDL_OK;
+        char *ws = static_cast<char *>(workspace);
+        const Scatter s = scatter_layout(n, k);
+        COGDL_HIP_TRY(radix_sort_pairs(a.keys, nullptr, const_cast<uint32_t *>(a.sorted), const_cast<uint32_t *>(a.order),
+                                       n, bits, reinterpret_cast<uint32_t *>(ws + s.ping_k),
+                                       reinterpret_cast<uint32_t *>(ws + s.ping_v), ws + s.radix, stream));
+    }
     return by_type(dtype, [&](auto ti) {
         using TI = decltype(ti);
         return by_type(d_dtype, [&](auto to) {

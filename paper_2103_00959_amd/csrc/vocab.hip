@@ -2,8 +2,8 @@
 // logits, of logits X W^T + bias that are never kept (the formulas: vocab.hpp).
 //
 // A tile of logits stays in the accumulators of the matrix cores; what leaves it is each row's (max, sum of
-// exp) over a slot of 64 columns.  A last kernel joins the slots and computes the logits of the targets as
-// plain dot products.
+// exp) over a slot of 64 columns.  A last kernel joins the slots.  The logits of the targets are
+// plain dot products, as the rows are gathered.
 #include "vocab.hpp"
 
 namespace cogdl {
@@ -13,8 +13,30 @@ constexpr int kBlock = 256;
 
 __device__ __forceinline__ bool counts(int32_t t, int32_t V) { return (uint32_t)t < (uint32_t)V; }
 
+// 8 features from column 8 v on of a row of k, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ uint4 load_vec8(const T *__restrict__ row, int v, int k)
+{
+    if (8 * v + 8 > k) return load_short(row + 8 * v, k - 8 * v);
+    const u32x4_u u = *reinterpret_cast<const u32x4_u *>(row + 8 * v);
+    return make_uint4(u.x, u.y, u.z, u.w);
+}
+
+template <typename T>
+__device__ __forceinline__ float dot8(uint4 a, uint4 b, float t)
+{
+    float f[8], g[8];
+    unpack8<T>(a, f);
+    unpack8<T>(b, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = fmaf(f[e], g[e], t);
+    return t;
+}
+
 // The teacher's rows: whether any entry counts (inside the vocabulary, its logit above -inf), and the log of
-// the sum of their exponentials.  A wavefront a row.
+// the sum of their exponentials.  FORWARD: also the student's logits of the entries, by 4 entries of 16 lanes,
+// into logp.  A wavefront a row.
+template <typename T, bool FORWARD>
 __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
 {
     const int lane = lane_id();
@@ -41,10 +63,28 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
             a.live[i] = live ? 0 : -1;
             a.tlse[i] = from + logf(s);
         }
+        if constexpr (FORWARD) {
+            const T *__restrict__ x = static_cast<const T *>(a.X) + i * a.k;
+            const int sub = lane & 15, vecs = a.kp / 8;
+            for (int e0 = 0; e0 < a.entries; e0 += kWave / 16) {
+                const int e = e0 + (lane >> 4);
+                const int32_t v = e < a.entries ? index[e] : -1;
+                const bool on = live && counts(v, a.V);
+                const T *__restrict__ w = static_cast<const T *>(a.W) + (int64_t)(on ? v : 0) * a.k;
+                float z = 0.f;
+                if (on) {
+#pragma unroll 4
+                    for (int c = sub; c < vecs; c += 16) z = dot8<T>(load_vec8(w, c, a.k), load_vec8(x, c, a.k), z);
+                }
+                z = group_sum(z, 16);
+                if (sub == 0 && e < a.entries) a.logp[i * a.entries + e] = on ? (a.bias ? z + a.bias[v] : z) / a.T : 0.f;
+            }
+        }
     }
 }
 
-// The rows that count, in order, and their features.  A workgroup takes `per` rows; how many count before them
+// The rows that count, in order, and their features; in the forward of the cross entropy also their targets'
+// logits, into loss.  A workgroup takes `per` rows; how many count before them
 // it finds by itself, from the targets (n targets a workgroup, from the L2s).
 template <typename T, bool BACKWARD>
 __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
@@ -114,29 +154,33 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
             }
         }
         const int here = to - r0 < kWave ? (int)(to - r0) : kWave;
+#pragma unroll 2
         for (int r = wave; r < here; r += W) {
             const bool on = mask >> r & 1;
             const int64_t i1 = r0 + r;
             if (on) {
                 const int64_t p = at + __popcll(mask & ((1ull << r) - 1));
+                const T *__restrict__ x = X + i1 * a.k;
+                const int32_t v1 = !BACKWARD && !a.distill ? a.index[i1] : 0;
+                const T *__restrict__ w = static_cast<const T *>(a.W) + (int64_t)v1 * a.k;
+                float z = 0.f;
                 for (int v = lane; v < vecs; v += kWave) {
-                    uint4 w;
-                    const T *__restrict__ src = X + i1 * a.k;
-                    if (8 * v + 8 <= a.k) {
-                        const u32x4_u u = *reinterpret_cast<const u32x4_u *>(src + 8 * v);
-                        w = make_uint4(u.x, u.y, u.z, u.w);
-                    } else {
-                        w = load_short(src + 8 * v, a.k - 8 * v);
+                    const uint4 f = load_vec8(x, v, a.k);
+                    *reinterpret_cast<uint4 *>(Xr + p * a.kp + 8 * v) = f;
+                    if constexpr (!BACKWARD)
+                        if (!a.distill) z = dot8<T>(f, load_vec8(w, v, a.k), z);
+                }
+                if constexpr (!BACKWARD) {
+                    if (!a.distill) {
+                        z = group_sum(z, kWave);
+                        if (lane == 0) a.loss[i1] = a.bias ? z + a.bias[v1] : z;
                     }
-                    *reinterpret_cast<uint4 *>(Xr + p * a.kp + 8 * v) = w;
                 }
             } else if constexpr (BACKWARD) {
                 if (dX) {
                     const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                     for (int v = lane; v < vecs; v += kWave) store8(dX + i1 * a.k, 8 * v, a.k, zeros);
                 }
-            } else if (a.logp) {
-                for (int e = lane; e < a.entries; e += kWave) a.logp[i1 * a.entries + e] = 0.f;
             }
         }
         at += __popcll(mask);
@@ -253,10 +297,9 @@ __global__ __launch_bounds__(WAVES * kWave) void k_vocab_logits(VocabArgs a)
         });
 }
 
-// The slots of a row joined to its lse, the targets' logits, and the loss.  kRowsBlock rows a workgroup.
+// The slots of a row joined to its lse, and the loss from its targets' logits.  kRowsBlock rows a workgroup.
 constexpr int kRowsBlock = 16;
 
-template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a)
 {
     constexpr int W = kBlock / kWave, S = kBlock / kRowsBlock;
@@ -285,54 +328,33 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a)
             const float from = top == -INFINITY ? 0.f : top;
             float sum = 0.f;
             for (int s = 0; s < S; ++s) sum += part[s][r].y * __builtin_amdgcn_exp2f(part[s][r].x - from);
-            lse_of[r] = (from + log2f(sum)) * kLn2;
-        }
-        __syncthreads();
-        for (int q = wave; q < kRowsBlock && r0 + q < live; q += W) {
-            const int64_t p = r0 + q, i = a.rows[p];
-            const float lse = lse_of[q];
-            const T *__restrict__ x = static_cast<const T *>(a.Xr) + p * a.kp;
-            float loss = 0.f;
-            for (int e = 0; e < a.entries; ++e) {
-                const int32_t v = a.index[i * a.entries + e];
-                if (!counts(v, a.V)) {
-                    if (a.distill && lane == 0) a.logp[i * a.entries + e] = 0.f;
-                    continue;
-                }
-                const T *__restrict__ w = static_cast<const T *>(a.W) + (int64_t)v * a.k;
-                float t = 0.f;
-                for (int c = lane; c < a.kp / 8; c += kWave) {
-                    uint4 ww;
-                    if (8 * c + 8 <= a.k) {
-                        const u32x4_u u = *reinterpret_cast<const u32x4_u *>(w + 8 * c);
-                        ww = make_uint4(u.x, u.y, u.z, u.w);
-                    } else {
-                        ww = load_short(w + 8 * c, a.k - 8 * c);
-                    }
-                    const uint4 xx = *reinterpret_cast<const uint4 *>(x + 8 * c);
-                    float f[8], g[8];
-                    unpack8<T>(ww, f);
-                    unpack8<T>(xx, g);
-#pragma unroll
-                    for (int h = 0; h < 8; ++h) t = fmaf(f[h], g[h], t);
-                }
-                t = group_sum(t, kWave);
-                if (a.bias) t += a.bias[v];
+            const float lse = (from + log2f(sum)) * kLn2;
+            lse_of[r] = lse;
+            if (r0 + r < live) {
+                const int64_t i = a.rows[r0 + r];
+                a.lse[i] = lse;
                 if (!a.distill) {
                     // (above 0 by definition; the two sums' roundings may differ)
-                    loss = lse - t;
-                    loss = loss < 0.f ? 0.f : loss;
-                } else {
-                    const float logp = t / a.T - lse, logq = a.teacher[i * a.entries + e] / a.T - a.tlse[i];
-                    const float share = expf(logq);
-                    if (!(share == 0.f)) loss += share * (logq - logp);
-                    if (lane == 0) a.logp[i * a.entries + e] = logp;
+                    const float loss = lse - a.loss[i];
+                    a.loss[i] = loss < 0.f ? 0.f : loss;
                 }
             }
-            if (lane == 0) {
-                a.lse[i] = lse;
-                a.loss[i] = a.distill ? loss * a.T * a.T : loss;
+        }
+        __syncthreads();
+        if (!a.distill) continue;
+        for (int q = wave; q < kRowsBlock && r0 + q < live; q += W) {
+            const int64_t i = a.rows[r0 + q];
+            const float lse = lse_of[q], tlse = a.tlse[i];
+            float loss = 0.f;
+            for (int e = lane; e < a.entries; e += kWave) {
+                if (!counts(a.index[i * a.entries + e], a.V)) continue;       // (logp is 0)
+                const float logp = a.logp[i * a.entries + e] - lse, logq = a.teacher[i * a.entries + e] / a.T - tlse;
+                a.logp[i * a.entries + e] = logp;
+                const float share = expf(logq);
+                if (!(share == 0.f)) loss += share * (logq - logp);
             }
+            loss = group_sum(loss, kWave);
+            if (lane == 0) a.loss[i] = loss * a.T * a.T;
         }
         __syncthreads();
     }
@@ -356,10 +378,13 @@ cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backw
 {
     if (a.distill && a.n > 0) {
         const int64_t blocks = (a.n + kBlock / kWave - 1) / (kBlock / kWave);
-        COGDL_LAUNCH("teacher_rows", k_teacher_rows, (unsigned)(blocks < 4096 ? blocks : 4096), kBlock, stream, a);
+        const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
+        if (backward) COGDL_LAUNCH("teacher_rows", (k_teacher_rows<bf16_t, false>), grid, kBlock, stream, a);    // (no features)
+        else if (dtype == COGDL_BF16) COGDL_LAUNCH("teacher_rows", (k_teacher_rows<bf16_t, true>), grid, kBlock, stream, a);
+        else COGDL_LAUNCH("teacher_rows", (k_teacher_rows<f16_t, true>), grid, kBlock, stream, a);
     }
-    int64_t per = (a.n + 255) / 256;
-    per = per < 16 ? 16 : per;
+    int64_t per = (a.n + 511) / 512;
+    per = per < 8 ? 8 : per;
     const unsigned blocks = a.n > 0 ? (unsigned)((a.n + per - 1) / per) : 1;
     if (dtype == COGDL_BF16) {
         if (backward) COGDL_LAUNCH("vocab_rows", (k_vocab_rows<bf16_t, true>), blocks, kBlock, stream, a, (int)per);
@@ -442,8 +467,7 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     if (s != COGDL_OK) return s;
     int64_t blocks = (a.n + kRowsBlock - 1) / kRowsBlock;
     if (blocks > 4096) blocks = 4096;
-    if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a);
-    else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a);
+    COGDL_LAUNCH("vocab_finish", k_vocab_finish, (unsigned)blocks, kBlock, stream, a);
     return COGDL_OK;
 }
 

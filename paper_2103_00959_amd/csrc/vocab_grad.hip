@@ -199,6 +199,9 @@ VocabKernel pick_dw(bool wide)
 
 int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1) / tile * ((cols + tile - 1) / tile); }
 
+// Partial sums of dX, at most.
+constexpr int64_t kMostSlices = 64;
+
 // The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).
 constexpr int64_t kPieceBytes = 256ll << 20;
 
@@ -206,6 +209,9 @@ struct Pieces {
     int32_t width;               // of a piece, the last may be smaller
     int32_t slices;              // of a piece, in dX's sums
 };
+
+// Whether dX's sums over a piece of `width` take tiles of 256 x 256 (where W is on the grid).
+bool wide_dx(int64_t n, int64_t width, int32_t k) { return k > 128 && k % 2 == 0 && tiles_of(n, k, 256) * (width / 512) >= 256; }
 
 Pieces pieces_of(int64_t n, int32_t V, int32_t k)
 {
@@ -217,10 +223,18 @@ Pieces pieces_of(int64_t n, int32_t V, int32_t k)
     if (width > V) width = V;
     Pieces p;
     p.width = (int32_t)width;
-    const int64_t tiles = tiles_of(n, k, 128);
-    int64_t slices = tiles > 0 ? 512 / tiles : 1;
-    const int64_t most = width / 256;
-    if (slices > most) slices = most;
+    const bool wide = wide_dx(n, width, k);
+    const int64_t tiles = tiles_of(n, k, wide ? 256 : 128), want = wide ? 256 : 512;
+    // the fewest rounds of resident workgroups for the work of a slice; a slice more has to gain a tenth
+    const int64_t most = width / (wide ? 512 : 256);
+    int64_t slices = 1, rounds = (tiles + want - 1) / want;
+    for (int64_t s = 2; s <= most && s <= kMostSlices; ++s) {
+        const int64_t r = (tiles * s + want - 1) / want;
+        if (10 * r * slices < 9 * rounds * s) {
+            slices = s;
+            rounds = r;
+        }
+    }
     p.slices = (int32_t)(slices < 1 ? 1 : slices);
     return p;
 }
@@ -310,7 +324,7 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
             else COGDL_LAUNCH("vocab_targets", k_vocab_targets<f16_t>, (unsigned)blocks, kBlock, stream, a);
         }
         if (a.dX) {
-            const bool wide = on_grid(a.W, a.k) && a.k > 128 && tiles_of(a.n, a.k, 256) * a.slices >= 128;
+            const bool wide = on_grid(a.W, a.k) && wide_dx(a.n, piece, a.k);
             const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
             a.tiles_c = (a.k + tile - 1) / tile;
             COGDL_TRY(launch_vocab("vocab_dx", bf16 ? pick_dx<bf16_t>(wide, on_grid(a.W, a.k)) : pick_dx<f16_t>(wide, on_grid(a.W, a.k)),
