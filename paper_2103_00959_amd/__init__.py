@@ -1104,17 +1104,40 @@ def grouped_linear_backward(dY, W, offsets, X=None, codes=None, exps=None, Y=Non
     return o
 
 
-def _scratch(workspace, need, like):
-    """A workspace of at least `need` bytes (None: a fresh one, or None where nothing is needed)."""
+def _take(t, name, dtype, device):
+    """The address of a contiguous tensor of this dtype (None: of any) on this device; None for None."""
+    if t is None:
+        return None
+    if (dtype is not None and t.dtype is not dtype) or t.get_device() != device or not t.is_contiguous():
+        _dev(t, name, dtype)
+        raise CogdlError(f"the tensors lie on several devices: {name} on {t.get_device()}, others on {device}")
+    return t.data_ptr()
+
+
+def _home(t, name):
+    """The device of the tensor that the others have to share, and a context with it current."""
+    import torch
+    if not t.is_cuda:
+        raise CogdlError(f"{name} must be a CUDA (HIP) tensor")
+    device = t.get_device()
+    return device, _HERE if device == torch._C._cuda_getDevice() else torch.cuda.device(device)
+
+
+def _stream_of(device):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _scratch(workspace, need, like, device):
+    """(address, bytes, tensor) of a workspace of at least `need` bytes: the one given, or a fresh one."""
     import torch
     if workspace is None:
-        return like.new_empty(need, dtype=torch.uint8) if need > 0 else None
+        if need == 0:
+            return None, 0, None
+        workspace = like.new_empty(need, dtype=torch.uint8)
+        return workspace.data_ptr(), need, workspace
     _at_least(workspace, "workspace", (need + workspace.element_size() - 1) // workspace.element_size())
-    return _dev(workspace, "workspace")
-
-
-def _bytes(workspace):
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _take(workspace, "workspace", None, device), workspace.numel() * workspace.element_size(), workspace
 
 
 def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
@@ -1127,13 +1150,14 @@ def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
         raise CogdlError("table needs at least one row")
     n = _index_array(index, "index")
     _numel(out, "out", n * k)
-    _dev(table, "table"), _dev(index, "index", torch.int32)
+    device, here = _home(table, "table")
+    pt, pi = _take(table, "table", None, device), _take(index, "index", torch.int32, device)
     if out is None:
         out = table.new_empty((n, k), dtype=out_dtype or table.dtype)
-    _dev(out, "out")
-    with _on_device(table, index, out):
-        _check(lib().cogdl_embedding(n, V, k, _addr(table), _dtype_code(table), _addr(index), float(scale), _addr(out),
-                                     _dtype_code(out), _stream()), "cogdl_embedding")
+    po = _take(out, "out", None, device)
+    with here:
+        _check(lib().cogdl_embedding(n, V, k, pt, _dtype_code(table), pi, scale, po, _dtype_code(out),
+                                     _stream_of(device)), "cogdl_embedding")
     return out
 
 
@@ -1155,7 +1179,6 @@ def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, ou
     bytes."""
     import torch
     n, k = _dims(dY, "dY", 2)
-    V = int(V)
     if V < 1:
         raise CogdlError("the table needs at least one row")
     _index_array(index, "index")
@@ -1164,15 +1187,16 @@ def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, ou
     if accumulate and out is None:
         raise CogdlError("accumulate needs out, the gradient to add to")
     need = embedding_backward_workspace(n, V, k)
-    _dev(dY, "dY"), _dev(index, "index", torch.int32)
+    device, here = _home(dY, "dY")
+    pd, pi = _take(dY, "dY", None, device), _take(index, "index", torch.int32, device)
     if out is None:
         out = dY.new_empty((V, k), dtype=out_dtype or dY.dtype)
-    _dev(out, "out")
-    workspace = _scratch(workspace, need, dY)
-    with _on_device(dY, index, out, workspace):
-        _check(lib().cogdl_embedding_backward(n, V, k, _addr(dY), _dtype_code(dY), _addr(index), float(scale),
-                                              _addr(out), _dtype_code(out), int(bool(accumulate)), _addr(workspace),
-                                              _bytes(workspace), _stream()), "cogdl_embedding_backward")
+    po = _take(out, "out", None, device)
+    pw, bytes_, workspace = _scratch(workspace, need, dY, device)
+    with here:
+        _check(lib().cogdl_embedding_backward(n, V, k, pd, _dtype_code(dY), pi, scale, po, _dtype_code(out),
+                                              1 if accumulate else 0, pw, bytes_, _stream_of(device)),
+               "cogdl_embedding_backward")
     return out
 
 
@@ -1197,15 +1221,16 @@ def linear_loss_backward_workspace(n: int, V: int, k: int, K: int = 0) -> int:
 
 
 def _head(X, W, bias):
-    """(n, V, k) of a linear layer over a vocabulary, with its sizes checked."""
+    """(n, V, k, dtype code) of a linear layer over a vocabulary, with its sizes checked."""
     n, k = _dims(X, "X", 2)
     V, kw = _dims(W, "W", 2)
     if kw != k or X.dtype != W.dtype:
         raise CogdlError("X must be [n, k] and W [V, k] of the same dtype")
     if V < 1:
         raise CogdlError("W needs at least one row")
-    _numel(bias, "bias", V)
-    return n, V, k
+    if bias is not None:
+        _numel(bias, "bias", V)
+    return n, V, k, _dtype_code(X)
 
 
 def _teacher(index, teacher, n, temperature):
@@ -1220,19 +1245,6 @@ def _teacher(index, teacher, n, temperature):
     return K
 
 
-def _loss_outputs(X, shapes, given):
-    """The forward's fp32 outputs: those given, checked, or fresh ones."""
-    import torch
-    outs = []
-    for (name, shape), t in zip(shapes.items(), given):
-        size = 1
-        for d in shape:
-            size *= d
-        _numel(t, name, size)
-        outs.append(X.new_empty(shape, dtype=torch.float32) if t is None else _dev(t, name, torch.float32))
-    return outs
-
-
 def linear_cross_entropy(X, W, target, bias=None, loss=None, lse=None, workspace=None):
     """Softmax cross entropy of the logits z = X W^T + bias over a large vocabulary, which are never kept: returns
     (loss, lse), fp32 [n] each, with lse = logsumexp(z) and loss = lse - z[target].  X [n, k] and W [V, k] both
@@ -1240,18 +1252,24 @@ def linear_cross_entropy(X, W, target, bias=None, loss=None, lse=None, workspace
     bias fp32 [V] or None (-inf takes an answer out).  ``workspace``: at least linear_loss_workspace bytes.  Not
     recorded by autograd: the gradients are linear_cross_entropy_backward's."""
     import torch
-    n, V, k = _head(X, W, bias)
+    n, V, k, dt = _head(X, W, bias)
     _index_array(target, "target")
     _numel(target, "target", n)
     _numel(loss, "loss", n), _numel(lse, "lse", n)
     need = linear_loss_workspace(n, V, k)
-    _dev(X, "X"), _dev(W, "W"), _dev(target, "target", torch.int32), _dev(bias, "bias", torch.float32)
-    loss, lse = _loss_outputs(X, {"loss": (n,), "lse": (n,)}, (loss, lse))
-    workspace = _scratch(workspace, need, X)
-    with _on_device(X, W, target, bias, loss, lse, workspace):
-        _check(lib().cogdl_linear_cross_entropy(n, V, k, _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(target),
-                                                _addr(loss), _addr(lse), _addr(workspace), _bytes(workspace),
-                                                _stream()), "cogdl_linear_cross_entropy")
+    device, here = _home(X, "X")
+    f32, i32 = torch.float32, torch.int32
+    px, pw, pt = _take(X, "X", None, device), _take(W, "W", None, device), _take(target, "target", i32, device)
+    pb = _take(bias, "bias", f32, device)
+    if loss is None:
+        loss = X.new_empty(n, dtype=f32)
+    if lse is None:
+        lse = X.new_empty(n, dtype=f32)
+    pl, ps = _take(loss, "loss", f32, device), _take(lse, "lse", f32, device)
+    ws, bytes_, workspace = _scratch(workspace, need, X, device)
+    with here:
+        _check(lib().cogdl_linear_cross_entropy(n, V, k, px, pw, dt, pb, pt, pl, ps, ws, bytes_, _stream_of(device)),
+               "cogdl_linear_cross_entropy")
     return loss, lse
 
 
@@ -1263,37 +1281,46 @@ def linear_distill(X, W, index, teacher, bias=None, temperature: float = 1.0, lo
     fp32.  index int32 [n, K] (outside [0, V): no entry), teacher fp32 [n, K]; a row without entries is left out
     (zeros).  Everything else as linear_cross_entropy; the gradients are linear_distill_backward's."""
     import torch
-    n, V, k = _head(X, W, bias)
+    n, V, k, dt = _head(X, W, bias)
     K = _teacher(index, teacher, n, temperature)
     _numel(loss, "loss", n), _numel(lse, "lse", n), _numel(logp, "logp", n * K)
     need = linear_loss_workspace(n, V, k, K)
-    _dev(X, "X"), _dev(W, "W"), _dev(index, "index", torch.int32), _dev(teacher, "teacher", torch.float32)
-    _dev(bias, "bias", torch.float32)
-    loss, lse, logp = _loss_outputs(X, {"loss": (n,), "lse": (n,), "logp": (n, K)}, (loss, lse, logp))
-    workspace = _scratch(workspace, need, X)
-    with _on_device(X, W, index, teacher, bias, loss, lse, logp, workspace):
-        _check(lib().cogdl_linear_distill(n, V, k, K, _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(index),
-                                          _addr(teacher), float(temperature), _addr(loss), _addr(lse), _addr(logp),
-                                          _addr(workspace), _bytes(workspace), _stream()), "cogdl_linear_distill")
+    device, here = _home(X, "X")
+    f32, i32 = torch.float32, torch.int32
+    px, pw, pi = _take(X, "X", None, device), _take(W, "W", None, device), _take(index, "index", i32, device)
+    pt, pb = _take(teacher, "teacher", f32, device), _take(bias, "bias", f32, device)
+    if loss is None:
+        loss = X.new_empty(n, dtype=f32)
+    if lse is None:
+        lse = X.new_empty(n, dtype=f32)
+    if logp is None:
+        logp = X.new_empty((n, K), dtype=f32)
+    pl, ps, pp = _take(loss, "loss", f32, device), _take(lse, "lse", f32, device), _take(logp, "logp", f32, device)
+    ws, bytes_, workspace = _scratch(workspace, need, X, device)
+    with here:
+        _check(lib().cogdl_linear_distill(n, V, k, K, px, pw, dt, pb, pi, pt, temperature, pl, ps, pp, ws, bytes_,
+                                          _stream_of(device)), "cogdl_linear_distill")
     return loss, lse, logp
 
 
-def _head_gradients(X, W, bias, out):
-    """The gradients' outputs: those given, checked, or fresh ones (db where there is a bias)."""
+def _head_gradients(X, W, bias, out, device):
+    """The gradients' outputs, those given, checked, or fresh ones (db where there is a bias), and their addresses."""
     import torch
-    n, k = X.shape
-    V = W.shape[0]
-    o = dict(out or {})
-    sizes = {"dX": n * k, "dW": V * k, "db": V}
+    if out is None:
+        dX, dW = torch.empty_like(X), torch.empty_like(W)
+        db = None if bias is None else torch.empty_like(bias)
+        return {"dX": dX, "dW": dW, "db": db}, dX.data_ptr(), dW.data_ptr(), None if db is None else db.data_ptr()
+    o = dict(out)
+    sizes = {"dX": X.numel(), "dW": W.numel(), "db": W.shape[0]}
     for name, t in o.items():
         if name not in sizes:
             raise CogdlError(f"unknown output {name!r}")
         _numel(t, name, sizes[name])
-    for name, t, dtype in (("dX", X, X.dtype), ("dW", W, X.dtype), ("db", bias, torch.float32)):
+    for name, like in (("dX", X), ("dW", W), ("db", bias)):
         if name not in o:
-            o[name] = None if t is None else torch.empty_like(t)
-        _dev(o[name], name, dtype)
-    return o
+            o[name] = None if like is None else torch.empty_like(like)
+    return (o, _take(o["dX"], "dX", X.dtype, device), _take(o["dW"], "dW", X.dtype, device),
+            _take(o["db"], "db", torch.float32, device))
 
 
 def linear_cross_entropy_backward(dloss, X, W, target, loss, lse, bias=None, out=None, workspace=None):
@@ -1303,21 +1330,23 @@ def linear_cross_entropy_backward(dloss, X, W, target, loss, lse, bias=None, out
     Rows left out get zeros in dX and enter no sum.  ``out`` may supply the tensors; a None among them leaves that
     gradient out.  ``workspace``: at least linear_loss_backward_workspace bytes."""
     import torch
-    n, V, k = _head(X, W, bias)
+    n, V, k, dt = _head(X, W, bias)
     _index_array(target, "target")
-    for name, t in (("dloss", dloss), ("target", target), ("loss", loss), ("lse", lse)):
-        _tensor(t, name)
-        _numel(t, name, n)
+    _numel(target, "target", n)
+    for name, t in (("dloss", dloss), ("loss", loss), ("lse", lse)):
+        if _tensor(t, name).numel() != n:
+            _numel(t, name, n)
     need = linear_loss_backward_workspace(n, V, k)
-    _dev(X, "X"), _dev(W, "W"), _dev(target, "target", torch.int32), _dev(bias, "bias", torch.float32)
-    _dev(dloss, "dloss", torch.float32), _dev(loss, "loss", torch.float32), _dev(lse, "lse", torch.float32)
-    o = _head_gradients(X, W, bias, out)
-    workspace = _scratch(workspace, need, X)
-    with _on_device(X, W, target, bias, dloss, loss, lse, o["dX"], o["dW"], o["db"], workspace):
-        _check(lib().cogdl_linear_cross_entropy_backward(
-            n, V, k, _addr(dloss), _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(target), _addr(loss),
-            _addr(lse), _addr(o["dX"]), _addr(o["dW"]), _addr(o["db"]), _addr(workspace), _bytes(workspace),
-            _stream()), "cogdl_linear_cross_entropy_backward")
+    device, here = _home(X, "X")
+    f32, i32 = torch.float32, torch.int32
+    px, pw, pt = _take(X, "X", None, device), _take(W, "W", None, device), _take(target, "target", i32, device)
+    pb, pd = _take(bias, "bias", f32, device), _take(dloss, "dloss", f32, device)
+    pl, ps = _take(loss, "loss", f32, device), _take(lse, "lse", f32, device)
+    o, dx, dw, db = _head_gradients(X, W, bias, out, device)
+    ws, bytes_, workspace = _scratch(workspace, need, X, device)
+    with here:
+        _check(lib().cogdl_linear_cross_entropy_backward(n, V, k, pd, px, pw, dt, pb, pt, pl, ps, dx, dw, db, ws, bytes_,
+                                                         _stream_of(device)), "cogdl_linear_cross_entropy_backward")
     return o
 
 
@@ -1326,20 +1355,20 @@ def linear_distill_backward(dloss, X, W, index, teacher, lse, logp, bias=None, t
     """Gradients of linear_distill for dloss = dL/dloss fp32 [n], from the forward's lse and logp: returns
     dict(dX, dW, db) as linear_cross_entropy_backward does (none of the teacher's logits)."""
     import torch
-    n, V, k = _head(X, W, bias)
+    n, V, k, dt = _head(X, W, bias)
     K = _teacher(index, teacher, n, temperature)
     for name, t, size in (("dloss", dloss, n), ("lse", lse, n), ("logp", logp, n * K)):
-        _tensor(t, name)
-        _numel(t, name, size)
+        if _tensor(t, name).numel() != size:
+            _numel(t, name, size)
     need = linear_loss_backward_workspace(n, V, k, K)
-    _dev(X, "X"), _dev(W, "W"), _dev(index, "index", torch.int32), _dev(teacher, "teacher", torch.float32)
-    _dev(bias, "bias", torch.float32), _dev(dloss, "dloss", torch.float32), _dev(lse, "lse", torch.float32)
-    _dev(logp, "logp", torch.float32)
-    o = _head_gradients(X, W, bias, out)
-    workspace = _scratch(workspace, need, X)
-    with _on_device(X, W, index, teacher, bias, dloss, lse, logp, o["dX"], o["dW"], o["db"], workspace):
-        _check(lib().cogdl_linear_distill_backward(
-            n, V, k, K, _addr(dloss), _addr(X), _addr(W), _dtype_code(X), _addr(bias), _addr(index), _addr(teacher),
-            float(temperature), _addr(lse), _addr(logp), _addr(o["dX"]), _addr(o["dW"]), _addr(o["db"]),
-            _addr(workspace), _bytes(workspace), _stream()), "cogdl_linear_distill_backward")
+    device, here = _home(X, "X")
+    f32, i32 = torch.float32, torch.int32
+    px, pw, pi = _take(X, "X", None, device), _take(W, "W", None, device), _take(index, "index", i32, device)
+    pt, pb = _take(teacher, "teacher", f32, device), _take(bias, "bias", f32, device)
+    pd, ps, pp = _take(dloss, "dloss", f32, device), _take(lse, "lse", f32, device), _take(logp, "logp", f32, device)
+    o, dx, dw, db = _head_gradients(X, W, bias, out, device)
+    ws, bytes_, workspace = _scratch(workspace, need, X, device)
+    with here:
+        _check(lib().cogdl_linear_distill_backward(n, V, k, K, pd, px, pw, dt, pb, pi, pt, temperature, ps, pp, dx, dw,
+                                                   db, ws, bytes_, _stream_of(device)), "cogdl_linear_distill_backward")
     return o

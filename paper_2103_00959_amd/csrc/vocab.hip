@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
         }
         if constexpr (FORWARD) {
             const T *__restrict__ x = static_cast<const T *>(a.X) + i * a.k;
-            const int sub = lane & 15, vecs = a.kp / 8;
+            const int sub = lane & 15, vecs = (a.k + 7) / 8;
             for (int e0 = 0; e0 < a.entries; e0 += kWave / 16) {
                 const int e = e0 + (lane >> 4);
                 const int32_t v = e < a.entries ? index[e] : -1;
@@ -86,6 +86,8 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
 // The rows that count, in order, and their features; in the forward of the cross entropy also their targets'
 // logits, into loss.  A workgroup takes `per` rows; how many count before them
 // it finds by itself, from the targets (n targets a workgroup, from the L2s).
+constexpr int kRowsDeep = 4;     // rows a wavefront moves at once
+
 template <typename T, bool BACKWARD>
 __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
 {
@@ -97,8 +99,13 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
     const int32_t limit = a.distill ? INT32_MAX : a.V;
     const int64_t from = (int64_t)blockIdx.x * per, to = from + per < a.n ? from + per : a.n;
     int before = 0;
-#pragma unroll 4
-    for (int64_t i = threadIdx.x; i < from; i += kBlock) before += counts(live[i], limit) ? 1 : 0;
+    for (int64_t i0 = threadIdx.x; i0 < from; i0 += kBlock * 16) {
+        int32_t t[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) t[u] = i0 + u * kBlock < from ? live[i0 + u * kBlock] : -1;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) before += counts(t[u], limit) ? 1 : 0;
+    }
     before = wave_inclusive_scan(before);
     if (lane == kWave - 1) wsum[wave] = before;
     __syncthreads();
@@ -109,9 +116,16 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         // the largest |g T| that counts, for a power of two that brings every dz below 2^15 (and keeps what
         // fp16 can of the small ones)
         float top = 0.f;
-#pragma unroll 4
-        for (int64_t i = threadIdx.x; i < a.n; i += kBlock)
-            if (counts(live[i], limit)) top = fmaxf(top, fabsf(a.dloss[i] * a.T));
+        for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kBlock * 8) {
+            float g[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int64_t i = i0 + u * kBlock;
+                g[u] = i < a.n && counts(live[i], limit) ? a.dloss[i] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) top = fmaxf(top, fabsf(g[u] * a.T));
+        }
         top = group_reduce(top, kWave, [](float x, float y) { return fmaxf(x, y); });
         if (lane == 0) wmax[wave] = top;
         __syncthreads();
@@ -135,18 +149,24 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
     T *__restrict__ Xr = static_cast<T *>(a.Xr);
     T *__restrict__ dX = static_cast<T *>(a.dX);
     const int vecs = a.kp / 8;
+    const bool dots = !BACKWARD && !a.distill;
     // 64 rows at a time, every wavefront alike; a wavefront moves every fourth row
     for (int64_t r0 = from; r0 < to; r0 += kWave) {
         const int64_t i = r0 + lane;
-        const bool mine = i < to && counts(live[i], limit);
-        const uint64_t mask = __ballot(mine);
+        const int32_t t = i < to ? live[i] : -1;
+        const uint64_t mask = __ballot(counts(t, limit));
         if (wave == 0 && i < to) {
-            if (mine) {
+            if (counts(t, limit)) {
                 const int p = at + __popcll(mask & ((1ull << lane) - 1));
                 a.rows[p] = (int32_t)i;
                 if constexpr (BACKWARD) {
+                    const float g = a.dloss[i] * a.T;
                     a.lse2[p] = a.lse_in[i] * kLog2e;
-                    a.g[p] = a.dloss[i] * a.T;
+                    a.g[p] = g;
+                    if (!a.distill) {
+                        a.col[p] = t;
+                        a.at_col[p] = g * expm1f(-a.loss_in[i]);      // p - 1, exact where p is near 1 too
+                    }
                 }
             } else if constexpr (!BACKWARD) {
                 a.loss[i] = 0.f;
@@ -154,56 +174,80 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
             }
         }
         const int here = to - r0 < kWave ? (int)(to - r0) : kWave;
-#pragma unroll 2
-        for (int r = wave; r < here; r += W) {
-            const bool on = mask >> r & 1;
-            const int64_t i1 = r0 + r;
-            if (on) {
-                const int64_t p = at + __popcll(mask & ((1ull << r) - 1));
-                const T *__restrict__ x = X + i1 * a.k;
-                const int32_t v1 = !BACKWARD && !a.distill ? a.index[i1] : 0;
-                const T *__restrict__ w = static_cast<const T *>(a.W) + (int64_t)v1 * a.k;
-                float z = 0.f;
-                for (int v = lane; v < vecs; v += kWave) {
-                    const uint4 f = load_vec8(x, v, a.k);
-                    *reinterpret_cast<uint4 *>(Xr + p * a.kp + 8 * v) = f;
-                    if constexpr (!BACKWARD)
-                        if (!a.distill) z = dot8<T>(f, load_vec8(w, v, a.k), z);
+        for (int b = wave; b < here; b += W * kRowsDeep) {
+            int64_t row[kRowsDeep];
+            int p[kRowsDeep];
+            int32_t target[kRowsDeep];
+            float z[kRowsDeep];
+#pragma unroll
+            for (int u = 0; u < kRowsDeep; ++u) {
+                const int r = b + u * W < kWave ? b + u * W : 0;
+                const bool on = b + u * W < here && (mask >> r & 1);
+                row[u] = r0 + r;
+                p[u] = on ? at + __popcll(mask & ((1ull << r) - 1)) : -1;
+                target[u] = __builtin_amdgcn_readlane(t, r);
+                z[u] = 0.f;
+            }
+            for (int v = lane; v < vecs; v += kWave) {
+                uint4 f[kRowsDeep], w[kRowsDeep];
+#pragma unroll
+                for (int u = 0; u < kRowsDeep; ++u) {
+                    f[u] = w[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (p[u] < 0) continue;
+                    f[u] = load_vec8(X + row[u] * a.k, v, a.k);
+                    if (dots) w[u] = load_vec8(static_cast<const T *>(a.W) + (int64_t)target[u] * a.k, v, a.k);
                 }
-                if constexpr (!BACKWARD) {
-                    if (!a.distill) {
-                        z = group_sum(z, kWave);
-                        if (lane == 0) a.loss[i1] = a.bias ? z + a.bias[v1] : z;
-                    }
+#pragma unroll
+                for (int u = 0; u < kRowsDeep; ++u) {
+                    if (p[u] < 0) continue;
+                    *reinterpret_cast<uint4 *>(Xr + (int64_t)p[u] * a.kp + 8 * v) = f[u];
+                    if (dots) z[u] = dot8<T>(f[u], w[u], z[u]);
                 }
-            } else if constexpr (BACKWARD) {
-                if (dX) {
+            }
+#pragma unroll
+            for (int u = 0; u < kRowsDeep; ++u) {
+                if (p[u] >= 0 && dots) {
+                    z[u] = group_sum(z[u], kWave);
+                    if (lane == 0) a.loss[row[u]] = a.bias ? z[u] + a.bias[target[u]] : z[u];
+                }
+                if (BACKWARD && p[u] < 0 && b + u * W < here && dX) {
                     const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    for (int v = lane; v < vecs; v += kWave) store8(dX + i1 * a.k, 8 * v, a.k, zeros);
+                    for (int v = lane; v < vecs; v += kWave) store8(dX + row[u] * a.k, 8 * v, a.k, zeros);
                 }
             }
         }
         at += __popcll(mask);
     }
-    if (to == a.n && threadIdx.x == 0) {
-        a.head->off[0] = 0;
-        a.head->off[1] = at;
+    if (to == a.n && wave == 0) {
+        if (lane == 0) {
+            a.head->off[0] = 0;
+            a.head->off[1] = at;
+        }
+        if constexpr (BACKWARD) {
+            // the slices of dX's sums that end soonest for so many rows: a candidate a lane
+            static_assert(kMostSlices == kWave, "a candidate a lane");
+            const float cost = lane < a.plan.most ? a.plan.cost(at, lane + 1) : INFINITY;
+            const float best = group_reduce(cost, kWave, [](float x, float y) { return fminf(x, y); });
+            const int first = __builtin_ctzll(__ballot(cost == best));
+            if (lane == 0) a.head->slices = first + 1;
+        }
     }
 }
 
-// Tiles of logits.  GRAD: dz of the piece, else each row's (max, sum) over the wavefront's columns.
-template <typename T, int WAVES, int TM, int TN, int SRCB, bool GRAD>
-__global__ __launch_bounds__(WAVES * kWave) void k_vocab_logits(VocabArgs a)
+// Tiles of logits.  GRAD: dz of the piece, else each row's (max, sum) over the wavefront's columns.  EXTRA: with a
+// bias, or db's sums over the tile's rows.
+template <typename T, int WAVES, int TM, int TN, int SRCB, bool GRAD, bool EXTRA>
+__global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
 {
     constexpr int N = WAVES * kWave;
     constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
     constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
     extern __shared__ __align__(16) char lds[];
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int wr = wave / WAVES_C, wc = wave % WAVES_C;
     const int r0 = wr * (32 * WR), c0 = wc * (32 * WC);
     GridWalk walk;
-    walk.start(a.head->off[1], TM, a.tiles_c, 1);
+    walk.start(!GRAD && a.plain ? a.n : a.head->off[1], TM, a.tiles_c, 1, blockIdx.x);
     RowOperand<T, TM, N, kDirect> A;
     RowOperand<T, TN, N, SRCB> B;
     const auto open = [&](const Span &s) {
@@ -212,138 +256,182 @@ __global__ __launch_bounds__(WAVES * kWave) void k_vocab_logits(VocabArgs a)
         B.open(static_cast<const T *>(a.W) + ((int64_t)a.v0 + col) * a.k, nullptr, cols, a.k, 0);
         return a.kp;
     };
+    const float scale = GRAD ? a.head->scale : 1.f;
     char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
     run_tiles<T, decltype(A), decltype(B), WR, WC>(
         lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.width; },
         [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
-        [&](const Span &s, const Acc<WR, WC> &acc) {
+        [&](const Span &s, Acc<WR, WC> &acc) {
             const int col0 = s.tile * TN + c0;
-            if constexpr (!GRAD) {
-                // this lane's columns of a block: 8 (t / 4) + 4 (lane / 32) + t % 4, of row lane % 32
-                float add[WC][16];
-                const int first = col0 + 4 * (lane >> 5);
+            if (col0 >= a.width || r0 >= s.have) return;
+            const int lane = lane_of_outputs();
+            // the bias, and -inf behind the last column: no part of a sum, no gradient
+            if (EXTRA || col0 + 32 * WC > a.width) {
 #pragma unroll
                 for (int j = 0; j < WC; ++j)
 #pragma unroll
                     for (int t = 0; t < 16; ++t) {
-                        const int c = first + 32 * j + 8 * (t / 4) + t % 4;
-                        add[j][t] = c < a.width ? a.bias ? a.bias[a.v0 + c] : 0.f : -INFINITY;
+                        const int c = col0 + 32 * j + 8 * (t / 4) + 4 * (lane >> 5) + t % 4;
+                        const float add = c < a.width ? EXTRA && a.bias ? a.bias[a.v0 + c] : 0.f : -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < WR; ++i) acc.a[i][j][t] += add;
                     }
+            }
+            if constexpr (!GRAD) {
                 const int slot = s.tile * WAVES_C + wc;
-                if (slot >= a.slots) return;
 #pragma unroll
                 for (int i = 0; i < WR; ++i) {
                     float m = -INFINITY;
-                    float z[WC][16];
 #pragma unroll
                     for (int j = 0; j < WC; ++j)
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) {
-                            z[j][t] = acc.a[i][j][t] + add[j][t];
-                            m = fmaxf(m, z[j][t]);
-                        }
+                        for (int t = 0; t < 16; ++t) m = fmaxf(m, acc.a[i][j][t]);
                     m = fmaxf(m, bfly_partner<32>(m)) * a.per_z;
                     const float from = m == -INFINITY ? 0.f : m;
                     float sum = 0.f;
 #pragma unroll
                     for (int j = 0; j < WC; ++j)
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) sum += __builtin_amdgcn_exp2f(fmaf(z[j][t], a.per_z, -from));
+                        for (int t = 0; t < 16; ++t) sum += __builtin_amdgcn_exp2f(fmaf(acc.a[i][j][t], a.per_z, -from));
                     sum += bfly_partner<32>(sum);
                     const int r = r0 + 32 * i + (lane & 31);
                     if (lane < 32 && r < s.have) a.part[(int64_t)slot * a.n + s.lo + r] = make_float2(m, sum);
                 }
             } else {
-                const float scale = a.head->scale;
                 T *__restrict__ dz = static_cast<T *>(a.dz) + s.lo * a.pitch;
-                float add[WC][8], sums[WC][8];
-#pragma unroll
-                for (int j = 0; j < WC; ++j)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int c = col0 + 32 * j + 8 * (lane & 3) + e;
-                        add[j][e] = c < a.width ? a.bias ? a.bias[a.v0 + c] : 0.f : -INFINITY;
-                        sums[j][e] = 0.f;
-                    }
-                for_outputs<WR, WC>(mine, acc, [&](int bc, int r, int c, float (&v)[8]) {
-                    r += r0;
-                    c += col0;
-                    if (r >= s.have || c >= a.pitch) return;
-                    const float less = a.lse2[s.lo + r], g = a.g[s.lo + r] * scale;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] = __builtin_amdgcn_exp2f(fmaf(v[e] + add[bc][e], a.per_z, -less)) * g;
-                        sums[bc][e] += v[e];
-                    }
-                    store_vec<T, 8>(dz + (int64_t)r * a.pitch, c, v);
-                });
-                if (a.db_part) {
-                    // over the 16 lanes that share 8 columns, in a fixed order
-                    float *__restrict__ to = a.db_part + ((int64_t)s.g * WAVES_R + wr) * a.V + a.v0;
-#pragma unroll
-                    for (int j = 0; j < WC; ++j)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float t = sums[j][e];
-                            t += __shfl_xor(t, 4);
-                            t += __shfl_xor(t, 8);
-                            t += __shfl_xor(t, 16);
-                            t += __shfl_xor(t, 32);
-                            const int c = col0 + 32 * j + 8 * (lane & 3) + e;
-                            if (lane < 4 && c < a.width) to[c] = t;
+                float sums[EXTRA ? 16 * WC : 1] = {};
+                float less = 0.f, g = 0.f;
+                int32_t col = -1;
+                int64_t p = 0;
+                for_rows16<T, WR, WC>(
+                    mine, acc,
+                    [&](int i, int j, int q, float (&v)[4]) {
+                        const int r = r0 + 32 * i + (lane & 31), c = col0 + 32 * j + 8 * q + 4 * (lane >> 5);
+                        if (j == 0 && q == 0) {          // (a row block's first)
+                            p = s.lo + (r < s.have ? r : 0);
+                            less = a.lse2[p];
+                            g = r < s.have ? a.g[p] * scale : 0.f;
+                            col = a.distill ? -1 : a.col[p] - a.v0;
                         }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(v[e], a.per_z, -less)) * g;
+                        if ((uint32_t)(col - c) < 4u) {  // (seldom)
+                            const float there = r < s.have ? a.at_col[p] * scale : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = col == c + e ? there : v[e];
+                        }
+                        if constexpr (EXTRA) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sums[16 * j + 4 * q + e] += r < s.have ? v[e] : 0.f;
+                        }
+                    },
+                    [&](int r, int c, uint4 w) {
+                        r += r0;
+                        c += col0;
+                        if (r < s.have && c < a.pitch) *reinterpret_cast<uint4 *>(dz + (int64_t)r * a.pitch + c) = w;
+                    });
+                if constexpr (EXTRA) {
+                    if (!a.db_part) return;
+                    // over the 32 rows' lanes, in a fixed order: two lanes share what either has left, and keep a half
+                    // each, down to one column a lane
+#pragma unroll
+                    for (int half = 16; half > 0; half /= 2) {
+                        const bool upper = lane & half;
+#pragma unroll
+                        for (int t = 0; t < half; ++t) {
+                            const float keep = upper ? sums[t + half] : sums[t], give = upper ? sums[t] : sums[t + half];
+                            sums[t] = keep + __shfl_xor(give, half);
+                        }
+                    }
+                    const int t = lane & 31, c = col0 + 32 * (t / 16) + 8 * (t / 4 % 4) + 4 * (lane >> 5) + t % 4;
+                    if (c < a.width) a.db_part[((int64_t)s.g * WAVES_R + wr) * a.V + a.v0 + c] = sums[0];
                 }
             }
         });
 }
 
-// The slots of a row joined to its lse, and the loss from its targets' logits.  kRowsBlock rows a workgroup.
-constexpr int kRowsBlock = 16;
-
-__global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a)
+// The slots of a row joined to its lse, and the loss from its targets' logits.  R rows a workgroup (a power of
+// two up to 16), 256 / R threads each.  Rows as they were given (R = 1): which count, and their target's logit, are
+// found here.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
 {
-    constexpr int W = kBlock / kWave, S = kBlock / kRowsBlock;
-    __shared__ float2 part[S][kRowsBlock];
-    __shared__ float lse_of[kRowsBlock];
+    constexpr int W = kBlock / kWave;
+    __shared__ float2 part[kBlock];
+    __shared__ float lse_of[16], dots[W];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int64_t live = a.head->off[1];
-    const int r = threadIdx.x % kRowsBlock, sg = threadIdx.x / kRowsBlock;
-    for (int64_t r0 = (int64_t)blockIdx.x * kRowsBlock; r0 < live; r0 += (int64_t)gridDim.x * kRowsBlock) {
-        float m = -INFINITY, z = 0.f;
-        if (r0 + r < live) {
-#pragma unroll 4
-            for (int s = sg; s < a.slots; s += S) {
-                const float2 p = a.part[(int64_t)s * a.n + r0 + r];
-                const float top = fmaxf(m, p.x);
-                const float from = top == -INFINITY ? 0.f : top;
-                z = z * __builtin_amdgcn_exp2f(m - from) + p.y * __builtin_amdgcn_exp2f(p.x - from);
-                m = top;
+    const int64_t live = a.plain ? a.n : a.head->off[1];
+    const int r = threadIdx.x & (R - 1), sg = threadIdx.x / R, S = kBlock / R;
+    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < live; r0 += (int64_t)gridDim.x * R) {
+        if (a.plain) {
+            const int32_t t = a.distill ? a.live[r0] : a.index[r0];
+            if (!counts(t, a.distill ? INT32_MAX : a.V)) {           // (uniform)
+                if (threadIdx.x == 0) a.loss[r0] = a.lse[r0] = 0.f;
+                continue;
+            }
+            if (!a.distill) {
+                float dot = 0.f;
+                for (int v = threadIdx.x; v < (a.k + 7) / 8; v += kBlock)
+                    dot = dot8<T>(load_vec8(static_cast<const T *>(a.X) + r0 * a.k, v, a.k),
+                                  load_vec8(static_cast<const T *>(a.W) + (int64_t)t * a.k, v, a.k), dot);
+                dot = group_sum(dot, kWave);
+                if (lane == 0) dots[wave] = dot;
             }
         }
-        part[sg][r] = make_float2(m, z);
-        __syncthreads();
-        if (threadIdx.x < kRowsBlock) {
-            float top = -INFINITY;
-            for (int s = 0; s < S; ++s) top = fmaxf(top, part[s][r].x);
+        float m = -INFINITY, z = 0.f;
+        // (the exponents are powers of two here)
+        const auto merge = [&](float2 p) {
+            const float top = fmaxf(m, p.x);
             const float from = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-            for (int s = 0; s < S; ++s) sum += part[s][r].y * __builtin_amdgcn_exp2f(part[s][r].x - from);
-            const float lse = (from + log2f(sum)) * kLn2;
+            z = z * __builtin_amdgcn_exp2f(m - from) + p.y * __builtin_amdgcn_exp2f(p.x - from);
+            m = top;
+        };
+        if (r0 + r < live) {
+            for (int s0 = sg; s0 < a.slots; s0 += 8 * S) {
+                float2 p[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int s = s0 + u * S;
+                    p[u] = s < a.slots ? a.part[(int64_t)s * a.n + r0 + r] : make_float2(-INFINITY, 0.f);
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) merge(p[u]);
+            }
+        }
+        part[threadIdx.x] = make_float2(m, z);
+        __syncthreads();
+        for (int half = S / 2; half > 0; half /= 2) {
+            if (sg < half) {
+                merge(part[threadIdx.x + half * R]);
+                part[threadIdx.x] = make_float2(m, z);
+            }
+            __syncthreads();
+        }
+        if ((int)threadIdx.x < R) {
+            const float lse = ((m == -INFINITY ? 0.f : m) + log2f(z)) * kLn2;
             lse_of[r] = lse;
             if (r0 + r < live) {
-                const int64_t i = a.rows[r0 + r];
+                const int64_t i = a.plain ? r0 : a.rows[r0 + r];
                 a.lse[i] = lse;
                 if (!a.distill) {
+                    float dot = 0.f;
+                    if (a.plain) {
+#pragma unroll
+                        for (int w = 0; w < W; ++w) dot += dots[w];
+                        if (a.bias) dot += a.bias[a.index[i]];
+                    } else {
+                        dot = a.loss[i];
+                    }
                     // (above 0 by definition; the two sums' roundings may differ)
-                    const float loss = lse - a.loss[i];
+                    const float loss = lse - dot;
                     a.loss[i] = loss < 0.f ? 0.f : loss;
                 }
             }
         }
-        __syncthreads();
+        __syncthreads();                                 // (lse_of; part and dots are read)
         if (!a.distill) continue;
-        for (int q = wave; q < kRowsBlock && r0 + q < live; q += W) {
-            const int64_t i = a.rows[r0 + q];
+        for (int q = wave; q < R && r0 + q < live; q += W) {
+            const int64_t i = a.plain ? r0 : a.rows[r0 + q];
             const float lse = lse_of[q], tlse = a.tlse[i];
             float loss = 0.f;
             for (int e = lane; e < a.entries; e += kWave) {
@@ -360,11 +448,18 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a)
     }
 }
 
-template <typename T, int WAVES, int TM, int TN>
-VocabKernel pick(bool direct, bool grad)
+template <typename T, bool GRAD, bool EXTRA>
+VocabKernel pick(bool wide, bool direct)
 {
-    if (grad) return direct ? k_vocab_logits<T, WAVES, TM, TN, kDirect, true> : k_vocab_logits<T, WAVES, TM, TN, kStaged, true>;
-    return direct ? k_vocab_logits<T, WAVES, TM, TN, kDirect, false> : k_vocab_logits<T, WAVES, TM, TN, kStaged, false>;
+    if (wide) return k_vocab_logits<T, 8, 256, 256, kDirect, GRAD, EXTRA>;
+    return direct ? k_vocab_logits<T, 4, 128, 128, kDirect, GRAD, EXTRA> : k_vocab_logits<T, 4, 128, 128, kStaged, GRAD, EXTRA>;
+}
+
+template <typename T>
+VocabKernel pick(bool grad, bool extra, bool wide, bool direct)
+{
+    if (grad) return extra ? pick<T, true, true>(wide, direct) : pick<T, true, false>(wide, direct);
+    return extra ? pick<T, false, true>(wide, direct) : pick<T, false, false>(wide, direct);
 }
 
 }  // namespace
@@ -383,6 +478,7 @@ cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backw
         else if (dtype == COGDL_BF16) COGDL_LAUNCH("teacher_rows", (k_teacher_rows<bf16_t, true>), grid, kBlock, stream, a);
         else COGDL_LAUNCH("teacher_rows", (k_teacher_rows<f16_t, true>), grid, kBlock, stream, a);
     }
+    if (a.plain) return COGDL_OK;
     int64_t per = (a.n + 511) / 512;
     per = per < 8 ? 8 : per;
     const unsigned blocks = a.n > 0 ? (unsigned)((a.n + per - 1) / per) : 1;
@@ -400,9 +496,8 @@ cogdl_status vocab_logits_launch(VocabArgs a, cogdl_dtype dtype, bool grad, bool
 {
     const bool direct = on_grid(a.W, a.k);
     const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
-    VocabKernel kern;
-    if (dtype == COGDL_BF16) kern = wide ? pick<bf16_t, 8, 256, 256>(true, grad) : pick<bf16_t, 4, 128, 128>(direct, grad);
-    else kern = wide ? pick<f16_t, 8, 256, 256>(true, grad) : pick<f16_t, 4, 128, 128>(direct, grad);
+    const bool extra = a.bias || (grad && a.db_part);
+    const VocabKernel kern = dtype == COGDL_BF16 ? pick<bf16_t>(grad, extra, wide, direct) : pick<f16_t>(grad, extra, wide, direct);
     a.tiles_c = (int32_t)(((int64_t)a.width + tile - 1) / tile);
     const int64_t all = (a.n + tile - 1) / tile * a.tiles_c;
     return launch_vocab(grad ? "vocab_dz" : "vocab_stats", kern, a, all, waves, lds_of(waves, tile, tile), stream);
@@ -461,13 +556,22 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < need) return COGDL_ERR_INVALID;
     a.v0 = 0;
     a.width = a.V;
+    // One row tile costs the same however many of its rows count, and rows do not meet in the forward: no need to
+    // gather them (one row, 50000 x 512: 22 us with the gathering launch, FIGURE without).
+    a.plain = a.n <= 128 && on_grid(a.X, a.k);
+    if (a.plain) {
+        a.Xr = const_cast<void *>(a.X);
+        a.kp = a.k;
+    }
     cogdl_status s = vocab_rows_launch(a, dtype, false, stream);
     if (s != COGDL_OK) return s;
     s = vocab_logits_launch(a, dtype, false, vocab_wide(a.n, a.V, a.k, a.W), stream);
     if (s != COGDL_OK) return s;
-    int64_t blocks = (a.n + kRowsBlock - 1) / kRowsBlock;
+    const int R = a.n <= 256 ? 1 : a.n <= 1024 ? 4 : 16;
+    int64_t blocks = (a.n + R - 1) / R;
     if (blocks > 4096) blocks = 4096;
-    COGDL_LAUNCH("vocab_finish", k_vocab_finish, (unsigned)blocks, kBlock, stream, a);
+    if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, R);
+    else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, R);
     return COGDL_OK;
 }
 

@@ -20,6 +20,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 // Most entries of a teacher's row.
 constexpr int kMaxEntries = COGDL_MAX_TEACHER;
+// Slices of dX's sums over a piece, at most.
+constexpr int kMostSlices = 64;
 // Rows of one call.
 constexpr int64_t kMaxRows = 1 << 24;
 
@@ -27,6 +29,35 @@ constexpr int64_t kMaxRows = 1 << 24;
 struct RowsHead {
     int32_t off[2];              // 0, live rows
     float scale, unscale;        // 2^e and 2^-e: |g T| 2^e < 2^15 for every live row
+    int32_t slices;              // of dX's sums over a piece
+};
+
+// The two products of a piece as tiles of tile x tile on `resident` workgroups of each XCD, one after another: dX's
+// sums (rows x k, a slice of the piece's `width` columns each), then dW (width x k, summed over the rows).  The time of
+// the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile costs its chunks and
+// kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  FIGURE.
+constexpr int kTileStart = 4, kTileSums = 2;
+
+struct ProductsPlan {
+    int32_t tile, resident, width, k, most;
+    bool dx, dw;
+
+    // (in floats: sizes are far apart, and no whole number has to come out)
+    __device__ __forceinline__ float cost(int32_t live, int32_t s) const
+    {
+        const float tr = (float)((live + tile - 1) / tile), tk = (float)((k + tile - 1) / tile), tw = (float)((width + tile - 1) / tile);
+        const float n1 = dx ? ceilf(tr * tk * s * 0.125f) : 0.f, n2 = dw ? ceilf(tw * tk * 0.125f) : 0.f, each = 1.f / resident;
+        const float c1 = ceilf((float)width / (64.f * s)) + kTileStart + kTileSums, c2 = (live + 63) / 64 + kTileStart;
+        // workgroup w of the XCD has the tiles w, w + resident, ... of n1 + n2: the most of it at the first, and at
+        // the first that begins with dW
+        float most_of = 0.f;
+        for (int h = 0; h < 2; ++h) {
+            const float w = h == 0 ? 0.f : n1 - floorf(n1 * each) * resident;
+            const float all = ceilf((n1 + n2 - w) * each), of_dx = n1 > w ? ceilf((n1 - w) * each) : 0.f;
+            most_of = fmaxf(most_of, of_dx * c1 + fmaxf(all - of_dx, 0.f) * c2);
+        }
+        return most_of + s * tr * tk * each * (1.f / 16);       // (what the sum over slices reads)
+    }
 };
 
 struct VocabArgs {
@@ -34,6 +65,7 @@ struct VocabArgs {
     int32_t V, k, kp;            // kp: k rounded up to 8, the pitch of the gathered rows
     int32_t entries;             // of a row: 1 (cross entropy), K (distillation)
     bool distill;
+    bool plain;                  // the rows as they were given stand for the gathered ones (few of them, forward)
     float T, per_z;              // per_z = log2(e) / T
     const void *X, *W;
     const float *bias;           // V, nullable
@@ -50,12 +82,14 @@ struct VocabArgs {
     float *tlse;                 // n: log sum_e exp(teacher / T) (distillation)
     int32_t *rows;               // live: the rows that count
     float *lse2, *g;             // live: lse log2(e), g T
+    int32_t *col;                // live: the target (cross entropy)
+    float *at_col;               // live: g (p - 1) there
     void *Xr;                    // live x kp: their features
     float2 *part;                // [slot][n]: (max, sum) of a row's logits in a slot of columns, in powers of two
     int32_t slots;
     void *dz;                    // live x (piece's columns, rounded up to 8): scaled by head->scale
     float *dx_part;              // [slice][live][kp]
-    int32_t slices;
+    ProductsPlan plan;           // (backward)
     float *db_part;              // [row tile][V]
     int32_t row_tiles;
     unsigned long long *db_q;    // V: the targets' part, in units of 2^-unit_bits
@@ -63,7 +97,8 @@ struct VocabArgs {
     // this launch
     int32_t v0, width;           // the vocabulary piece [v0, v0 + width)
     int32_t pitch;               // of dz
-    int32_t tiles_c;
+    int32_t tiles_c;             // column tiles of the logits, of dX's sums
+    int32_t tiles_w;             // column tiles of dW
     bool first;                  // the first piece
 };
 
@@ -80,15 +115,16 @@ struct GridWalk {
     int64_t rows;
     uint32_t j, step, end;
 
-    __device__ __forceinline__ void start(int64_t n, int rows_a_tile, int col_tiles, int slices)
+    // `block`: this workgroup's number among those of the grid.
+    __device__ __forceinline__ void start(int64_t n, int rows_a_tile, int col_tiles, int slices, uint32_t block)
     {
         rows = n;
         tm = rows_a_tile;
         R = (int)((n + tm - 1) / tm);
         C = col_tiles;
         const int64_t all = (int64_t)R * C * slices;
-        const uint32_t xcd = blockIdx.x & 7;
-        j = (uint32_t)(all * xcd / 8) + (blockIdx.x >> 3);
+        const uint32_t xcd = block & 7;
+        j = (uint32_t)(all * xcd / 8) + (block >> 3);
         end = (uint32_t)(all * (xcd + 1) / 8);
         step = gridDim.x >> 3;
     }
@@ -108,6 +144,48 @@ struct GridWalk {
         return true;
     }
 };
+
+// The lane's number as the outputs of a tile use it: what follows from it is computed anew for each tile, and takes
+// no registers from the products (hoisted out of the loop over tiles, it made 256 x 256 tiles spill).
+__device__ __forceinline__ int lane_of_outputs()
+{
+    int lane = lane_id();
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// A wavefront's 16-bit outputs, 64 columns of them: calls map(row block, column block, g, v) for its outputs four at a
+// time, of row lane % 32 and columns 8 g + 4 (lane / 32) ... + 3 of the block, rounds them, and calls out(row, column,
+// w) for 8 of a row as 16 bytes, through the wavefront's part of the LDS: eight neighbouring lanes then hold a row's 128
+// bytes, a whole cache line.  (dz of 8192 x 131072 logits, 1024 features: FIGURE)
+template <typename T, int WR, int WC, typename Map, typename Out>
+__device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, Map map, Out out)
+{
+    static_assert(WC == 2 && 32 * 64 * 2 == kOutBytes, "32 rows of 64 columns");
+    const int lane = lane_of_outputs(), r = lane & 31, hi = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < WR; ++i) {
+#pragma unroll
+        for (int j = 0; j < WC; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float v[4] = {acc.a[i][j][4 * g], acc.a[i][j][4 * g + 1], acc.a[i][j][4 * g + 2], acc.a[i][j][4 * g + 3]};
+                map(i, j, g, v);
+                // (the 16-byte pieces of a row permuted by the row)
+                *reinterpret_cast<uint2 *>(mine + r * 128 + (((4 * j + g) ^ (r & 7)) << 4) + 8 * hi) =
+                    make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = 8 * u + (lane >> 3), piece = lane & 7;
+            out(32 * i + row, 8 * piece, *reinterpret_cast<const uint4 *>(mine + row * 128 + ((piece ^ (row & 7)) << 4)));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
 
 // Launches a kernel of resident workgroups over at most `all` tiles.
 inline cogdl_status launch_vocab(const char *name, VocabKernel kern, const VocabArgs &a, int64_t all, int waves, size_t lds,

@@ -8,45 +8,36 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// The targets' part of dz, in fp32 from the loss itself: dz = g T (p - sum q), where p of a likely target is
-// near sum q and dz of it was rounded as g T p.  Several entries of a row on the same answer all write their
-// common value.  On the first piece also the targets' part of db, in whole numbers (any order gives the same
-// sum).  A wavefront a row, an entry a lane (cross entropy: a row a lane).
+// The entries' part of dz (distillation), in fp32 from their log-probabilities: dz = g T (p - sum q), where p may
+// be near sum q and dz of it was rounded as g T p.  Several entries of a row on the same answer all write their
+// common value.  On the first piece also the entries' part of db, in whole numbers (any order gives the same
+// sum).  A wavefront a row, an entry a lane.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_vocab_targets(VocabArgs a)
+__global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
 {
     const int64_t live = a.head->off[1];
     const float scale = a.head->scale;
     T *__restrict__ dz = static_cast<T *>(a.dz);
-    const int64_t me = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
-    const int64_t group = a.distill ? me / kWave : me, groups = a.distill ? all / kWave : all;
-    const int first = a.distill ? lane_id() : 0, step = a.distill ? kWave : 1;
-    for (int64_t p = group; p < live; p += groups) {
+    const int64_t waves = (int64_t)gridDim.x * (kBlock / kWave);
+    for (int64_t p = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave; p < live; p += waves) {
         const int64_t i = a.rows[p];
         const int32_t *__restrict__ index = a.index + i * a.entries;
-        const float g = a.g[p] * scale;
-        for (int e = first; e < a.entries; e += step) {
+        const float *__restrict__ teacher = a.teacher + i * a.entries;
+        const float g = a.g[p] * scale, tlse = a.tlse[i];
+        for (int e = lane_id(); e < a.entries; e += kWave) {
             const int32_t v = index[e];
             if ((uint32_t)v >= (uint32_t)a.V) continue;
-            const bool here = v >= a.v0 && v - a.v0 < a.width;
-            float d, mine = 1.f;
-            if (a.distill) {
-                const float *__restrict__ teacher = a.teacher + i * a.entries;
-                const float tlse = a.tlse[i];
-                mine = expf(teacher[e] / a.T - tlse);
-                float q = 0.f;
-                if (here)
-                    for (int o = 0; o < a.entries; ++o)
-                        if (index[o] == v) q += expf(teacher[o] / a.T - tlse);
-                d = expf(a.logp_in[i * a.entries + e]) - q;
-            } else {
-                d = expm1f(-a.loss_in[i]);
-            }
+            const bool here = v >= a.v0 && v - a.v0 < a.width, db = a.first && a.db_q;
+            if (!here && !db) continue;
+            const float mine = expf(teacher[e] / a.T - tlse);
             if (here) {
-                const float one[1] = {d * g};
+                float q = 0.f;
+                for (int o = 0; o < a.entries; ++o)
+                    if (index[o] == v) q += o == e ? mine : expf(teacher[o] / a.T - tlse);
+                const float one[1] = {(expf(a.logp_in[i * a.entries + e]) - q) * g};
                 store_out<T, 1>(dz + p * a.pitch, v - a.v0, one);
             }
-            if (a.first && a.db_q) {
+            if (db) {
                 const float w = ldexpf(mine * g, a.unit_bits);
                 // (a row whose gradient is not finite makes all of db NaN by its dz)
                 if (fabsf(w) < 9e18f) atomicAdd(&a.db_q[v], (unsigned long long)(long long)rintf(w));
@@ -55,58 +46,11 @@ __global__ __launch_bounds__(kBlock) void k_vocab_targets(VocabArgs a)
     }
 }
 
-// dX's sums over the piece: rows by k, a slice of the piece's columns each.
+// Both products of a piece, each workgroup's tiles of dX's sums (rows by k, a slice of the piece's columns each),
+// then its tiles of dW (vocabulary by k, over the live rows): workgroups that have no tile of the first begin with
+// the second.
 template <typename T, int WAVES, int TM, int TN, int SRCB>
-__global__ __launch_bounds__(WAVES * kWave) void k_vocab_dx(VocabArgs a)
-{
-    constexpr int N = WAVES * kWave;
-    constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
-    constexpr int WR = TM / WAVES_R / 32, WC = TN / WAVES_C / 32;
-    extern __shared__ __align__(16) char lds[];
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
-    const int64_t live = a.head->off[1];
-    const int per = ((a.pitch + a.slices - 1) / a.slices + kX - 1) / kX * kX;
-    GridWalk walk;
-    walk.start(live, TM, a.tiles_c, a.slices);
-    RowOperand<T, TM, N, kDirect> A;
-    ColOperand<T, TN, N, SRCB, false> B;
-    const auto open = [&](const Span &s) {
-        int x0 = s.slot * per;
-        if (x0 > a.pitch) x0 = a.pitch;
-        const int wide = a.pitch - x0 < per ? a.pitch - x0 : per, real = a.width - x0 < 0 ? 0 : a.width - x0 < wide ? a.width - x0 : wide;
-        A.open(static_cast<const T *>(a.dz) + s.lo * a.pitch + x0, nullptr, s.have, a.pitch, 0);
-        A.width = wide;
-        B.open(static_cast<const T *>(a.W) + ((int64_t)a.v0 + x0) * a.k, nullptr, nullptr, nullptr, s.tile * TN, a.k, real, 0, false);
-        return wide;
-    };
-    char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
-    run_tiles<T, decltype(A), decltype(B), WR, WC>(
-        lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; },
-        [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
-        [&](const Span &s, const Acc<WR, WC> &acc) {
-            const int col0 = s.tile * TN + c0;
-            float *__restrict__ part = a.dx_part + (s.slot * a.n + s.lo) * a.kp;
-            for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
-                r += r0;
-                c += col0;
-                if (r >= s.have || c >= a.kp) return;
-                float *__restrict__ to = part + (int64_t)r * a.kp + c;
-                if (!a.first) {
-                    float w[2][4];
-                    load_vec<float, 4>(to, 0, w[0]);
-                    load_vec<float, 4>(to, 4, w[1]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += w[e / 4][e % 4];
-                }
-                store_vec<float, 8>(to, 0, v);
-            });
-        });
-}
-
-// The piece's rows of dW: vocabulary by k, summed over the live rows.
-template <typename T, int WAVES, int TM, int TN>
-__global__ __launch_bounds__(WAVES * kWave) void k_vocab_dw(VocabArgs a)
+__global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a)
 {
     constexpr int N = WAVES * kWave;
     constexpr int WAVES_C = TN >= 256 ? 4 : 2, WAVES_R = WAVES / WAVES_C;
@@ -115,47 +59,115 @@ __global__ __launch_bounds__(WAVES * kWave) void k_vocab_dw(VocabArgs a)
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
     const int live = a.head->off[1];
-    const float unscale = a.head->unscale;
-    GridWalk walk;
-    walk.start(a.width, TM, a.tiles_c, 1);
-    ColOperand<T, TM, N, kDirect, false> A;
-    ColOperand<T, TN, N, kDirect, false> B;
-    const auto open = [&](const Span &s) {
-        A.open(static_cast<const T *>(a.dz), nullptr, nullptr, nullptr, (int)s.lo, a.pitch, live, 0, false);
-        B.open(static_cast<const T *>(a.Xr), nullptr, nullptr, nullptr, s.tile * TN, a.kp, live, 0, false);
-        return live;
-    };
     char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
-    run_tiles<T, decltype(A), decltype(B), WR, WC>(
-        lds, walk, A, B, r0, c0, open, [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; },
-        [](const Span &, const uint4 (&)[WR]) {}, [](const Span &) {},
-        [&](const Span &s, const Acc<WR, WC> &acc) {
-            const int col0 = s.tile * TN + c0;
-            T *__restrict__ dW = static_cast<T *>(a.dW) + (a.v0 + s.lo) * a.k;
-            for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
-                r += r0;
-                c += col0;
-                if (r >= s.have || c >= a.k) return;
+    const auto busy = [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; };
+    const auto nothing = [](const Span &) {};
+    uint32_t block = blockIdx.x;
+    GridWalk walk;
+    if (a.dX) {
+        const int slices = a.head->slices;
+        const int per = ((a.pitch + slices - 1) / slices + kX - 1) / kX * kX;
+        walk.start(live, TM, a.tiles_c, slices, block);
+        block = (uint32_t)((block + gridDim.x - (((uint32_t)(walk.R * walk.C) * (uint32_t)slices + 7) / 8 * 8) % gridDim.x) % gridDim.x);
+        RowOperand<T, TM, N, kDirect> A;
+        ColOperand<T, TN, N, SRCB, false> B;
+        const auto open = [&](const Span &s) {
+            const int x0 = s.slot * per < a.pitch ? s.slot * per : a.pitch;
+            const int wide = a.pitch - x0 < per ? a.pitch - x0 : per;
+            const int real = a.width - x0 < wide ? a.width - x0 : wide;
+            A.open(static_cast<const T *>(a.dz) + s.lo * a.pitch + x0, nullptr, s.have, a.pitch, 0);
+            A.width = wide;
+            B.open(static_cast<const T *>(a.W) + ((int64_t)a.v0 + x0) * a.k, nullptr, nullptr, nullptr, s.tile * TN, a.k,
+                   real > 0 ? real : 0, 0, false);
+            return wide;
+        };
+        run_tiles<T, decltype(A), decltype(B), WR, WC>(
+            lds, walk, A, B, r0, c0, open, busy, [](const Span &, const uint4 (&)[WR]) {}, nothing,
+            [&](const Span &s, const Acc<WR, WC> &acc) {
+                const int col0 = s.tile * TN + c0;
+                float *__restrict__ part = a.dx_part + (s.slot * a.n + s.lo) * a.kp;
+                for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
+                    r += r0;
+                    c += col0;
+                    if (r >= s.have || c >= a.kp) return;
+                    float *__restrict__ to = part + (int64_t)r * a.kp + c;
+                    if (!a.first) {
+                        float w[2][4];
+                        load_vec<float, 4>(to, 0, w[0]);
+                        load_vec<float, 4>(to, 4, w[1]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= unscale;
-                store8(dW + (int64_t)r * a.k, c, a.k, v);
+                        for (int e = 0; e < 8; ++e) v[e] += w[e / 4][e % 4];
+                    }
+                    store_vec<float, 8>(to, 0, v);
+                });
             });
-        });
+        __syncthreads();                                 // (the LDS is the next product's)
+    }
+    if (a.dW) {
+        const float unscale = a.head->unscale;
+        walk.start(a.width, TM, a.tiles_w, 1, block);
+        ColOperand<T, TM, N, kDirect, false> A;
+        ColOperand<T, TN, N, kDirect, false> B;
+        const auto open = [&](const Span &s) {
+            A.open(static_cast<const T *>(a.dz), nullptr, nullptr, nullptr, (int)s.lo, a.pitch, live, 0, false);
+            B.open(static_cast<const T *>(a.Xr), nullptr, nullptr, nullptr, s.tile * TN, a.kp, live, 0, false);
+            return live;
+        };
+        run_tiles<T, decltype(A), decltype(B), WR, WC>(
+            lds, walk, A, B, r0, c0, open, busy, [](const Span &, const uint4 (&)[WR]) {}, nothing,
+            [&](const Span &s, const Acc<WR, WC> &acc) {
+                const int col0 = s.tile * TN + c0;
+                T *__restrict__ dW = static_cast<T *>(a.dW) + (a.v0 + s.lo) * a.k;
+                for_rows16<T, WR, WC>(
+                    mine, acc,
+                    [&](int, int, int, float (&v)[4]) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] *= unscale;
+                    },
+                    [&](int r, int c, uint4 w) {
+                        r += r0;
+                        c += col0;
+                        if (r >= s.have || c >= a.k) return;
+                        T *__restrict__ to = dW + (int64_t)r * a.k + c;
+                        if (c + 8 <= a.k) {
+                            *reinterpret_cast<u32x4_u *>(to) = u32x4_u{w.x, w.y, w.z, w.w};
+                        } else {
+                            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (c + e < a.k) to[e].bits = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+                        }
+                    });
+            });
+    }
 }
 
-// dX of the live rows from their slices' sums.
+// dX of the live rows from their slices' sums (workgroups below `dx_blocks`), db from the row tiles' sums and the
+// entries' part.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_vocab_dx_out(VocabArgs a)
+__global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int rows_a_part)
 {
     const int64_t live = a.head->off[1];
     const float unscale = a.head->unscale;
-    const int vecs = a.kp / 8;
+    if ((int)blockIdx.x >= dx_blocks) {
+        const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
+        const int64_t v = (int64_t)(blockIdx.x - dx_blocks) * kBlock + threadIdx.x;
+        if (v >= a.V) return;
+        float t = 0.f;
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.V + v];
+        if (a.db_q) t = (float)((double)t - ldexp((double)(long long)a.db_q[v], -a.unit_bits));
+        a.db[v] = t * unscale;
+        return;
+    }
+    const int vecs = a.kp / 8, slices = a.head->slices;
     const int64_t all = live * vecs;
-    for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < all; u += (int64_t)gridDim.x * kBlock) {
+    for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < all; u += (int64_t)dx_blocks * kBlock) {
         const int64_t p = u / vecs;
         const int c = (int)(u % vecs) * 8;
         float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < a.slices; ++s) {
+#pragma unroll 4
+        for (int s = 0; s < slices; ++s) {
             float w[2][4];
             const float *__restrict__ from = a.dx_part + (s * a.n + p) * a.kp + c;
             load_vec<float, 4>(from, 0, w[0]);
@@ -169,74 +181,44 @@ __global__ __launch_bounds__(kBlock) void k_vocab_dx_out(VocabArgs a)
     }
 }
 
-// db from the row tiles' sums and the targets' part.
-__global__ __launch_bounds__(kBlock) void k_vocab_db(VocabArgs a, int rows_a_part)
-{
-    const int64_t live = a.head->off[1];
-    const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
-    const int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (v >= a.V) return;
-    float t = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.V + v];
-    const double q = ldexp((double)(long long)a.db_q[v], -a.unit_bits);
-    a.db[v] = (float)((double)t - q) * a.head->unscale;
-}
-
 template <typename T>
-VocabKernel pick_dx(bool wide, bool direct)
+VocabKernel pick_products(bool wide, bool direct)
 {
-    if (wide) return k_vocab_dx<T, 8, 256, 256, kDirect>;
-    return direct ? k_vocab_dx<T, 4, 128, 128, kDirect> : k_vocab_dx<T, 4, 128, 128, kStaged>;
-}
-
-template <typename T>
-VocabKernel pick_dw(bool wide)
-{
-    if (wide) return k_vocab_dw<T, 8, 256, 256>;
-    return k_vocab_dw<T, 4, 128, 128>;
+    if (wide) return k_vocab_products<T, 8, 256, 256, kDirect>;
+    return direct ? k_vocab_products<T, 4, 128, 128, kDirect> : k_vocab_products<T, 4, 128, 128, kStaged>;
 }
 
 int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1) / tile * ((cols + tile - 1) / tile); }
 
-// Partial sums of dX, at most.
-constexpr int64_t kMostSlices = 64;
+// The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).  The Infinity Cache's
+// size: 8192 rows, vocabulary 131072, 1024 features, FIGURE.
+constexpr int64_t kPieceBytes = 512ll << 20;
 
-// The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).
-constexpr int64_t kPieceBytes = 256ll << 20;
+// Whether the products over a piece take tiles of 256 x 256 (where W is on the grid): enough of them for most of
+// the chip.
+bool wide_products(int64_t n, int64_t width, int32_t k)
+{
+    return k > 128 && k % 2 == 0 && tiles_of(n, k, 256) * (width / 512) + tiles_of(width, k, 256) >= 256;
+}
 
-struct Pieces {
-    int32_t width;               // of a piece, the last may be smaller
-    int32_t slices;              // of a piece, in dX's sums
-};
-
-// Whether dX's sums over a piece of `width` take tiles of 256 x 256 (where W is on the grid).
-bool wide_dx(int64_t n, int64_t width, int32_t k) { return k > 128 && k % 2 == 0 && tiles_of(n, k, 256) * (width / 512) >= 256; }
-
-Pieces pieces_of(int64_t n, int32_t V, int32_t k)
+int32_t piece_width(int64_t n, int32_t V)
 {
     int64_t cols = kPieceBytes / (2 * (n > 0 ? n : 1)) / 256 * 256;
     if (cols < 256) cols = 256;
     if (cols > kMaxWidth) cols = kMaxWidth;
     const int64_t count = (V + cols - 1) / cols;
-    int64_t width = ((V + count - 1) / count + 255) / 256 * 256;
-    if (width > V) width = V;
-    Pieces p;
-    p.width = (int32_t)width;
-    const bool wide = wide_dx(n, width, k);
-    const int64_t tiles = tiles_of(n, k, wide ? 256 : 128), want = wide ? 256 : 512;
-    // the fewest rounds of resident workgroups for the work of a slice; a slice more has to gain a tenth
-    const int64_t most = width / (wide ? 512 : 256);
-    int64_t slices = 1, rounds = (tiles + want - 1) / want;
-    for (int64_t s = 2; s <= most && s <= kMostSlices; ++s) {
-        const int64_t r = (tiles * s + want - 1) / want;
-        if (10 * r * slices < 9 * rounds * s) {
-            slices = s;
-            rounds = r;
-        }
-    }
-    p.slices = (int32_t)(slices < 1 ? 1 : slices);
-    return p;
+    const int64_t width = ((V + count - 1) / count + 255) / 256 * 256;
+    return (int32_t)(width < V ? width : V);
+}
+
+// Slices of 256 columns or more, and no more than the workspace has room for: 4 bytes of sums for each 2 of dz.
+int32_t most_slices(int32_t width, int32_t kp)
+{
+    int64_t most = width / 256, room = (int64_t)width / (kp > 0 ? kp : 1);
+    if (room < 16) room = 16;
+    if (most > room) most = room;
+    if (most > kMostSlices) most = kMostSlices;
+    return (int32_t)(most < 1 ? 1 : most);
 }
 
 struct Layout {
@@ -251,10 +233,10 @@ struct Layout {
 
 size_t lay_backward(VocabArgs &a, char *ws)
 {
-    const Pieces p = pieces_of(a.n, a.V, a.k);
-    a.width = p.width;
-    a.pitch = (p.width + 7) / 8 * 8;
-    a.slices = p.slices;
+    a.width = piece_width(a.n, a.V);
+    a.pitch = (a.width + 7) / 8 * 8;
+    a.plan.most = most_slices(a.width, a.kp);
+    while (a.plan.most > 1 && !countable(tiles_of(a.n, a.k, 128), a.plan.most)) a.plan.most /= 2;
     a.row_tiles = (int32_t)((a.n + 127) / 128 * 2);
     const size_t n = (size_t)a.n;
     Layout l;
@@ -264,11 +246,13 @@ size_t lay_backward(VocabArgs &a, char *ws)
     a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * n));
     a.lse2 = reinterpret_cast<float *>(ws + l.take(4 * n));
     a.g = reinterpret_cast<float *>(ws + l.take(4 * n));
+    a.col = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 0 : 4 * n));
+    a.at_col = reinterpret_cast<float *>(ws + l.take(a.distill ? 0 : 4 * n));
     a.Xr = ws + l.take(2 * n * a.kp);
     a.dz = ws + l.take(2 * n * a.pitch);
-    a.dx_part = reinterpret_cast<float *>(ws + l.take(4 * n * a.kp * a.slices));
+    a.dx_part = reinterpret_cast<float *>(ws + l.take(4 * n * a.kp * a.plan.most));
     a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.V));
-    a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(8 * (size_t)a.V));
+    a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(a.distill ? 8 * (size_t)a.V : 0));
     return l.total;
 }
 
@@ -302,15 +286,21 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
     const size_t need = lay_backward(a, static_cast<char *>(workspace));
     if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < need) return COGDL_ERR_INVALID;
     const int piece = a.width;
-    if (!a.db) {
-        a.db_part = nullptr;
-        a.db_q = nullptr;
-    }
+    if (!a.db) a.db_part = nullptr;
+    if (!a.db || !a.distill) a.db_q = nullptr;
     // n terms below 2^15, in 62 bits
     a.unit_bits = 46 - bits_for((uint64_t)a.n);
     const bool bf16 = dtype == COGDL_BF16;
-    COGDL_TRY(vocab_rows_launch(a, dtype, true, stream));
     const bool wide_logits = vocab_wide(a.n, piece, a.k, a.W);
+    const bool wide = on_grid(a.W, a.k) && wide_products(a.n, piece, a.k);
+    const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
+    a.plan.tile = tile;
+    a.plan.resident = wide ? 32 : 64;
+    a.plan.width = piece;
+    a.plan.k = a.k;
+    a.plan.dx = a.dX != nullptr;
+    a.plan.dw = a.dW != nullptr;
+    COGDL_TRY(vocab_rows_launch(a, dtype, true, stream));
     for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
         a.v0 = (int32_t)v0;
         a.width = (int32_t)(a.V - v0 < piece ? a.V - v0 : piece);
@@ -318,33 +308,25 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
         a.first = v0 == 0;
         if (a.n > 0) {
             COGDL_TRY(vocab_logits_launch(a, dtype, true, wide_logits, stream));
-            int64_t blocks = ((a.distill ? a.n * kWave : a.n) + kBlock - 1) / kBlock;
-            if (blocks > 2048) blocks = 2048;
-            if (bf16) COGDL_LAUNCH("vocab_targets", k_vocab_targets<bf16_t>, (unsigned)blocks, kBlock, stream, a);
-            else COGDL_LAUNCH("vocab_targets", k_vocab_targets<f16_t>, (unsigned)blocks, kBlock, stream, a);
+            if (a.distill) {
+                const int64_t blocks = (a.n * kWave + kBlock - 1) / kBlock;
+                const unsigned grid = (unsigned)(blocks < 2048 ? blocks : 2048);
+                if (bf16) COGDL_LAUNCH("vocab_entries", k_vocab_entries<bf16_t>, grid, kBlock, stream, a);
+                else COGDL_LAUNCH("vocab_entries", k_vocab_entries<f16_t>, grid, kBlock, stream, a);
+            }
         }
-        if (a.dX) {
-            const bool wide = on_grid(a.W, a.k) && wide_dx(a.n, piece, a.k);
-            const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
-            a.tiles_c = (a.k + tile - 1) / tile;
-            COGDL_TRY(launch_vocab("vocab_dx", bf16 ? pick_dx<bf16_t>(wide, on_grid(a.W, a.k)) : pick_dx<f16_t>(wide, on_grid(a.W, a.k)),
-                                   a, tiles_of(a.n, a.k, tile) * a.slices, waves, lds_of(waves, tile, tile), stream));
-        }
-        if (a.dW) {
-            const bool wide = a.k > 128 && tiles_of(a.width, a.k, 256) >= 128;
-            const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
-            a.tiles_c = (a.k + tile - 1) / tile;
-            COGDL_TRY(launch_vocab("vocab_dw", bf16 ? pick_dw<bf16_t>(wide) : pick_dw<f16_t>(wide), a, tiles_of(a.width, a.k, tile),
-                                   waves, lds_of(waves, tile, tile), stream));
-        }
+        if (!a.dX && !a.dW) continue;
+        a.tiles_c = a.tiles_w = (a.k + tile - 1) / tile;
+        const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) : 0);
+        COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
+                               a, tiles, waves, lds_of(waves, tile, tile), stream));
     }
-    if (a.dX) {
-        int64_t blocks = (a.n * (a.kp / 8) + kBlock - 1) / kBlock;
-        if (blocks > 4096) blocks = 4096;
-        if (bf16) COGDL_LAUNCH("vocab_dx_out", k_vocab_dx_out<bf16_t>, (unsigned)blocks, kBlock, stream, a);
-        else COGDL_LAUNCH("vocab_dx_out", k_vocab_dx_out<f16_t>, (unsigned)blocks, kBlock, stream, a);
-    }
-    if (a.db) COGDL_LAUNCH("vocab_db", k_vocab_db, (unsigned)((a.V + kBlock - 1) / kBlock), kBlock, stream, a, wide_logits ? 128 : 64);
+    if (!a.dX && !a.db) return COGDL_OK;
+    int64_t dx_blocks = a.dX ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
+    if (dx_blocks > 4096) dx_blocks = 4096;
+    const unsigned grid = (unsigned)(dx_blocks + (a.db ? ((int64_t)a.V + kBlock - 1) / kBlock : 0));
+    if (bf16) COGDL_LAUNCH("vocab_out", k_vocab_out<bf16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
+    else COGDL_LAUNCH("vocab_out", k_vocab_out<f16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
     return COGDL_OK;
 }
 
