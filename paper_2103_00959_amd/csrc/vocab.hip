@@ -247,12 +247,17 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
     const int wr = wave / WAVES_C, wc = wave % WAVES_C;
     const int r0 = wr * (32 * WR), c0 = wc * (32 * WC);
     GridWalk walk;
-    walk.start(!GRAD && a.plain ? a.n : a.head->off[1], TM, a.tiles_c, 1, blockIdx.x);
+    int64_t rows = !GRAD && a.plain ? a.n : a.head->off[1];
+    if constexpr (!GRAD) {
+        rows -= a.p0;
+        rows = rows < 0 ? 0 : rows < a.block ? rows : a.block;
+    }
+    walk.start(rows, TM, a.tiles_c, 1, blockIdx.x);
     RowOperand<T, TM, N, kDirect> A;
     RowOperand<T, TN, N, SRCB> B;
     const auto open = [&](const Span &s) {
         const int col = s.tile * TN, cols = a.width - col < TN ? a.width - col : TN;
-        A.open(static_cast<const T *>(a.Xr) + s.lo * a.kp, nullptr, s.have, a.kp, 0);
+        A.open(static_cast<const T *>(a.Xr) + ((GRAD ? 0 : a.p0) + s.lo) * a.kp, nullptr, s.have, a.kp, 0);
         B.open(static_cast<const T *>(a.W) + ((int64_t)a.v0 + col) * a.k, nullptr, cols, a.k, 0);
         return a.kp;
     };
@@ -295,7 +300,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
                         for (int t = 0; t < 16; ++t) sum += __builtin_amdgcn_exp2f(fmaf(acc.a[i][j][t], a.per_z, -from));
                     sum += bfly_partner<32>(sum);
                     const int r = r0 + 32 * i + (lane & 31);
-                    if (lane < 32 && r < s.have) a.part[(int64_t)slot * a.n + s.lo + r] = make_float2(m, sum);
+                    if (lane < 32 && r < s.have) a.part[(int64_t)slot * a.block + s.lo + r] = make_float2(m, sum);
                 }
             } else {
                 T *__restrict__ dz = static_cast<T *>(a.dz) + s.lo * a.pitch;
@@ -328,7 +333,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
                     [&](int r, int c, uint4 w) {
                         r += r0;
                         c += col0;
-                        if (r < s.have && c < a.pitch) *reinterpret_cast<uint4 *>(dz + (int64_t)r * a.pitch + c) = w;
+                        // (past the caches: it is read when the whole piece is there; of 8192 x 131072, 1024 features, the
+                        // products took 3885 us, so 3790)
+                        if (r < s.have && c < a.pitch)
+                            __builtin_nontemporal_store(__builtin_bit_cast(u32x4_u, w), reinterpret_cast<u32x4_u *>(dz + (int64_t)r * a.pitch + c));
                     });
                 if constexpr (EXTRA) {
                     if (!a.db_part) return;
@@ -344,7 +352,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
                         }
                     }
                     const int t = lane & 31, c = col0 + 32 * (t / 16) + 8 * (t / 4 % 4) + 4 * (lane >> 5) + t % 4;
-                    if (c < a.width) a.db_part[((int64_t)s.g * WAVES_R + wr) * a.V + a.v0 + c] = sums[0];
+                    if (c < a.width) a.db_part[((int64_t)s.g * WAVES_R + wr) * a.pitch + c] = sums[0];
                 }
             }
         });
@@ -360,9 +368,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
     __shared__ float2 part[kBlock];
     __shared__ float lse_of[16], dots[W];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int64_t live = a.plain ? a.n : a.head->off[1];
+    int64_t live = a.plain ? a.n : a.head->off[1];
+    live = live < a.p0 + a.block ? live : a.p0 + a.block;
     const int r = threadIdx.x & (R - 1), sg = threadIdx.x / R, S = kBlock / R;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < live; r0 += (int64_t)gridDim.x * R) {
+    for (int64_t r0 = a.p0 + (int64_t)blockIdx.x * R; r0 < live; r0 += (int64_t)gridDim.x * R) {
         if (a.plain) {
             const int32_t t = a.distill ? a.live[r0] : a.index[r0];
             if (!counts(t, a.distill ? INT32_MAX : a.V)) {           // (uniform)
@@ -392,7 +401,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const int s = s0 + u * S;
-                    p[u] = s < a.slots ? a.part[(int64_t)s * a.n + r0 + r] : make_float2(-INFINITY, 0.f);
+                    p[u] = s < a.slots ? a.part[(int64_t)s * a.block + (r0 - a.p0) + r] : make_float2(-INFINITY, 0.f);
                 }
 #pragma unroll
                 for (int u = 0; u < 8; ++u) merge(p[u]);
@@ -464,9 +473,13 @@ VocabKernel pick(bool grad, bool extra, bool wide, bool direct)
 
 }  // namespace
 
+// The fewer rounds of resident workgroups, at their chunks' times and about 3 chunks' for a tile's start and outputs:
+// FIGURE.
 bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W)
 {
-    return on_grid(W, k) && ((n + 255) / 256) * ((cols + 255) / 256) >= 256;
+    if (!on_grid(W, k)) return false;
+    const int64_t w = ((n + 255) / 256) * ((cols + 255) / 256), s = ((n + 127) / 128) * ((cols + 127) / 128);
+    return (float)((w + 255) / 256) * kWideChunk < (float)((s + 511) / 512) * (s <= 256 ? kNarrowChunk : kNarrowChunks);
 }
 
 cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backward, hipStream_t stream)
@@ -499,7 +512,8 @@ cogdl_status vocab_logits_launch(VocabArgs a, cogdl_dtype dtype, bool grad, bool
     const bool extra = a.bias || (grad && a.db_part);
     const VocabKernel kern = dtype == COGDL_BF16 ? pick<bf16_t>(grad, extra, wide, direct) : pick<f16_t>(grad, extra, wide, direct);
     a.tiles_c = (int32_t)(((int64_t)a.width + tile - 1) / tile);
-    const int64_t all = (a.n + tile - 1) / tile * a.tiles_c;
+    const int64_t rows = grad ? a.n : a.block;
+    const int64_t all = (rows + tile - 1) / tile * a.tiles_c;
     return launch_vocab(grad ? "vocab_dz" : "vocab_stats", kern, a, all, waves, lds_of(waves, tile, tile), stream);
 }
 
@@ -519,17 +533,23 @@ struct Layout {
     }
 };
 
+// Bytes of statistics kept at once, about (256 rows' at least).
+constexpr int64_t kPartBytes = 256ll << 20;
+
 // The forward's workspace.
 size_t lay_forward(VocabArgs &a, char *ws)
 {
     Layout l;
     a.slots = (int32_t)(((int64_t)a.V + 63) / 64);
+    int64_t block = kPartBytes / ((int64_t)sizeof(float2) * a.slots) / 256 * 256;
+    if (block < 256) block = 256;
+    a.block = (int32_t)(block < a.n ? block : a.n);
     a.head = reinterpret_cast<RowsHead *>(ws + l.take(sizeof(RowsHead)));
     a.live = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 4 * (size_t)a.n : 0));
     a.tlse = reinterpret_cast<float *>(ws + l.take(a.distill ? 4 * (size_t)a.n : 0));
     a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * (size_t)a.n));
     a.Xr = ws + l.take(2 * (size_t)a.n * a.kp);
-    a.part = reinterpret_cast<float2 *>(ws + l.take(sizeof(float2) * (size_t)a.n * a.slots));
+    a.part = reinterpret_cast<float2 *>(ws + l.take(sizeof(float2) * (size_t)a.block * a.slots));
     return l.total;
 }
 
@@ -565,13 +585,17 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     }
     cogdl_status s = vocab_rows_launch(a, dtype, false, stream);
     if (s != COGDL_OK) return s;
-    s = vocab_logits_launch(a, dtype, false, vocab_wide(a.n, a.V, a.k, a.W), stream);
-    if (s != COGDL_OK) return s;
-    const int R = a.n <= 256 ? 1 : a.n <= 1024 ? 4 : 16;
-    int64_t blocks = (a.n + R - 1) / R;
+    const bool wide = vocab_wide(a.block, a.V, a.k, a.W);
+    const int R = a.block <= 256 ? 1 : a.block <= 1024 ? 4 : 16;
+    int64_t blocks = (a.block + R - 1) / R;
+    if (a.plain) blocks = a.n;
     if (blocks > 4096) blocks = 4096;
-    if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, R);
-    else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, R);
+    for (a.p0 = 0; a.p0 < a.n; a.p0 += a.block) {
+        s = vocab_logits_launch(a, dtype, false, wide, stream);
+        if (s != COGDL_OK) return s;
+        if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, a.plain ? 1 : R);
+        else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, a.plain ? 1 : R);
+    }
     return COGDL_OK;
 }
 

@@ -43,7 +43,7 @@ struct ProductsPlan {
     bool dx, dw;
 
     // (in floats: sizes are far apart, and no whole number has to come out)
-    __device__ __forceinline__ float cost(int32_t live, int32_t s) const
+    __host__ __device__ __forceinline__ float cost(int32_t live, int32_t s) const
     {
         const float tr = (float)((live + tile - 1) / tile), tk = (float)((k + tile - 1) / tile), tw = (float)((width + tile - 1) / tile);
         const float n1 = dx ? ceilf(tr * tk * s * 0.125f) : 0.f, n2 = dw ? ceilf(tw * tk * 0.125f) : 0.f, each = 1.f / resident;
@@ -85,12 +85,14 @@ struct VocabArgs {
     int32_t *col;                // live: the target (cross entropy)
     float *at_col;               // live: g (p - 1) there
     void *Xr;                    // live x kp: their features
-    float2 *part;                // [slot][n]: (max, sum) of a row's logits in a slot of columns, in powers of two
+    float2 *part;                // [slot][block]: (max, sum) of a row's logits in a slot of columns, in powers of two
     int32_t slots;
+    int32_t block;               // rows whose statistics are kept at once
+    int64_t p0;                  // the first of them
     void *dz;                    // live x (piece's columns, rounded up to 8): scaled by head->scale
     float *dx_part;              // [slice][live][kp]
     ProductsPlan plan;           // (backward)
-    float *db_part;              // [row tile][V]
+    float *db_part;              // [row tile][pitch]: a piece's
     int32_t row_tiles;
     unsigned long long *db_q;    // V: the targets' part, in units of 2^-unit_bits
     int32_t unit_bits;
@@ -202,6 +204,9 @@ inline cogdl_status launch_vocab(const char *name, VocabKernel kern, const Vocab
 cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backward, hipStream_t stream);
 // The logits: their (max, sum) by slots of columns, or the piece's dz.
 cogdl_status vocab_logits_launch(VocabArgs a, cogdl_dtype dtype, bool grad, bool wide, hipStream_t stream);
+
+// Time of a chunk of 64 for a compute unit, us: a tile of 256 x 256, or two of 128 x 128 (one alone).
+constexpr float kWideChunk = 1.85f, kNarrowChunks = 1.23f, kNarrowChunk = 0.75f;
 
 // Whether the logits of n rows by `cols` columns take tiles of 256 x 256 (else 128 x 128).
 bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W);

@@ -142,8 +142,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     }
 }
 
-// dX of the live rows from their slices' sums (workgroups below `dx_blocks`), db from the row tiles' sums and the
-// entries' part.
+// The piece's db from the row tiles' sums and the entries' part (workgroups from `dx_blocks` on), and, behind the last
+// piece, dX of the live rows from their slices' sums.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int rows_a_part)
 {
@@ -151,13 +151,13 @@ __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks
     const float unscale = a.head->unscale;
     if ((int)blockIdx.x >= dx_blocks) {
         const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
-        const int64_t v = (int64_t)(blockIdx.x - dx_blocks) * kBlock + threadIdx.x;
-        if (v >= a.V) return;
+        const int c = (int)(blockIdx.x - dx_blocks) * kBlock + (int)threadIdx.x;
+        if (c >= a.width) return;
         float t = 0.f;
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.V + v];
-        if (a.db_q) t = (float)((double)t - ldexp((double)(long long)a.db_q[v], -a.unit_bits));
-        a.db[v] = t * unscale;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.pitch + c];
+        if (a.db_q) t = (float)((double)t - ldexp((double)(long long)a.db_q[a.v0 + c], -a.unit_bits));
+        a.db[a.v0 + c] = t * unscale;
         return;
     }
     const int vecs = a.kp / 8, slices = a.head->slices;
@@ -194,11 +194,19 @@ int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1
 // size: 8192 rows, vocabulary 131072, 1024 features, FIGURE.
 constexpr int64_t kPieceBytes = 512ll << 20;
 
-// Whether the products over a piece take tiles of 256 x 256 (where W is on the grid): enough of them for most of
-// the chip.
-bool wide_products(int64_t n, int64_t width, int32_t k)
+// The plan of a piece's products with tiles of 256 x 256 or of 128 x 128, whichever ends first.
+void plan_products(ProductsPlan &p, int64_t n, const void *W)
 {
-    return k > 128 && k % 2 == 0 && tiles_of(n, k, 256) * (width / 512) + tiles_of(width, k, 256) >= 256;
+    float best[2];
+    for (int wide = 0; wide < 2; ++wide) {
+        p.tile = wide ? 256 : 128;
+        p.resident = wide ? 32 : 64;
+        best[wide] = p.cost((int32_t)n, 1);
+        for (int s = 2; s <= p.most; ++s) best[wide] = fminf(best[wide], p.cost((int32_t)n, s));
+    }
+    const bool wide = on_grid(W, p.k) && p.k > 128 && best[1] * kWideChunk < best[0] * kNarrowChunks;
+    p.tile = wide ? 256 : 128;
+    p.resident = wide ? 32 : 64;
 }
 
 int32_t piece_width(int64_t n, int32_t V)
@@ -211,12 +219,12 @@ int32_t piece_width(int64_t n, int32_t V)
     return (int32_t)(width < V ? width : V);
 }
 
-// Slices of 256 columns or more, and no more than the workspace has room for: 4 bytes of sums for each 2 of dz.
-int32_t most_slices(int32_t width, int32_t kp)
+// Slices of 256 columns or more, and no more than make 1024 tiles of dX.
+int32_t most_slices(int64_t n, int32_t width, int32_t k)
 {
-    int64_t most = width / 256, room = (int64_t)width / (kp > 0 ? kp : 1);
-    if (room < 16) room = 16;
-    if (most > room) most = room;
+    const int64_t tiles = tiles_of(n, k, 128);
+    int64_t most = tiles > 0 ? (1024 + tiles - 1) / tiles : 1;
+    if (most > width / 256) most = width / 256;
     if (most > kMostSlices) most = kMostSlices;
     return (int32_t)(most < 1 ? 1 : most);
 }
@@ -235,8 +243,7 @@ size_t lay_backward(VocabArgs &a, char *ws)
 {
     a.width = piece_width(a.n, a.V);
     a.pitch = (a.width + 7) / 8 * 8;
-    a.plan.most = most_slices(a.width, a.kp);
-    while (a.plan.most > 1 && !countable(tiles_of(a.n, a.k, 128), a.plan.most)) a.plan.most /= 2;
+    a.plan.most = most_slices(a.n, a.width, a.k);
     a.row_tiles = (int32_t)((a.n + 127) / 128 * 2);
     const size_t n = (size_t)a.n;
     Layout l;
@@ -251,7 +258,7 @@ size_t lay_backward(VocabArgs &a, char *ws)
     a.Xr = ws + l.take(2 * n * a.kp);
     a.dz = ws + l.take(2 * n * a.pitch);
     a.dx_part = reinterpret_cast<float *>(ws + l.take(4 * n * a.kp * a.plan.most));
-    a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.V));
+    a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.pitch));
     a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(a.distill ? 8 * (size_t)a.V : 0));
     return l.total;
 }
@@ -292,14 +299,13 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
     a.unit_bits = 46 - bits_for((uint64_t)a.n);
     const bool bf16 = dtype == COGDL_BF16;
     const bool wide_logits = vocab_wide(a.n, piece, a.k, a.W);
-    const bool wide = on_grid(a.W, a.k) && wide_products(a.n, piece, a.k);
-    const int tile = wide ? 256 : 128, waves = wide ? 8 : 4;
-    a.plan.tile = tile;
-    a.plan.resident = wide ? 32 : 64;
     a.plan.width = piece;
     a.plan.k = a.k;
     a.plan.dx = a.dX != nullptr;
     a.plan.dw = a.dW != nullptr;
+    plan_products(a.plan, a.n, a.W);
+    const int tile = a.plan.tile, waves = tile == 256 ? 8 : 4;
+    const bool wide = tile == 256;
     COGDL_TRY(vocab_rows_launch(a, dtype, true, stream));
     for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
         a.v0 = (int32_t)v0;
@@ -315,18 +321,20 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
                 else COGDL_LAUNCH("vocab_entries", k_vocab_entries<f16_t>, grid, kBlock, stream, a);
             }
         }
-        if (!a.dX && !a.dW) continue;
-        a.tiles_c = a.tiles_w = (a.k + tile - 1) / tile;
-        const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) : 0);
-        COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
-                               a, tiles, waves, lds_of(waves, tile, tile), stream));
+        if (a.dX || a.dW) {
+            a.tiles_c = a.tiles_w = (a.k + tile - 1) / tile;
+            const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) : 0);
+            COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
+                                   a, tiles, waves, lds_of(waves, tile, tile), stream));
+        }
+        const bool last = a.V - v0 <= piece;
+        int64_t dx_blocks = a.dX && last ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
+        if (dx_blocks > 4096) dx_blocks = 4096;
+        const unsigned grid = (unsigned)(dx_blocks + (a.db ? (a.width + kBlock - 1) / kBlock : 0));
+        if (grid == 0) continue;
+        if (bf16) COGDL_LAUNCH("vocab_out", k_vocab_out<bf16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
+        else COGDL_LAUNCH("vocab_out", k_vocab_out<f16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
     }
-    if (!a.dX && !a.db) return COGDL_OK;
-    int64_t dx_blocks = a.dX ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
-    if (dx_blocks > 4096) dx_blocks = 4096;
-    const unsigned grid = (unsigned)(dx_blocks + (a.db ? ((int64_t)a.V + kBlock - 1) / kBlock : 0));
-    if (bf16) COGDL_LAUNCH("vocab_out", k_vocab_out<bf16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
-    else COGDL_LAUNCH("vocab_out", k_vocab_out<f16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
     return COGDL_OK;
 }
 

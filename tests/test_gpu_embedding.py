@@ -172,3 +172,31 @@ def test_gradient_has_the_same_bits_again():
     index = tokens(50_000, 300, g, 3.0).cuda()
     first = cg.embedding_backward(dY, index, 300)
     assert all(torch.equal(first, cg.embedding_backward(dY, index, 300)) for _ in range(3))
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 1023, 1025, 8191, 8192, 8193])
+def test_gradient_around_the_lengths_of_the_sorts(n):
+    """Lists up to 8192 are sorted by one workgroup, longer ones by radix passes over the chip; tokens of 2 to 22 bits."""
+    for V, k in ((3, 40), (5000, 7), (4_000_000, 2)):
+        check_gradient(n, V, k, "f32", "f32", 1.3, n % 2 == 0, n + V)
+
+
+def test_gradient_is_summed_in_the_order_of_the_batch():
+    """One token's rows that only add up right in order: 2^24 + 1 + 1 ... stays 2^24 in fp32, 1 + 1 + ... + 2^24 does
+    not.  (15 rows: one piece.)"""
+    big = torch.full((15, 4), 1.0, device="cuda")
+    big[0] = 2.0 ** 24
+    zeros = torch.zeros(15, dtype=torch.int32, device="cuda")
+    assert (cg.embedding_backward(big, zeros, 1) == 2.0 ** 24).all()
+    assert (cg.embedding_backward(big.flip(0).contiguous(), zeros, 1) == 2.0 ** 24 + 14).all()
+
+
+def test_gradient_of_one_token_among_millions_added():
+    """Adding touches the rows it names and no other: the rest of a large table keeps its bits, NaN among them."""
+    V, k = 1_000_000, 8
+    base = torch.full((V, k), float("nan"), device="cuda")
+    at = torch.tensor([7, 999_999, 7], dtype=torch.int32, device="cuda")
+    base[7], base[999_999] = 1.0, 2.0
+    got = cg.embedding_backward(torch.ones(3, k, device="cuda"), at, V, scale=0.5, out=base, accumulate=True)
+    assert got is base and (got[7] == 2).all() and (got[999_999] == 2.5).all()
+    assert int(torch.isnan(got).all(1).sum()) == V - 2

@@ -93,7 +93,7 @@ def gradients(X, W, index, q, held, live, g, bias=None, T=1.0):
 
 
 def close(name, got, value, bound):
-    d = (got.double().cpu() - value).abs()
+    d = (got.double().to(value.device) - value).abs()
     bad = ~(d <= bound)
     assert not bad.any(), (f"{name}: {int(bad.sum())} of {bad.numel()} past the bound, the worst "
                            f"{float((d / bound.clamp(min=1e-300)).max()):.3g} times, off by {float(d.max()):.3g}")
