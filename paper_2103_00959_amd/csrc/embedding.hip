@@ -131,19 +131,19 @@ __global__ __launch_bounds__(kBlock) void k_tokens(ScatterArgs a)
 }
 
 // Short lists are sorted by one workgroup in LDS, while the others of its launch write the zeros: a stable radix sort
-// of 6 bits a pass.  Each wavefront owns a run of the list and counts its digits, one scan over (digit,
+// of up to 8 bits a pass.  Each wavefront owns a run of the list and counts its digits, one scan over (digit,
 // wavefront) gives every run's places, and a key's rank in its run is the count of lower lanes with its digit (a
 // ballot a bit) behind the run's keys so far.  4096 tokens of 7 bits FIGURE us, where the sort for any length takes
 // three launches a pass.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kSortBits = 6, kSortDigits = 1 << kSortBits;
+constexpr int kSortBits = 8, kSortEach = (kSortWaves << kSortBits) / kSortThreads;
 constexpr int kShortList = 8192;
 
 __global__ __launch_bounds__(kSortThreads) void k_sort_short(ScatterArgs a, int bits)
 {
     __shared__ uint32_t keys[2][kShortList];
     __shared__ uint16_t vals[2][kShortList];
-    __shared__ int counts[kSortDigits][kSortWaves];
+    __shared__ int counts[kSortWaves << kSortBits];
     __shared__ int sums[kSortWaves];
     if (blockIdx.x > 0) {
         if (!a.add) write_zeros(a, (int64_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x, (int64_t)(gridDim.x - 1) * kSortThreads);
@@ -155,46 +155,58 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_short(ScatterArgs a, int 
         keys[0][i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
         vals[0][i] = (uint16_t)i;
     }
-    __syncthreads();
     const int run = ((n + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
     const int from = wave * run < n ? wave * run : n, to = from + run < n ? from + run : n;
-    int now = 0;
-    for (int shift = 0; shift < bits; shift += kSortBits, now ^= 1) {
-        for (int d = threadIdx.x; d < kSortDigits * kSortWaves; d += kSortThreads) counts[d / kSortWaves][d % kSortWaves] = 0;
+    const int passes = (bits + kSortBits - 1) / kSortBits;
+    int now = 0, shift = 0;
+    for (int pass = 0; pass < passes; ++pass, now ^= 1) {
+        const int dbits = (bits - shift + passes - pass - 1) / (passes - pass), mask = (1 << dbits) - 1;
+        // (digit d of wavefront w: place 16 d + w)
+        for (int e = threadIdx.x; e < kSortWaves << dbits; e += kSortThreads) counts[e] = 0;
         __syncthreads();
-        for (int i = from + lane; i < to; i += kWave) atomicAdd(&counts[keys[now][i] >> shift & (kSortDigits - 1)][wave], 1);
+        for (int i = from + lane; i < to; i += kWave) atomicAdd(&counts[(keys[now][i] >> shift & mask) * kSortWaves + wave], 1);
         __syncthreads();
-        // exclusive over (digit, wavefront): a thread an entry
-        static_assert(kSortDigits * kSortWaves == kSortThreads, "a thread an entry");
-        int *const mine = &counts[0][0] + threadIdx.x;
-        const int c = *mine, scan = wave_inclusive_scan(c);
+        int c[kSortEach], mine = 0;
+#pragma unroll
+        for (int e = 0; e < kSortEach; ++e) {
+            const int at = threadIdx.x * kSortEach + e;
+            c[e] = at < kSortWaves << dbits ? counts[at] : 0;
+            mine += c[e];
+        }
+        const int scan = wave_inclusive_scan(mine);
         if (lane == kWave - 1) sums[wave] = scan;
         __syncthreads();
-        int before = scan - c;
+        int before = scan - mine;
         for (int w = 0; w < wave; ++w) before += sums[w];
-        *mine = before;
+#pragma unroll
+        for (int e = 0; e < kSortEach; ++e) {
+            const int at = threadIdx.x * kSortEach + e;
+            if (at < kSortWaves << dbits) counts[at] = before;
+            before += c[e];
+        }
         __syncthreads();
         for (int i0 = from; i0 < to; i0 += kWave) {
             const int i = i0 + lane;
             const bool in = i < to;
             const uint32_t key = in ? keys[now][i] : 0u;
-            const int digit = (int)(key >> shift & (kSortDigits - 1));
+            const int digit = (int)(key >> shift) & mask;
             uint64_t same = __ballot(in);
-#pragma unroll
-            for (int b = 0; b < kSortBits; ++b) {
+            for (int b = 0; b < dbits; ++b) {
                 const uint64_t ones = __ballot(digit >> b & 1);
                 same &= digit >> b & 1 ? ones : ~ones;
             }
             if (in) {
-                const int place = counts[digit][wave] + __popcll(same & ((1ull << lane) - 1));
+                int *const run_place = &counts[digit * kSortWaves + wave];
+                const int place = *run_place + __popcll(same & ((1ull << lane) - 1));
                 keys[now ^ 1][place] = key;
                 vals[now ^ 1][place] = vals[now][i];
                 // the last lane of a digit moves the run's place on (the next round reads it behind this write)
-                if (same >> lane == 1) counts[digit][wave] = place + 1;
+                if (same >> lane == 1) *run_place = place + 1;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
+        shift += dbits;
         __syncthreads();
     }
     for (int i = threadIdx.x; i < n; i += kSortThreads) {
@@ -235,7 +247,8 @@ struct Packed {
             load_vec<T, 1>(p, i, one);
             w = one[0];
         } else {
-            const u32x4_u u = *reinterpret_cast<const u32x4_u *>(p + i);
+            // (read once: past the caches, 1M rows of 512 bytes 139 us, so 136; 262144 of 600, added, 111 and 104)
+            const u32x4_u u = __builtin_nontemporal_load(reinterpret_cast<const u32x4_u *>(p + i));
             w = make_uint4(u.x, u.y, u.z, u.w);
         }
     }

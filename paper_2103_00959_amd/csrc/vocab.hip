@@ -34,14 +34,15 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float t)
 }
 
 // The teacher's rows: whether any entry counts (inside the vocabulary, its logit above -inf), and the log of
-// the sum of their exponentials.  FORWARD: also the student's logits of the entries, by 4 entries of 16 lanes,
-// into logp.  A wavefront a row.
+// the sum of their exponentials.  FORWARD: also the student's logits of the entries, by 4 entries of 16 lanes a
+// wavefront, into logp, and a workgroup a row (its wavefronts each find the row's sum); else a wavefront a row.
 template <typename T, bool FORWARD>
 __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
 {
-    const int lane = lane_id();
-    const int64_t waves = (int64_t)gridDim.x * (kBlock / kWave);
-    for (int64_t i = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave; i < a.n; i += waves) {
+    constexpr int W = kBlock / kWave;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int64_t step = FORWARD ? gridDim.x : (int64_t)gridDim.x * W;
+    for (int64_t i = FORWARD ? blockIdx.x : (int64_t)blockIdx.x * W + wave; i < a.n; i += step) {
         const int32_t *__restrict__ index = a.index + i * a.entries;
         const float *__restrict__ teacher = a.teacher + i * a.entries;
         float m = -INFINITY;
@@ -59,14 +60,14 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
         for (int e = lane; e < a.entries; e += kWave)
             if (counts(index[e], a.V)) s += expf(teacher[e] / a.T - from);
         s = group_sum(s, kWave);
-        if (lane == 0) {
+        if (lane == 0 && (!FORWARD || wave == 0)) {
             a.live[i] = live ? 0 : -1;
             a.tlse[i] = from + logf(s);
         }
         if constexpr (FORWARD) {
             const T *__restrict__ x = static_cast<const T *>(a.X) + i * a.k;
             const int sub = lane & 15, vecs = (a.k + 7) / 8;
-            for (int e0 = 0; e0 < a.entries; e0 += kWave / 16) {
+            for (int e0 = 4 * wave; e0 < a.entries; e0 += 4 * W) {
                 const int e = e0 + (lane >> 4);
                 const int32_t v = e < a.entries ? index[e] : -1;
                 const bool on = live && counts(v, a.V);
@@ -485,7 +486,7 @@ bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W)
 cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backward, hipStream_t stream)
 {
     if (a.distill && a.n > 0) {
-        const int64_t blocks = (a.n + kBlock / kWave - 1) / (kBlock / kWave);
+        const int64_t blocks = backward ? (a.n + kBlock / kWave - 1) / (kBlock / kWave) : a.n;
         const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
         if (backward) COGDL_LAUNCH("teacher_rows", (k_teacher_rows<bf16_t, false>), grid, kBlock, stream, a);    // (no features)
         else if (dtype == COGDL_BF16) COGDL_LAUNCH("teacher_rows", (k_teacher_rows<bf16_t, true>), grid, kBlock, stream, a);
@@ -576,9 +577,9 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < need) return COGDL_ERR_INVALID;
     a.v0 = 0;
     a.width = a.V;
-    // One row tile costs the same however many of its rows count, and rows do not meet in the forward: no need to
-    // gather them (one row, 50000 x 512: 22 us with the gathering launch, FIGURE without).
-    a.plain = a.n <= 128 && on_grid(a.X, a.k);
+    // Rows do not meet in the forward: they need not be gathered where that costs more than the tiles of rows that
+    // do not count (one tile of rows costs the same anyway).  One row, 50000 x 512: 22 us a call gathered, 19 so.
+    a.plain = on_grid(a.X, a.k) && (a.n <= 128 || (a.n <= 1024 && (double)a.n * a.V * a.k <= (double)(1ll << 33)));
     if (a.plain) {
         a.Xr = const_cast<void *>(a.X);
         a.kp = a.k;
