@@ -544,8 +544,7 @@ cogdl_status cogdl_embedding(int64_t n, int32_t V, int32_t k, const void *table,
  * "never accumulated into": the other gradient of a tied table), and the rows
  * of indices that do not occur are neither read nor written; else they become
  * zeros.  Places whose index lies outside [0, V) count for nothing, whatever dY
- * holds there.  The sums are fp32, over the places of an index in order, and
- * rounded once.  workspace: device scratch of at least the size that
+ * holds there.  The sums are fp32, in a fixed order, and rounded once.  workspace: device scratch of at least the size that
  * cogdl_embedding_backward_workspace reports (0 where n or k is 0: NULL is then
  * accepted), 256-byte aligned; its contents are clobbered, and calls in flight
  * together need one each.
@@ -568,8 +567,8 @@ cogdl_status cogdl_embedding_backward(int64_t n, int32_t V, int32_t k, const voi
  * are fp32; a loss is off by the rounding of its logits, so one far below
  * 2^-24 of them (a certain answer) may come out as 0, never below.  A NaN in a
  * row that counts, or a logit of +inf, makes its loss NaN.
- * n up to 2^24, k up to 2^22, and n x V up to 2^45 (tiles of 128 x 128 are
- * counted in 31 bits; COGDL_ERR_TOO_LARGE past these).  Any alignment of X and W
+ * n up to 2^24, k up to 2^22, and n x V, n x k and V x k up to 2^45 (tiles of
+ * 128 x 128 are counted in 31 bits; COGDL_ERR_TOO_LARGE past these).  Any alignment of X and W
  * is right; rows of W of an even number of elements on the 4-byte grid are
  * fastest.  workspace: device scratch of at least the size that
  * cogdl_linear_loss_workspace reports (K = 0 for cross entropy, the entries
@@ -608,7 +607,7 @@ cogdl_status cogdl_linear_cross_entropy_backward(int64_t n, int32_t V, int32_t k
 
 /* ------------------------------------------------------------------------
  * Distillation from a teacher's top logits: the loss of the same layer against
- * the K answers that a teacher gives each row.  With temperature T > 0,
+ * the K answers that a teacher gives each row.  With temperature T in [2^-20, 2^20],
  *   q[i, :]    = softmax over the entries that count of teacher[i, :] / T
  *   lse[i]     = log sum_v exp(z[i, v] / T)          (over the whole vocabulary)
  *   logp[i, e] = z[i, index[i, e]] / T - lse[i]

@@ -1172,7 +1172,7 @@ def embedding_backward_workspace(n: int, V: int, k: int) -> int:
 def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, out=None, accumulate: bool = False,
                        workspace=None):
     """Gradient of embedding for dY = dL/dY [n, k]: dtable [V, k] in out_dtype (dY's by default), with
-    dtable[v] = scale * the sum of dY over the places of v, in fp32 and in order (the same bits every run).
+    dtable[v] = scale * the sum of dY over the places of v, in fp32 and in a fixed order (the same bits every run).
     With ``accumulate``, ``out`` must be given: the sums are added to it, and its other rows are left alone (the
     other gradient of a tied table, such as linear_cross_entropy_backward's dW); else they become zeros.  Padded
     places (an index outside [0, V)) count for nothing.  ``workspace``: at least embedding_backward_workspace
@@ -1240,8 +1240,8 @@ def _teacher(index, teacher, n, temperature):
     K = index.shape[1]
     if K < 1 or K > MAX_TEACHER:
         raise CogdlError(f"index has {K} entries a row, 1 to {MAX_TEACHER} are supported")
-    if not 0.0 < float(temperature) < float("inf"):
-        raise CogdlError(f"temperature must be positive and finite, got {temperature}")
+    if not 2.0 ** -20 <= float(temperature) <= 2.0 ** 20:
+        raise CogdlError(f"temperature must be positive, from 2^-20 to 2^20, got {temperature}")
     return K
 
 

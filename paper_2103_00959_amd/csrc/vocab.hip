@@ -360,32 +360,29 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
 }
 
 // The slots of a row joined to its lse, and the loss from its targets' logits.  R rows a workgroup (a power of
-// two up to 16), 256 / R threads each.  Rows as they were given (R = 1): which count, and their target's logit, are
-// found here.
+// two up to 16), 256 / R threads each.  Of rows as they were given, which count, and their targets' logits, are found
+// here.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
 {
     constexpr int W = kBlock / kWave;
     __shared__ float2 part[kBlock];
-    __shared__ float lse_of[16], dots[W];
+    __shared__ float lse_of[16], dots[16];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     int64_t live = a.plain ? a.n : a.head->off[1];
     live = live < a.p0 + a.block ? live : a.p0 + a.block;
     const int r = threadIdx.x & (R - 1), sg = threadIdx.x / R, S = kBlock / R;
     for (int64_t r0 = a.p0 + (int64_t)blockIdx.x * R; r0 < live; r0 += (int64_t)gridDim.x * R) {
-        if (a.plain) {
-            const int32_t t = a.distill ? a.live[r0] : a.index[r0];
-            if (!counts(t, a.distill ? INT32_MAX : a.V)) {           // (uniform)
-                if (threadIdx.x == 0) a.loss[r0] = a.lse[r0] = 0.f;
-                continue;
-            }
-            if (!a.distill) {
+        if (a.plain && !a.distill) {
+            for (int q = wave; q < R && r0 + q < live; q += W) {
+                const int32_t t = a.index[r0 + q];
                 float dot = 0.f;
-                for (int v = threadIdx.x; v < (a.k + 7) / 8; v += kBlock)
-                    dot = dot8<T>(load_vec8(static_cast<const T *>(a.X) + r0 * a.k, v, a.k),
-                                  load_vec8(static_cast<const T *>(a.W) + (int64_t)t * a.k, v, a.k), dot);
+                if (counts(t, a.V))
+                    for (int v = lane; v < (a.k + 7) / 8; v += kWave)
+                        dot = dot8<T>(load_vec8(static_cast<const T *>(a.X) + (r0 + q) * a.k, v, a.k),
+                                      load_vec8(static_cast<const T *>(a.W) + (int64_t)t * a.k, v, a.k), dot);
                 dot = group_sum(dot, kWave);
-                if (lane == 0) dots[wave] = dot;
+                if (lane == 0) dots[q] = dot;
             }
         }
         float m = -INFINITY, z = 0.f;
@@ -421,27 +418,29 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
             const float lse = ((m == -INFINITY ? 0.f : m) + log2f(z)) * kLn2;
             lse_of[r] = lse;
             if (r0 + r < live) {
-                const int64_t i = a.plain ? r0 : a.rows[r0 + r];
-                a.lse[i] = lse;
-                if (!a.distill) {
-                    float dot = 0.f;
-                    if (a.plain) {
-#pragma unroll
-                        for (int w = 0; w < W; ++w) dot += dots[w];
-                        if (a.bias) dot += a.bias[a.index[i]];
-                    } else {
-                        dot = a.loss[i];
+                const int64_t i = a.plain ? r0 + r : a.rows[r0 + r];
+                if (a.plain && !counts(a.distill ? a.live[i] : a.index[i], a.distill ? INT32_MAX : a.V)) {
+                    a.lse[i] = 0.f;
+                    if (!a.distill) a.loss[i] = 0.f;
+                } else {
+                    a.lse[i] = lse;
+                    if (!a.distill) {
+                        const float dot = a.plain ? dots[r] + (a.bias ? a.bias[a.index[i]] : 0.f) : a.loss[i];
+                        // (above 0 by definition; the two sums' roundings may differ)
+                        const float loss = lse - dot;
+                        a.loss[i] = loss < 0.f ? 0.f : loss;
                     }
-                    // (above 0 by definition; the two sums' roundings may differ)
-                    const float loss = lse - dot;
-                    a.loss[i] = loss < 0.f ? 0.f : loss;
                 }
             }
         }
         __syncthreads();                                 // (lse_of; part and dots are read)
         if (!a.distill) continue;
         for (int q = wave; q < R && r0 + q < live; q += W) {
-            const int64_t i = a.plain ? r0 : a.rows[r0 + q];
+            const int64_t i = a.plain ? r0 + q : a.rows[r0 + q];
+            if (a.plain && a.live[i] < 0) {
+                if (lane == 0) a.loss[i] = 0.f;
+                continue;
+            }
             const float lse = lse_of[q], tlse = a.tlse[i];
             float loss = 0.f;
             for (int e = lane; e < a.entries; e += kWave) {
@@ -524,16 +523,6 @@ using namespace cogdl;
 
 namespace {
 
-struct Layout {
-    size_t total = 0;
-    size_t take(size_t bytes)
-    {
-        const size_t at = total;
-        total += (bytes + 255) & ~size_t(255);
-        return at;
-    }
-};
-
 // Bytes of statistics kept at once, about (256 rows' at least).
 constexpr int64_t kPartBytes = 256ll << 20;
 
@@ -554,20 +543,11 @@ size_t lay_forward(VocabArgs &a, char *ws)
     return l.total;
 }
 
-cogdl_status check_sizes(int64_t n, int32_t V, int32_t k, int32_t K)
-{
-    if (n < 0 || V < 1 || k < 0 || K < 1) return COGDL_ERR_INVALID;
-    if (n > kMaxRows || k > kMaxWidth || K > kMaxEntries) return COGDL_ERR_TOO_LARGE;
-    if (!countable((n + 127) / 128, ((int64_t)V + 127) / 128)) return COGDL_ERR_TOO_LARGE;
-    return COGDL_OK;
-}
-
 cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
     if (dtype != COGDL_BF16 && dtype != COGDL_F16) return COGDL_ERR_DTYPE;
-    const cogdl_status st = check_sizes(a.n, a.V, a.k, a.entries);
+    const cogdl_status st = check_sizes(a);
     if (st != COGDL_OK) return st;
-    if (!(a.T > 0.f) || a.T > 3.4e38f) return COGDL_ERR_INVALID;
     if (a.n == 0) return COGDL_OK;
     if (!a.index || !a.loss || !a.lse || (a.k > 0 && (!a.X || !a.W))) return COGDL_ERR_INVALID;
     if (a.distill && (!a.teacher || !a.logp)) return COGDL_ERR_INVALID;
@@ -579,7 +559,7 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     a.width = a.V;
     // Rows do not meet in the forward: they need not be gathered where that costs more than the tiles of rows that
     // do not count (one tile of rows costs the same anyway).  One row, 50000 x 512: 22 us a call gathered, 19 so.
-    a.plain = on_grid(a.X, a.k) && (a.n <= 128 || (a.n <= 1024 && (double)a.n * a.V * a.k <= (double)(1ll << 33)));
+    a.plain = on_grid(a.X, a.k) && (a.n <= 128 || (a.n <= 4096 && (double)a.n * a.V * a.k <= (double)(1ll << 33)));
     if (a.plain) {
         a.Xr = const_cast<void *>(a.X);
         a.kp = a.k;
@@ -589,13 +569,12 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     const bool wide = vocab_wide(a.block, a.V, a.k, a.W);
     const int R = a.block <= 256 ? 1 : a.block <= 1024 ? 4 : 16;
     int64_t blocks = (a.block + R - 1) / R;
-    if (a.plain) blocks = a.n;
     if (blocks > 4096) blocks = 4096;
     for (a.p0 = 0; a.p0 < a.n; a.p0 += a.block) {
         s = vocab_logits_launch(a, dtype, false, wide, stream);
         if (s != COGDL_OK) return s;
-        if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, a.plain ? 1 : R);
-        else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, a.plain ? 1 : R);
+        if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, R);
+        else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, R);
     }
     return COGDL_OK;
 }
@@ -611,7 +590,8 @@ cogdl_status cogdl_linear_loss_workspace(int64_t n, int32_t V, int32_t k, int32_
     a.n = n; a.V = V; a.k = k;
     a.entries = K > 0 ? K : 1;
     a.distill = K > 0;
-    const cogdl_status st = check_sizes(n, V, k, a.entries);
+    a.T = 1.f;
+    const cogdl_status st = check_sizes(a);
     if (st != COGDL_OK) return st;
     a.kp = (k + 7) / 8 * 8;
     *bytes = n > 0 ? lay_forward(a, nullptr) : 0;

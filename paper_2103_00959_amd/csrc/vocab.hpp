@@ -104,6 +104,27 @@ struct VocabArgs {
     bool first;                  // the first piece
 };
 
+// Sizes and temperature of a call.  (Temperatures past 2^20 either way: logits over them leave fp32's range.)
+inline cogdl_status check_sizes(const VocabArgs &a)
+{
+    if (a.n < 0 || a.V < 1 || a.k < 0 || a.entries < 1) return COGDL_ERR_INVALID;
+    if (!(a.T >= 1.f / (1 << 20) && a.T <= (float)(1 << 20))) return COGDL_ERR_INVALID;
+    if (a.n > kMaxRows || a.k > kMaxWidth || a.entries > kMaxEntries) return COGDL_ERR_TOO_LARGE;
+    const int64_t tr = (a.n + 127) / 128, tv = ((int64_t)a.V + 127) / 128, tk = ((int64_t)a.k + 127) / 128;
+    return countable(tr, tv) && countable(tr, tk) && countable(tv, tk) ? COGDL_OK : COGDL_ERR_TOO_LARGE;
+}
+
+// Parts of a workspace, one after another on 256 bytes.
+struct Layout {
+    size_t total = 0;
+    size_t take(size_t bytes)
+    {
+        const size_t at = total;
+        total += (bytes + 255) & ~size_t(255);
+        return at;
+    }
+};
+
 using VocabKernel = void (*)(VocabArgs);
 
 // The tiles of one output of R x C tiles (R >= 0, known on the device), S slices of the sum each.  Tiles are

@@ -229,16 +229,6 @@ int32_t most_slices(int64_t n, int32_t width, int32_t k)
     return (int32_t)(most < 1 ? 1 : most);
 }
 
-struct Layout {
-    size_t total = 0;
-    size_t take(size_t bytes)
-    {
-        const size_t at = total;
-        total += (bytes + 255) & ~size_t(255);
-        return at;
-    }
-};
-
 size_t lay_backward(VocabArgs &a, char *ws)
 {
     a.width = piece_width(a.n, a.V);
@@ -263,15 +253,6 @@ size_t lay_backward(VocabArgs &a, char *ws)
     return l.total;
 }
 
-cogdl_status check_sizes(int64_t n, int32_t V, int32_t k, int32_t K)
-{
-    if (n < 0 || V < 1 || k < 0 || K < 1) return COGDL_ERR_INVALID;
-    if (n > kMaxRows || k > kMaxWidth || K > kMaxEntries) return COGDL_ERR_TOO_LARGE;
-    const int64_t tr = (n + 127) / 128, tv = ((int64_t)V + 127) / 128, tk = ((int64_t)k + 127) / 128;
-    if (!countable(tr, tv) || !countable(tr, tk) || !countable(tv, tk)) return COGDL_ERR_TOO_LARGE;
-    return COGDL_OK;
-}
-
 #define COGDL_TRY(expr)                              \
     do {                                             \
         const cogdl_status _s = (expr);              \
@@ -281,8 +262,7 @@ cogdl_status check_sizes(int64_t n, int32_t V, int32_t k, int32_t K)
 cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
     if (dtype != COGDL_BF16 && dtype != COGDL_F16) return COGDL_ERR_DTYPE;
-    COGDL_TRY(check_sizes(a.n, a.V, a.k, a.entries));
-    if (!(a.T > 0.f) || a.T > 3.4e38f) return COGDL_ERR_INVALID;
+    COGDL_TRY(check_sizes(a));
     if (a.n > 0 && (!a.index || !a.dloss || !a.lse_in || (a.k > 0 && (!a.X || !a.W)))) return COGDL_ERR_INVALID;
     if (a.n > 0 && (a.distill ? !a.teacher || !a.logp_in : !a.loss_in)) return COGDL_ERR_INVALID;
     if (a.k == 0) a.dX = a.dW = nullptr;
@@ -352,7 +332,8 @@ cogdl_status cogdl_linear_loss_backward_workspace(int64_t n, int32_t V, int32_t 
     a.n = n; a.V = V; a.k = k;
     a.entries = K > 0 ? K : 1;
     a.distill = K > 0;
-    COGDL_TRY(check_sizes(n, V, k, a.entries));
+    a.T = 1.f;
+    COGDL_TRY(check_sizes(a));
     a.kp = (k + 7) / 8 * 8;
     *bytes = lay_backward(a, nullptr);
     return COGDL_OK;

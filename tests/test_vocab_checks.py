@@ -85,7 +85,8 @@ def test_loss_validation(L, way, K):
     for bad in ((-1, 100, 16, K), (8, 0, 16, K), (8, 100, -1, K), (8, 100, 16, -1)):
         assert S(*bad, ctypes.byref(size)) == INVALID
     assert S(8, 100, 16, K, None) == INVALID
-    large = ((2 ** 24 + 1, 100, 16), (8, 100, 2 ** 22 + 1), (2 ** 24, 2 ** 31 - 1, 16))
+    large = ((2 ** 24 + 1, 100, 16), (8, 100, 2 ** 22 + 1), (2 ** 24, 2 ** 31 - 1, 16), (2 ** 24, 100, 2 ** 22),
+             (8, 2 ** 31 - 1, 2 ** 22))
     for bad in large:
         assert S(*bad, K, ctypes.byref(size)) == TOO_LARGE and f(*bad) == TOO_LARGE
     assert S(8, 100, 16, 1025, ctypes.byref(size)) == TOO_LARGE
@@ -105,7 +106,7 @@ def test_loss_validation(L, way, K):
     if K:
         assert f(teacher=None) == INVALID and f(logp=None) == INVALID
         assert f(K=0 - 1) == INVALID and f(K=1025) == TOO_LARGE
-        for T in (0.0, -1.0, INF, float("nan")):
+        for T in (0.0, -1.0, INF, float("nan"), 2.0 ** -21, 2.0 ** 21):
             assert f(T=T) == INVALID
 
 
@@ -165,7 +166,7 @@ def test_distill_sizes():
     refused(lambda: f(X, W, index, teacher[:, :2]), r"must both be \[4, K\]")
     refused(lambda: f(X, W, index[:, :0], teacher[:, :0]), "0 entries")
     refused(lambda: f(X, W, torch.zeros(4, 1025, dtype=i32), torch.zeros(4, 1025)), "1025 entries")
-    for T in (0.0, -2.0, INF, float("nan")):
+    for T in (0.0, -2.0, INF, float("nan"), 2.0 ** -21, 2.0 ** 21):
         refused(lambda: f(X, W, index, teacher, temperature=T), "temperature must be positive")
     refused(lambda: f(X, W, index, teacher, logp=torch.zeros(4, 2)), "logp has 8 elements, expected 12")
     reaches_device_check(lambda: b(v, X, W, index, teacher, v, teacher))
