@@ -253,7 +253,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
         rows -= a.p0;
         rows = rows < 0 ? 0 : rows < a.block ? rows : a.block;
     }
-    walk.start(rows, TM, a.tiles_c, 1, blockIdx.x);
+    walk.start(rows, TM, a.tiles_c, 1, blockIdx.x, GRAD ? kPanel : 2 * kPanel, GRAD);
     RowOperand<T, TM, N, kDirect> A;
     RowOperand<T, TN, N, SRCB> B;
     const auto open = [&](const Span &s) {
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
                         c += col0;
                         // (past the caches: it is read when the whole piece is there; of 8192 x 131072, 1024 features, the
                         // products took 3885 us, so 3790)
-                        if (r < s.have && c < a.pitch)
+                        if (r < s.have && c < a.width)
                             __builtin_nontemporal_store(__builtin_bit_cast(u32x4_u, w), reinterpret_cast<u32x4_u *>(dz + (int64_t)r * a.pitch + c));
                     });
                 if constexpr (EXTRA) {

@@ -62,7 +62,7 @@ struct ProductsPlan {
 
 struct VocabArgs {
     int64_t n;                   // rows given
-    int32_t V, k, kp;            // kp: k rounded up to 8, the pitch of the gathered rows
+    int32_t V, k, kp;            // kp: k rounded up to 8
     int32_t entries;             // of a row: 1 (cross entropy), K (distillation)
     bool distill;
     bool plain;                  // the rows as they were given stand for the gathered ones (few of them, forward)
@@ -84,12 +84,12 @@ struct VocabArgs {
     float *lse2, *g;             // live: lse log2(e), g T
     int32_t *col;                // live: the target (cross entropy)
     float *at_col;               // live: g (p - 1) there
-    void *Xr;                    // live x kp: their features
+    void *Xr;                    // live x kp: their features, zeros from k on
     float2 *part;                // [slot][block]: (max, sum) of a row's logits in a slot of columns, in powers of two
     int32_t slots;
     int32_t block;               // rows whose statistics are kept at once
     int64_t p0;                  // the first of them
-    void *dz;                    // live x (piece's columns, rounded up to 8): scaled by head->scale
+    void *dz;                    // live x pitch: scaled by head->scale, zeros from width to the next multiple of 8
     float *dx_part;              // [slice][live][kp]
     ProductsPlan plan;           // (backward)
     float *db_part;              // [row tile][pitch]: a piece's
@@ -128,38 +128,46 @@ struct Layout {
 using VocabKernel = void (*)(VocabArgs);
 
 // The tiles of one output of R x C tiles (R >= 0, known on the device), S slices of the sum each.  Tiles are
-// numbered slice by slice, then in panels of kPanel row tiles, in a panel column by column; the XCDs take equal runs
-// of them, their workgroups one after another: those that run together on an XCD take kPanel rows of tiles by a
-// few columns, and share both operands in its L2.
-constexpr int kPanel = 8;
+// numbered slice by slice, then in panels of so many row tiles, in a panel column by column; the XCDs take equal runs
+// of them, their workgroups one after another: those that run together on an XCD take a panel's rows of tiles by a
+// few columns, and share both operands in its L2.  TURNED: each XCD begins an eighth of its run further on than the
+// one before.  The XCDs that go through the same columns side by side share them in the Infinity Cache (the
+// statistics of 8192 x 131072 logits, 1024 features: 1935 us, turned 2025), but their stores to rows a power of two
+// apart meet on the same channels (dz there: 2440 us, turned 2190).
+constexpr int kPanel = 4;
 
 struct GridWalk {
-    int R, C, tm;
+    int R, C, tm, tallest;
     int64_t rows;
-    uint32_t j, step, end;
+    uint32_t j, step, end;       // the next tile in the XCD's own order, the way to the one after, its tiles
+    uint32_t first, turn;        // the XCD's first tile, and where in its run it begins
 
     // `block`: this workgroup's number among those of the grid.
-    __device__ __forceinline__ void start(int64_t n, int rows_a_tile, int col_tiles, int slices, uint32_t block)
+    __device__ __forceinline__ void start(int64_t n, int rows_a_tile, int col_tiles, int slices, uint32_t block, int panel, bool turned)
     {
+        tallest = panel;
         rows = n;
         tm = rows_a_tile;
         R = (int)((n + tm - 1) / tm);
         C = col_tiles;
         const int64_t all = (int64_t)R * C * slices;
         const uint32_t xcd = block & 7;
-        j = (uint32_t)(all * xcd / 8) + (block >> 3);
-        end = (uint32_t)(all * (xcd + 1) / 8);
+        first = (uint32_t)(all * xcd / 8);
+        end = (uint32_t)(all * (xcd + 1) / 8) - first;
+        turn = turned ? (uint32_t)((uint64_t)end * xcd / 8) : 0;
+        j = block >> 3;
         step = gridDim.x >> 3;
     }
     __device__ __forceinline__ bool next(Span &s)
     {
         if (j >= end) return false;
         const uint32_t one = (uint32_t)R * (uint32_t)C;
-        const uint32_t slice = j / one, u = j % one;
+        const uint32_t at = first + (j + turn < end ? j + turn : j + turn - end);
+        const uint32_t slice = at / one, u = at % one;
         j = end - j > step ? j + step : end;
-        const uint32_t panel = u / (uint32_t)(kPanel * C), w = u % (uint32_t)(kPanel * C);
-        const int left = R - (int)panel * kPanel, tall = left < kPanel ? left : kPanel;
-        s.g = (int)panel * kPanel + (int)(w % (uint32_t)tall);          // row tile
+        const uint32_t panel = u / (uint32_t)(tallest * C), w = u % (uint32_t)(tallest * C);
+        const int left = R - (int)panel * tallest, tall = left < tallest ? left : tallest;
+        s.g = (int)panel * tallest + (int)(w % (uint32_t)tall);          // row tile
         s.tile = (int)(w / (uint32_t)tall);
         s.slot = (int)slice;
         s.lo = (int64_t)s.g * tm;
@@ -208,6 +216,15 @@ __device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, M
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// The pitch of rows of `cols` 16-bit elements: an odd number of 256 bytes, so that the rows of a tile start on
+// different channels of the memory.  (4096 rows, 30% of them padded, 40943 x 512
+// fp16: dz 177 us, so 172; the products 271 and 261.)
+inline int64_t odd_pitch(int64_t cols)
+{
+    const int64_t lines = (cols + 127) / 128;
+    return (lines | 1) * 128;
 }
 
 // Launches a kernel of resident workgroups over at most `all` tiles.

@@ -66,14 +66,14 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     GridWalk walk;
     if (a.dX) {
         const int slices = a.head->slices;
-        const int per = ((a.pitch + slices - 1) / slices + kX - 1) / kX * kX;
-        walk.start(live, TM, a.tiles_c, slices, block);
+        const int cols = (a.width + 7) / 8 * 8, per = ((cols + slices - 1) / slices + kX - 1) / kX * kX;
+        walk.start(live, TM, a.tiles_c, slices, block, kPanel, false);
         block = (uint32_t)((block + gridDim.x - (((uint32_t)(walk.R * walk.C) * (uint32_t)slices + 7) / 8 * 8) % gridDim.x) % gridDim.x);
         RowOperand<T, TM, N, kDirect> A;
         ColOperand<T, TN, N, SRCB, false> B;
         const auto open = [&](const Span &s) {
-            const int x0 = s.slot * per < a.pitch ? s.slot * per : a.pitch;
-            const int wide = a.pitch - x0 < per ? a.pitch - x0 : per;
+            const int x0 = s.slot * per < cols ? s.slot * per : cols;
+            const int wide = cols - x0 < per ? cols - x0 : per;
             const int real = a.width - x0 < wide ? a.width - x0 : wide;
             A.open(static_cast<const T *>(a.dz) + s.lo * a.pitch + x0, nullptr, s.have, a.pitch, 0);
             A.width = wide;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     }
     if (a.dW) {
         const float unscale = a.head->unscale;
-        walk.start(a.width, TM, a.tiles_w, 1, block);
+        walk.start(a.width, TM, a.tiles_w, 1, block, kPanel, false);
         ColOperand<T, TM, N, kDirect, false> A;
         ColOperand<T, TN, N, kDirect, false> B;
         const auto open = [&](const Span &s) {
@@ -232,7 +232,7 @@ int32_t most_slices(int64_t n, int32_t width, int32_t k)
 size_t lay_backward(VocabArgs &a, char *ws)
 {
     a.width = piece_width(a.n, a.V);
-    a.pitch = (a.width + 7) / 8 * 8;
+    a.pitch = (int32_t)odd_pitch(a.width);
     a.plan.most = most_slices(a.n, a.width, a.k);
     a.row_tiles = (int32_t)((a.n + 127) / 128 * 2);
     const size_t n = (size_t)a.n;
@@ -290,7 +290,6 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
     for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
         a.v0 = (int32_t)v0;
         a.width = (int32_t)(a.V - v0 < piece ? a.V - v0 : piece);
-        a.pitch = (a.width + 7) / 8 * 8;
         a.first = v0 == 0;
         if (a.n > 0) {
             COGDL_TRY(vocab_logits_launch(a, dtype, true, wide_logits, stream));
