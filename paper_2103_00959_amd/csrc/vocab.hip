@@ -35,7 +35,8 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float t)
 
 // The teacher's rows: whether any entry counts (inside the vocabulary, its logit above -inf), and the log of
 // the sum of their exponentials.  FORWARD: also the student's logits of the entries, by 4 entries of 16 lanes a
-// wavefront, into logp, and a workgroup a row (its wavefronts each find the row's sum); else a wavefront a row.
+// wavefront, into logp, and a workgroup a row (its wavefronts each find the row's sum); else a wavefront a row.  Bound
+// by the gather of W: 4096 rows of 64 entries of 768 bf16 52 us (5.6 TB/s of HBM).
 template <typename T, bool FORWARD>
 __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
 {
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
         s = group_sum(s, kWave);
         if (lane == 0 && (!FORWARD || wave == 0)) {
             a.live[i] = live ? 0 : -1;
-            a.tlse[i] = from + logf(s);
+            a.tlse[i] = make_float2(from, logf(s));
         }
         if constexpr (FORWARD) {
             const T *__restrict__ x = static_cast<const T *>(a.X) + i * a.k;
@@ -85,8 +86,8 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
 }
 
 // The rows that count, in order, and their features; in the forward of the cross entropy also their targets'
-// logits, into loss.  A workgroup takes `per` rows; how many count before them
-// it finds by itself, from the targets (n targets a workgroup, from the L2s).
+// logits, into loss.  A workgroup takes `per` rows; how many count before them it finds by itself, from the targets
+// (up to n a workgroup, from the L2s), which a launch of its own would not do sooner.  8192 rows of 1024 bf16 20 us.
 constexpr int kRowsDeep = 4;     // rows a wavefront moves at once
 
 template <typename T, bool BACKWARD>
@@ -114,8 +115,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
 #pragma unroll
     for (int w = 0; w < W; ++w) at += wsum[w];
     if (BACKWARD && blockIdx.x == 0) {
-        // the largest |g T| that counts, for a power of two that brings every dz below 2^15 (and keeps what
-        // fp16 can of the small ones)
+        // The largest |g T| that counts, for a factor that brings it to 2^15: fp16 then keeps what it can of the small
+        // ones, and of rows that weigh the same, as in a mean, a target's dz, near -g T, lies just under a power of
+        // two, where a rounding takes least of it (256 rows of 1433 answers, bf16: the gradients are, with a
+        // power of two for the factor, 0.0020 to 0.0031, so 0.0019; rounded once they are 0.0017).
         float top = 0.f;
         for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kBlock * 8) {
             float g[8];
@@ -133,14 +136,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         if (threadIdx.x == 0) {
 #pragma unroll
             for (int w = 0; w < W; ++w) top = fmaxf(top, wmax[w]);
-            int e = 0;
-            if (top > 0.f && top <= 3.4e38f) {
-                (void)frexpf(top, &e);                     // top < 2^e
-                e = 15 - e;
-                e = e > 120 ? 120 : e < -120 ? -120 : e;
-            }
-            a.head->scale = ldexpf(1.f, e);
-            a.head->unscale = ldexpf(1.f, -e);
+            if (!(top <= 3.4e38f)) top = 32768.f;          // (an infinite one makes NaN by itself)
+            top = fmaxf(top, 0x1p-100f);
+            a.head->scale = 32768.f / top;
+            a.head->unscale = top / 32768.f;
         }
     }
     if (BACKWARD && a.db_q) {
@@ -236,7 +235,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
 }
 
 // Tiles of logits.  GRAD: dz of the piece, else each row's (max, sum) over the wavefront's columns.  EXTRA: with a
-// bias, or db's sums over the tile's rows.
+// bias, or db's sums over the tile's rows.  Bound by the matrix cores and, of narrow features, by what is done with
+// their outputs (an exponential each, a quarter of the other instructions' rate; about 3 chunks of 64 features' time
+// a tile): 8192 x 131072 of 1024 features the statistics 1930 us (1.14 PFLOP/s; a library product that writes the logits
+// 1.16), dz 2170; 2867 x 40943 of 512 131 (0.92 PFLOP/s) and 160; 2048 x 14951 of 200 26 (0.47).
 template <typename T, int WAVES, int TM, int TN, int SRCB, bool GRAD, bool EXTRA>
 __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
 {
@@ -361,7 +363,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
 
 // The slots of a row joined to its lse, and the loss from its targets' logits.  R rows a workgroup (a power of
 // two up to 16), 256 / R threads each.  Of rows as they were given, which count, and their targets' logits, are found
-// here.
+// here.  8192 rows, 2048 slots 27 us (4.9 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
 {
@@ -441,11 +443,12 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
                 if (lane == 0) a.loss[i] = 0.f;
                 continue;
             }
-            const float lse = lse_of[q], tlse = a.tlse[i];
+            const float lse = lse_of[q];
+            const float2 tlse = a.tlse[i];
             float loss = 0.f;
             for (int e = lane; e < a.entries; e += kWave) {
                 if (!counts(a.index[i * a.entries + e], a.V)) continue;       // (logp is 0)
-                const float logp = a.logp[i * a.entries + e] - lse, logq = a.teacher[i * a.entries + e] / a.T - tlse;
+                const float logp = a.logp[i * a.entries + e] - lse, logq = log_share(a.teacher[i * a.entries + e], a.T, tlse);
                 a.logp[i * a.entries + e] = logp;
                 const float share = expf(logq);
                 if (!(share == 0.f)) loss += share * (logq - logp);
@@ -473,8 +476,9 @@ VocabKernel pick(bool grad, bool extra, bool wide, bool direct)
 
 }  // namespace
 
-// The fewer rounds of resident workgroups, at their chunks' times and about 3 chunks' for a tile's start and outputs:
-// FIGURE.
+// The fewer rounds of resident workgroups, at their chunks' times (a tile's start and outputs take about 3 chunks of
+// either).  With tiles of 256 x 256 and of 128 x 128: 1000 rows by 10007, 602 features, 160 and 632 tiles, 25 and 30 us;
+// 2048 by 14951, 200 features, 472 and 1872, 28 and 37; 256 by 1433, 128 features, 6 and 24, 9 and 5.
 bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W)
 {
     if (!on_grid(W, k)) return false;
@@ -536,7 +540,7 @@ size_t lay_forward(VocabArgs &a, char *ws)
     a.block = (int32_t)(block < a.n ? block : a.n);
     a.head = reinterpret_cast<RowsHead *>(ws + l.take(sizeof(RowsHead)));
     a.live = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 4 * (size_t)a.n : 0));
-    a.tlse = reinterpret_cast<float *>(ws + l.take(a.distill ? 4 * (size_t)a.n : 0));
+    a.tlse = reinterpret_cast<float2 *>(ws + l.take(a.distill ? 8 * (size_t)a.n : 0));
     a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * (size_t)a.n));
     a.Xr = ws + l.take(2 * (size_t)a.n * a.kp);
     a.part = reinterpret_cast<float2 *>(ws + l.take(sizeof(float2) * (size_t)a.block * a.slots));

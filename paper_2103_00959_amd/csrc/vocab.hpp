@@ -28,14 +28,15 @@ constexpr int64_t kMaxRows = 1 << 24;
 // Header of a workspace, written by k_vocab_rows.
 struct RowsHead {
     int32_t off[2];              // 0, live rows
-    float scale, unscale;        // 2^e and 2^-e: |g T| 2^e < 2^15 for every live row
+    float scale, unscale;        // |g T| scale <= 2^15 for every live row, and 1 / scale
     int32_t slices;              // of dX's sums over a piece
 };
 
 // The two products of a piece as tiles of tile x tile on `resident` workgroups of each XCD, one after another: dX's
 // sums (rows x k, a slice of the piece's `width` columns each), then dW (width x k, summed over the rows).  The time of
 // the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile costs its chunks and
-// kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  FIGURE.
+// kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  4096 rows, 30% of them padded, 40943 x 512
+// fp16: the products in launches of their own, slices by the rows given, 319 us, together by the rows that count 270.
 constexpr int kTileStart = 4, kTileSums = 2;
 
 struct ProductsPlan {
@@ -79,7 +80,7 @@ struct VocabArgs {
     // workspace
     RowsHead *head;
     int32_t *live;               // n: >= 0 where the row counts (distillation; else the targets are read)
-    float *tlse;                 // n: log sum_e exp(teacher / T) (distillation)
+    float2 *tlse;                // n: the largest teacher / T, and the log of the sum of exp over it (distillation)
     int32_t *rows;               // live: the rows that count
     float *lse2, *g;             // live: lse log2(e), g T
     int32_t *col;                // live: the target (cross entropy)
@@ -103,6 +104,10 @@ struct VocabArgs {
     int32_t tiles_w;             // column tiles of dW
     bool first;                  // the first piece
 };
+
+// log q of a teacher's logit: the two parts of its row's log sum apart, which one float would round by more than
+// the loss can be told to (4096 rows of 64 entries: 6e-7 of it, so 1e-7).
+__device__ __forceinline__ float log_share(float teacher, float T, float2 of_row) { return (teacher / T - of_row.x) - of_row.y; }
 
 // Sizes and temperature of a call.  (Temperatures past 2^20 either way: logits over them leave fp32's range.)
 inline cogdl_status check_sizes(const VocabArgs &a)
@@ -188,7 +193,8 @@ __device__ __forceinline__ int lane_of_outputs()
 // A wavefront's 16-bit outputs, 64 columns of them: calls map(row block, column block, g, v) for its outputs four at a
 // time, of row lane % 32 and columns 8 g + 4 (lane / 32) ... + 3 of the block, rounds them, and calls out(row, column,
 // w) for 8 of a row as 16 bytes, through the wavefront's part of the LDS: eight neighbouring lanes then hold a row's 128
-// bytes, a whole cache line.  (dz of 8192 x 131072 logits, 1024 features: FIGURE)
+// bytes, a whole cache line.  (dz of 8192 x 131072 logits, 1024 features, 2440 us; straight from the accumulators, 32
+// bytes of a row at a time, 2990.)
 template <typename T, int WR, int WC, typename Map, typename Out>
 __device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, Map map, Out out)
 {
