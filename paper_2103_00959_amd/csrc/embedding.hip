@@ -482,8 +482,8 @@ struct Scatter {
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
 // The sorted list's pieces: all of them at once on the chip, 16 tokens or more, and no more than the join takes in a
-// few us.  With 3072, 4608, 6144 and 8192 wavefronts of pieces: 1M rows of 512 bytes 161, 140, 133 and 154 us, the
-// join 12, 17, 19 and 25; 262144 rows of 600, added, 129, 111, 142 and 116.
+// few us.  With 4608 wavefronts of pieces 1M rows of 512 bytes take 140 us and their join 17, 262144 rows of 600, added,
+// 111; with a third less 161, 12 and 129, with a third more 133, 19 and 142, with 8192 154, 25 and 116.
 int32_t piece_of(int64_t n, int32_t vecs)
 {
     const int lanes = vecs >= kWave ? kWave : next_pow2(vecs);

@@ -33,22 +33,23 @@ struct RowsHead {
 };
 
 // The two products of a piece as tiles of tile x tile on `resident` workgroups of each XCD, one after another: dX's
-// sums (rows x k, a slice of the piece's `width` columns each), then dW (width x k, summed over the rows).  The time of
+// sums (rows x k, a slice of the piece's `width` columns each), then dW (width x k, summed over the rows, a part of
+// `parts` each).  The time of
 // the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile costs its chunks and
 // kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  4096 rows, 30% of them padded, 40943 x 512
 // fp16: the products in launches of their own, slices by the rows given, 319 us, together by the rows that count 270.
 constexpr int kTileStart = 4, kTileSums = 2;
 
 struct ProductsPlan {
-    int32_t tile, resident, width, k, most;
+    int32_t tile, resident, width, k, most, parts;
     bool dx, dw;
 
     // (in floats: sizes are far apart, and no whole number has to come out)
     __host__ __device__ __forceinline__ float cost(int32_t live, int32_t s) const
     {
         const float tr = (float)((live + tile - 1) / tile), tk = (float)((k + tile - 1) / tile), tw = (float)((width + tile - 1) / tile);
-        const float n1 = dx ? ceilf(tr * tk * s * 0.125f) : 0.f, n2 = dw ? ceilf(tw * tk * 0.125f) : 0.f, each = 1.f / resident;
-        const float c1 = ceilf((float)width / (64.f * s)) + kTileStart + kTileSums, c2 = (live + 63) / 64 + kTileStart;
+        const float n1 = dx ? ceilf(tr * tk * s * 0.125f) : 0.f, n2 = dw ? ceilf(tw * tk * parts * 0.125f) : 0.f, each = 1.f / resident;
+        const float c1 = ceilf((float)width / (64.f * s)) + kTileStart + kTileSums, c2 = ceilf((float)live / (64.f * parts)) + kTileStart;
         // workgroup w of the XCD has the tiles w, w + resident, ... of n1 + n2: the most of it at the first, and at
         // the first that begins with dW
         float most_of = 0.f;
@@ -102,7 +103,9 @@ struct VocabArgs {
     int32_t pitch;               // of dz
     int32_t tiles_c;             // column tiles of the logits, of dX's sums
     int32_t tiles_w;             // column tiles of dW
+    float *dw_part;              // [part][piece's width][kp] (more than one part)
     bool first;                  // the first piece
+    bool direct;                 // dX leaves the products as it is: one piece, one slice
 };
 
 // log q of a teacher's logit: the two parts of its row's log sum apart, which one float would round by more than

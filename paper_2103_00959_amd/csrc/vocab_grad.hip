@@ -47,6 +47,20 @@ __global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
     }
 }
 
+// Those of 8 packed outputs from column c on that lie below width.
+template <typename T>
+__device__ __forceinline__ void store_packed(T *__restrict__ row, int c, int width, uint4 w)
+{
+    if (c + 8 <= width) {
+        *reinterpret_cast<u32x4_u *>(row + c) = u32x4_u{w.x, w.y, w.z, w.w};
+        return;
+    }
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < width) row[c + e].bits = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+}
+
 // Both products of a piece, each workgroup's tiles of dX's sums (rows by k, a slice of the piece's columns each),
 // then its tiles of dW (vocabulary by k, over the live rows): workgroups that have no tile of the first begin with
 // the second.  Bound by the matrix cores: 8192 rows, vocabulary 131072, 1024 features 3810 us in four pieces (1.15
@@ -87,6 +101,21 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
             lds, walk, A, B, r0, c0, open, busy, [](const Span &, const uint4 (&)[WR]) {}, nothing,
             [&](const Span &s, const Acc<WR, WC> &acc) {
                 const int col0 = s.tile * TN + c0;
+                if (a.direct) {
+                    const float unscale = a.head->unscale;
+                    for_rows16<T, WR, WC>(
+                        mine, acc,
+                        [&](int, int, int, float (&v)[4]) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] *= unscale;
+                        },
+                        [&](int r, int c, uint4 w) {
+                            r += r0;
+                            c += col0;
+                            if (r < s.have && c < a.k) store_packed(static_cast<T *>(a.dX) + a.rows[s.lo + r] * (int64_t)a.k, c, a.k, w);
+                        });
+                    return;
+                }
                 float *__restrict__ part = a.dx_part + (s.slot * a.n + s.lo) * a.kp;
                 for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
                     r += r0;
@@ -107,18 +136,29 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     }
     if (a.dW) {
         const float unscale = a.head->unscale;
-        walk.start(a.width, TM, a.tiles_w, 1, block, kPanel, false);
+        const int parts = a.plan.parts, per = ((live + parts - 1) / parts + kX - 1) / kX * kX;
+        walk.start(a.width, TM, a.tiles_w, parts, block, kPanel, false);
         ColOperand<T, TM, N, kDirect, false> A;
         ColOperand<T, TN, N, kDirect, false> B;
         const auto open = [&](const Span &s) {
-            A.open(static_cast<const T *>(a.dz), nullptr, nullptr, nullptr, (int)s.lo, a.pitch, live, 0, false);
-            B.open(static_cast<const T *>(a.Xr), nullptr, nullptr, nullptr, s.tile * TN, a.kp, live, 0, false);
-            return live;
+            const int x0 = s.slot * per < live ? s.slot * per : live, rows = live - x0 < per ? live - x0 : per;
+            A.open(static_cast<const T *>(a.dz) + (int64_t)x0 * a.pitch, nullptr, nullptr, nullptr, (int)s.lo, a.pitch, rows, 0, false);
+            B.open(static_cast<const T *>(a.Xr) + (int64_t)x0 * a.kp, nullptr, nullptr, nullptr, s.tile * TN, a.kp, rows, 0, false);
+            return rows;
         };
         run_tiles<T, decltype(A), decltype(B), WR, WC>(
             lds, walk, A, B, r0, c0, open, busy, [](const Span &, const uint4 (&)[WR]) {}, nothing,
             [&](const Span &s, const Acc<WR, WC> &acc) {
                 const int col0 = s.tile * TN + c0;
+                if (parts > 1) {
+                    float *__restrict__ part = a.dw_part + ((int64_t)s.slot * a.plan.width + s.lo) * a.kp;
+                    for_outputs<WR, WC>(mine, acc, [&](int, int r, int c, float (&v)[8]) {
+                        r += r0;
+                        c += col0;
+                        if (r < s.have && c < a.kp) store_vec<float, 8>(part + (int64_t)r * a.kp, c, v);
+                    });
+                    return;
+                }
                 T *__restrict__ dW = static_cast<T *>(a.dW) + (a.v0 + s.lo) * a.k;
                 for_rows16<T, WR, WC>(
                     mine, acc,
@@ -129,28 +169,48 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
                     [&](int r, int c, uint4 w) {
                         r += r0;
                         c += col0;
-                        if (r >= s.have || c >= a.k) return;
-                        T *__restrict__ to = dW + (int64_t)r * a.k + c;
-                        if (c + 8 <= a.k) {
-                            *reinterpret_cast<u32x4_u *>(to) = u32x4_u{w.x, w.y, w.z, w.w};
-                        } else {
-                            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (c + e < a.k) to[e].bits = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
-                        }
+                        if (r < s.have && c < a.k) store_packed(dW + (int64_t)r * a.k, c, a.k, w);
                     });
             });
     }
 }
 
-// The piece's db from the row tiles' sums and the entries' part (workgroups from `dx_blocks` on), and, behind the last
-// piece, dX of the live rows from their slices' sums.  Bound by memory: 8192 x 1024 of two slices 20 us (4.3 TB/s).
+// 8 values' sums over slots, `stride` floats apart.
+__device__ __forceinline__ void sum_slots(const float *__restrict__ from, int64_t stride, int slots, float unscale, float (&t)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < slots; ++s) {
+        float w[2][4];
+        load_vec<float, 4>(from, s * stride, w[0]);
+        load_vec<float, 4>(from, s * stride + 4, w[1]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] += w[e / 4][e % 4];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] *= unscale;
+}
+
+// The piece's db from the row tiles' sums and the entries' part (`db_blocks` workgroups from `dx_blocks` on), its dW from
+// its parts' sums (those behind), and, with the last piece, dX of the live rows from their slices' sums.  Bound by memory: 8192 x 1024 of two slices 20 us (4.3 TB/s).
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int rows_a_part)
+__global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int db_blocks, int rows_a_part)
 {
     const int64_t live = a.head->off[1];
     const float unscale = a.head->unscale;
+    if ((int)blockIdx.x >= dx_blocks + db_blocks) {
+        const int vecs = a.kp / 8;
+        const int64_t all = (int64_t)a.width * vecs, from = (int64_t)(blockIdx.x - dx_blocks - db_blocks) * kBlock + threadIdx.x;
+        for (int64_t u = from; u < all; u += (int64_t)(gridDim.x - dx_blocks - db_blocks) * kBlock) {
+            const int64_t r = u / vecs;
+            const int c = (int)(u % vecs) * 8;
+            float t[8];
+            sum_slots(a.dw_part + r * a.kp + c, (int64_t)a.plan.width * a.kp, a.plan.parts, unscale, t);
+            store8(static_cast<T *>(a.dW) + (a.v0 + r) * a.k, c, a.k, t);
+        }
+        return;
+    }
     if ((int)blockIdx.x >= dx_blocks) {
         const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
         const int c = (int)(blockIdx.x - dx_blocks) * kBlock + (int)threadIdx.x;
@@ -167,18 +227,8 @@ __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks
     for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < all; u += (int64_t)dx_blocks * kBlock) {
         const int64_t p = u / vecs;
         const int c = (int)(u % vecs) * 8;
-        float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int s = 0; s < slices; ++s) {
-            float w[2][4];
-            const float *__restrict__ from = a.dx_part + (s * a.n + p) * a.kp + c;
-            load_vec<float, 4>(from, 0, w[0]);
-            load_vec<float, 4>(from, 4, w[1]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] += w[e / 4][e % 4];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] *= unscale;
+        float t[8];
+        sum_slots(a.dx_part + p * a.kp + c, a.n * a.kp, slices, unscale, t);
         store8(static_cast<T *>(a.dX) + a.rows[p] * (int64_t)a.k, c, a.k, t);
     }
 }
@@ -196,9 +246,20 @@ int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1
 // 8192 rows, vocabulary 131072, 1024 features 8440, 8420 and 8305 us; 4096 rows, 65536 x 768, 1800, 1727 and 1719.
 constexpr int64_t kPieceBytes = 512ll << 20;
 
+// Parts of the rows that dW of a piece is summed in: many rows and few classes make few tiles, each a sum over all
+// rows.  As many as the chip holds tiles, of 1024 rows or more.  FIGURE
+int32_t dw_parts(int64_t n, int32_t width, int32_t k, int tile)
+{
+    const int64_t tiles = tiles_of(width, k, tile), want = tile == 256 ? 256 : 512;
+    int64_t parts = tiles > 0 ? want / tiles : 1;
+    if (parts > n / 1024) parts = n / 1024;
+    return (int32_t)(parts < 1 ? 1 : parts);
+}
+
 // The plan of a piece's products with tiles of 256 x 256 or of 128 x 128, whichever ends first.
 void plan_products(ProductsPlan &p, int64_t n, const void *W)
 {
+    p.parts = 1;
     float best[2];
     for (int wide = 0; wide < 2; ++wide) {
         p.tile = wide ? 256 : 128;
@@ -209,6 +270,7 @@ void plan_products(ProductsPlan &p, int64_t n, const void *W)
     const bool wide = on_grid(W, p.k) && p.k > 128 && best[1] * kWideChunk < best[0] * kNarrowChunks;
     p.tile = wide ? 256 : 128;
     p.resident = wide ? 32 : 64;
+    if (p.dw) p.parts = dw_parts(n, p.width, p.k, p.tile);
 }
 
 int32_t piece_width(int64_t n, int32_t V)
@@ -249,7 +311,11 @@ size_t lay_backward(VocabArgs &a, char *ws)
     a.at_col = reinterpret_cast<float *>(ws + l.take(a.distill ? 0 : 4 * n));
     a.Xr = ws + l.take(2 * n * a.kp);
     a.dz = ws + l.take(2 * n * a.pitch);
-    a.dx_part = reinterpret_cast<float *>(ws + l.take(4 * n * a.kp * a.plan.most));
+    a.direct = a.width == a.V && a.plan.most == 1;
+    a.dx_part = reinterpret_cast<float *>(ws + l.take(a.direct ? 0 : 4 * n * a.kp * a.plan.most));
+    const int32_t small = dw_parts(a.n, a.width, a.k, 128), large = dw_parts(a.n, a.width, a.k, 256);
+    const int32_t parts = small > large ? small : large;           // (which tiles, W's alignment decides)
+    a.dw_part = reinterpret_cast<float *>(ws + l.take(parts > 1 ? 4 * (size_t)parts * a.width * a.kp : 0));
     a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.pitch));
     a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(a.distill ? 8 * (size_t)a.V : 0));
     return l.total;
@@ -304,17 +370,20 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
         }
         if (a.dX || a.dW) {
             a.tiles_c = a.tiles_w = (a.k + tile - 1) / tile;
-            const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) : 0);
+            const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) * a.plan.parts : 0);
             COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
                                    a, tiles, waves, lds_of(waves, tile, tile), stream));
         }
         const bool last = a.V - v0 <= piece;
-        int64_t dx_blocks = a.dX && last ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
+        int64_t dx_blocks = a.dX && last && !a.direct ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
         if (dx_blocks > 4096) dx_blocks = 4096;
-        const unsigned grid = (unsigned)(dx_blocks + (a.db ? (a.width + kBlock - 1) / kBlock : 0));
+        const int db_blocks = a.db ? (a.width + kBlock - 1) / kBlock : 0;
+        int64_t dw_blocks = a.dW && a.plan.parts > 1 ? ((int64_t)a.width * (a.kp / 8) + kBlock - 1) / kBlock : 0;
+        if (dw_blocks > 4096) dw_blocks = 4096;
+        const unsigned grid = (unsigned)(dx_blocks + db_blocks + dw_blocks);
         if (grid == 0) continue;
-        if (bf16) COGDL_LAUNCH("vocab_out", k_vocab_out<bf16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
-        else COGDL_LAUNCH("vocab_out", k_vocab_out<f16_t>, grid, kBlock, stream, a, (int)dx_blocks, wide_logits ? 128 : 64);
+        if (bf16) COGDL_LAUNCH("vocab_out", k_vocab_out<bf16_t>, grid, kBlock, stream, a, (int)dx_blocks, db_blocks, wide_logits ? 128 : 64);
+        else COGDL_LAUNCH("vocab_out", k_vocab_out<f16_t>, grid, kBlock, stream, a, (int)dx_blocks, db_blocks, wide_logits ? 128 : 64);
     }
     return COGDL_OK;
 }

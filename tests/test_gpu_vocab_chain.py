@@ -222,10 +222,12 @@ def one_hot(t, V):
 
 @pytest.mark.parametrize("n,V,k,dt", [(8192, 70001, 24, torch.bfloat16), (8100, 66000, 18, torch.float16),
                                       (2560, 4096, 264, torch.bfloat16), (1024, 20000, 1024, torch.float16),
-                                      (3000, 9000, 515, torch.bfloat16)])
+                                      (3000, 9000, 515, torch.bfloat16), (30000, 41, 48, torch.bfloat16),
+                                      (150_000, 3, 130, torch.float16), (70_000, 200, 260, torch.bfloat16)])
 def test_several_pieces_and_wide_tiles(n, V, k, dt):
-    """Vocabularies in pieces with a short last one, tiles of 256 x 256 and of 128 x 128, odd widths; with and without
-    the bias and its gradient (kernels of their own)."""
+    """Vocabularies in pieces with a short last one, tiles of 256 x 256 and of 128 x 128, odd widths, many rows over a
+    few classes (dW in parts of the rows, dX without slices); with and without the bias and its gradient (kernels of
+    their own)."""
     X, W, t, b, g = random_layer(n, V, k, dt, n + V)
     for bias in (b, None):
         loss, lse = cg.linear_cross_entropy(X, W, t, bias)
