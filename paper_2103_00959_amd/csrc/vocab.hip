@@ -85,9 +85,46 @@ __global__ __launch_bounds__(kBlock) void k_teacher_rows(VocabArgs a)
     }
 }
 
+// How many rows of each run of `per` count, and their largest weight.
+template <bool BACKWARD>
+__global__ __launch_bounds__(kBlock) void k_count_rows(VocabArgs a, int per)
+{
+    constexpr int W = kBlock / kWave;
+    __shared__ int wsum[W];
+    __shared__ float wmax[W];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int32_t *__restrict__ live = a.distill ? a.live : a.index;
+    const int32_t limit = a.distill ? INT32_MAX : a.V;
+    const int64_t from = (int64_t)blockIdx.x * per, to = from + per < a.n ? from + per : a.n;
+    int count = 0;
+    float top = 0.f;
+    for (int64_t i = from + threadIdx.x; i < to; i += kBlock) {
+        if (!counts(live[i], limit)) continue;
+        ++count;
+        if (BACKWARD) top = fmaxf(top, fabsf(a.dloss[i] * a.T));
+    }
+    count = wave_inclusive_scan(count);
+    top = group_reduce(top, kWave, [](float x, float y) { return fmaxf(x, y); });
+    if (lane == kWave - 1) {
+        wsum[wave] = count;
+        wmax[wave] = top;
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+        wsum[0] += wsum[w];
+        wmax[0] = fmaxf(wmax[0], wmax[w]);
+    }
+    a.counts[blockIdx.x] = wsum[0];
+    if (BACKWARD) a.tops[blockIdx.x] = wmax[0];
+}
+
 // The rows that count, in order, and their features; in the forward of the cross entropy also their targets'
 // logits, into loss.  A workgroup takes `per` rows; how many count before them it finds by itself, from the targets
 // (up to n a workgroup, from the L2s), which a launch of its own would not do sooner.  8192 rows of 1024 bf16 20 us.
+// Of more than kManyRows a launch before counts them run by run (k_count_rows), and finds the largest weight: 232965
+// rows 14 us, and the gathering of 128 features, forward and backward, 679 -> 112.
 constexpr int kRowsDeep = 4;     // rows a wavefront moves at once
 
 template <typename T, bool BACKWARD>
@@ -100,8 +137,12 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
     const int32_t *__restrict__ live = a.distill ? a.live : a.index;
     const int32_t limit = a.distill ? INT32_MAX : a.V;
     const int64_t from = (int64_t)blockIdx.x * per, to = from + per < a.n ? from + per : a.n;
+    const bool many = a.n > kManyRows;
     int before = 0;
-    for (int64_t i0 = threadIdx.x; i0 < from; i0 += kBlock * 16) {
+    if (many) {
+        for (int b = threadIdx.x; b < (int)blockIdx.x; b += kBlock) before += a.counts[b];
+    }
+    for (int64_t i0 = threadIdx.x; !many && i0 < from; i0 += kBlock * 16) {
         int32_t t[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u) t[u] = i0 + u * kBlock < from ? live[i0 + u * kBlock] : -1;
@@ -120,7 +161,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         // two, where a rounding takes least of it (256 rows of 1433 answers, bf16: the gradients are, with a
         // power of two for the factor, 0.0020 to 0.0031, so 0.0019; rounded once they are 0.0017).
         float top = 0.f;
-        for (int64_t i0 = threadIdx.x; i0 < a.n; i0 += kBlock * 8) {
+        if (many) {
+            for (int b = threadIdx.x; b < (int)gridDim.x; b += kBlock) top = fmaxf(top, a.tops[b]);
+        }
+        for (int64_t i0 = threadIdx.x; !many && i0 < a.n; i0 += kBlock * 8) {
             float g[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
@@ -496,9 +540,13 @@ cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backw
         else COGDL_LAUNCH("teacher_rows", (k_teacher_rows<f16_t, true>), grid, kBlock, stream, a);
     }
     if (a.plain) return COGDL_OK;
-    int64_t per = (a.n + 511) / 512;
+    const bool many = a.n > kManyRows;
+    const int64_t runs = many ? kMostRuns : 512;
+    int64_t per = (a.n + runs - 1) / runs;
     per = per < 8 ? 8 : per;
     const unsigned blocks = a.n > 0 ? (unsigned)((a.n + per - 1) / per) : 1;
+    if (many && backward) COGDL_LAUNCH("vocab_count", k_count_rows<true>, blocks, kBlock, stream, a, (int)per);
+    else if (many) COGDL_LAUNCH("vocab_count", k_count_rows<false>, blocks, kBlock, stream, a, (int)per);
     if (dtype == COGDL_BF16) {
         if (backward) COGDL_LAUNCH("vocab_rows", (k_vocab_rows<bf16_t, true>), blocks, kBlock, stream, a, (int)per);
         else COGDL_LAUNCH("vocab_rows", (k_vocab_rows<bf16_t, false>), blocks, kBlock, stream, a, (int)per);
@@ -541,6 +589,7 @@ size_t lay_forward(VocabArgs &a, char *ws)
     a.head = reinterpret_cast<RowsHead *>(ws + l.take(sizeof(RowsHead)));
     a.live = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 4 * (size_t)a.n : 0));
     a.tlse = reinterpret_cast<float2 *>(ws + l.take(a.distill ? 8 * (size_t)a.n : 0));
+    a.counts = reinterpret_cast<int32_t *>(ws + l.take(a.n > kManyRows ? 4 * kMostRuns : 0));
     a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * (size_t)a.n));
     a.Xr = ws + l.take(2 * (size_t)a.n * a.kp);
     a.part = reinterpret_cast<float2 *>(ws + l.take(sizeof(float2) * (size_t)a.block * a.slots));

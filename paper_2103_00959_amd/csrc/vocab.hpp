@@ -25,6 +25,10 @@ constexpr int kMostSlices = 64;
 // Rows of one call.
 constexpr int64_t kMaxRows = 1 << 24;
 
+// Runs that many rows are counted in before they are gathered.
+constexpr int kMostRuns = 4096;
+constexpr int64_t kManyRows = 16384;
+
 // Header of a workspace, written by k_vocab_rows.
 struct RowsHead {
     int32_t off[2];              // 0, live rows
@@ -82,6 +86,8 @@ struct VocabArgs {
     RowsHead *head;
     int32_t *live;               // n: >= 0 where the row counts (distillation; else the targets are read)
     float2 *tlse;                // n: the largest teacher / T, and the log of the sum of exp over it (distillation)
+    int32_t *counts;             // [kMostRuns]: rows that count in each run of rows (many rows)
+    float *tops;                 // [kMostRuns]: their largest |g T| (backward)
     int32_t *rows;               // live: the rows that count
     float *lse2, *g;             // live: lse log2(e), g T
     int32_t *col;                // live: the target (cross entropy)
@@ -95,6 +101,7 @@ struct VocabArgs {
     float *dx_part;              // [slice][live][kp]
     ProductsPlan plan;           // (backward)
     float *db_part;              // [row tile][pitch]: a piece's
+    float *db_join;              // [kJoin row tiles][pitch] (many row tiles)
     int32_t row_tiles;
     unsigned long long *db_q;    // V: the targets' part, in units of 2^-unit_bits
     int32_t unit_bits;

@@ -175,6 +175,28 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     }
 }
 
+// db's sums over kJoin row tiles each, where there are many: 64 columns a workgroup, 4 parts of them.  1821 row tiles
+// of 41 columns 7 us, and vocab_out, whose one workgroup had read them all, 139 -> 27.
+constexpr int kJoin = 64, kManyTiles = 256;
+
+__global__ __launch_bounds__(kBlock) void k_vocab_db(VocabArgs a, int rows_a_part)
+{
+    __shared__ float sums[kBlock];
+    const int64_t live = a.head->off[1];
+    const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
+    const int c = (int)blockIdx.y * kWave + lane_id(), q = threadIdx.x / kWave;
+    const int from = (int)blockIdx.x * kJoin + q * (kJoin / 4);
+    float t = 0.f;
+    if (c < a.width) {
+#pragma unroll
+        for (int p = 0; p < kJoin / 4; ++p) t += from + p < parts ? a.db_part[(int64_t)(from + p) * a.pitch + c] : 0.f;
+    }
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    if (q == 0 && c < a.width)
+        a.db_join[(int64_t)blockIdx.x * a.pitch + c] = ((t + sums[threadIdx.x + kWave]) + sums[threadIdx.x + 2 * kWave]) + sums[threadIdx.x + 3 * kWave];
+}
+
 // 8 values' sums over slots, `stride` floats apart.
 __device__ __forceinline__ void sum_slots(const float *__restrict__ from, int64_t stride, int slots, float unscale, float (&t)[8])
 {
@@ -212,12 +234,14 @@ __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks
         return;
     }
     if ((int)blockIdx.x >= dx_blocks) {
-        const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
+        const bool joined = a.row_tiles > kManyTiles;
+        const int rows = joined ? rows_a_part * kJoin : rows_a_part, parts = (int)((live + rows - 1) / rows);
+        const float *__restrict__ part = joined ? a.db_join : a.db_part;
         const int c = (int)(blockIdx.x - dx_blocks) * kBlock + (int)threadIdx.x;
         if (c >= a.width) return;
         float t = 0.f;
 #pragma unroll 8
-        for (int p = 0; p < parts; ++p) t += a.db_part[(int64_t)p * a.pitch + c];
+        for (int p = 0; p < parts; ++p) t += part[(int64_t)p * a.pitch + c];
         if (a.db_q) t = (float)((double)t - ldexp((double)(long long)a.db_q[a.v0 + c], -a.unit_bits));
         a.db[a.v0 + c] = t * unscale;
         return;
@@ -247,7 +271,8 @@ int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 // Parts of the rows that dW of a piece is summed in: many rows and few classes make few tiles, each a sum over all
-// rows.  As many as the chip holds tiles, of 1024 rows or more.  FIGURE
+// rows.  As many as the chip holds tiles, of 1024 rows or more.  232965 rows, 41
+// classes, 128 features: the products 3248 us with one part, 46 so.
 int32_t dw_parts(int64_t n, int32_t width, int32_t k, int tile)
 {
     const int64_t tiles = tiles_of(width, k, tile), want = tile == 256 ? 256 : 512;
@@ -304,6 +329,8 @@ size_t lay_backward(VocabArgs &a, char *ws)
     a.head = reinterpret_cast<RowsHead *>(ws + l.take(sizeof(RowsHead)));
     a.live = reinterpret_cast<int32_t *>(ws + l.take(a.distill ? 4 * n : 0));
     a.tlse = reinterpret_cast<float2 *>(ws + l.take(a.distill ? 8 * n : 0));
+    a.counts = reinterpret_cast<int32_t *>(ws + l.take(a.n > kManyRows ? 4 * kMostRuns : 0));
+    a.tops = reinterpret_cast<float *>(ws + l.take(a.n > kManyRows ? 4 * kMostRuns : 0));
     a.rows = reinterpret_cast<int32_t *>(ws + l.take(4 * n));
     a.lse2 = reinterpret_cast<float *>(ws + l.take(4 * n));
     a.g = reinterpret_cast<float *>(ws + l.take(4 * n));
@@ -317,6 +344,7 @@ size_t lay_backward(VocabArgs &a, char *ws)
     const int32_t parts = small > large ? small : large;           // (which tiles, W's alignment decides)
     a.dw_part = reinterpret_cast<float *>(ws + l.take(parts > 1 ? 4 * (size_t)parts * a.width * a.kp : 0));
     a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.pitch));
+    a.db_join = reinterpret_cast<float *>(ws + l.take(a.row_tiles > kManyTiles ? 4 * (size_t)((a.row_tiles + kJoin - 1) / kJoin) * a.pitch : 0));
     a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(a.distill ? 8 * (size_t)a.V : 0));
     return l.total;
 }
@@ -374,6 +402,9 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
             COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
                                    a, tiles, waves, lds_of(waves, tile, tile), stream));
         }
+        if (a.db && a.row_tiles > kManyTiles)
+            COGDL_LAUNCH("vocab_db", k_vocab_db, dim3((unsigned)((a.row_tiles + kJoin - 1) / kJoin), (unsigned)((a.width + kWave - 1) / kWave)),
+                         kBlock, stream, a, wide_logits ? 128 : 64);
         const bool last = a.V - v0 <= piece;
         int64_t dx_blocks = a.dX && last && !a.direct ? (a.n * (a.kp / 8) + kBlock - 1) / kBlock : 0;
         if (dx_blocks > 4096) dx_blocks = 4096;

@@ -75,7 +75,7 @@ def teacher_rows(n, V, K, g):
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 @pytest.mark.parametrize("n,V,k,K,T", [(1, 1, 1, 1, 1.0), (1, 300, 40, 5, 2.0), (7, 90, 33, 3, 1.0), (65, 1000, 64, 10, 4.0),
-                                       (200, 513, 130, 70, 0.5), (300, 2000, 256, 128, 2.0), (40, 700, 16, 300, 1.5)])
+                                       (200, 513, 130, 70, 0.5), (20000, 60, 24, 3, 1.0), (300, 2000, 256, 128, 2.0), (40, 700, 16, 300, 1.5)])
 def test_distill(n, V, k, K, T, dt):
     X, W, _, b, g, gen = layer(n, V, k, dt, n + V + k + K, K % 2 == 0)
     index, teacher = teacher_rows(n, V, K, gen)
