@@ -84,17 +84,6 @@ __global__ __launch_bounds__(WAVES * kWave) void k_grouped_rows(GroupedArgs a)
 // bf16: 64 workgroups of 128 x 128 tiles took 20 us, these 512 take 6.
 constexpr int kFewRows = 16, kFewCols = 16, kFewSteps = 8, kFewWaves = 4;
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-template <typename T>
-__device__ __forceinline__ f32x4 mfma_16x16x32(uint4 a, uint4 b, f32x4 c)
-{
-    if constexpr (Fmt<T>::code == COGDL_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
 template <typename T>
 __global__ __launch_bounds__(kFewWaves * kWave) void k_grouped_few(GroupedArgs a)
 {

@@ -405,6 +405,81 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
         });
 }
 
+// The statistics of up to 16 rows (single queries), where one tile a wavefront covers W: the reads of W are all there
+// is.  A wavefront owns 16 columns over all features, 8 steps of 32 loaded at once straight into the operands of the
+// 16 x 16 x 32 matrix instructions; the rows lie in LDS.  Lane l holds columns 4 (l / 16) ... + 3 of row l % 16; the
+// (max, sum) of a workgroup's 64 columns are one slot.  In place of 128 x 128 tiles: 1 row, 14541 classes of 512
+// features 7.5 us for 10.6, 8000 of 2048 14 for 27.  Not for more rows or columns: 64 of those rows 12.8 for 10.7, and
+// 1 row, 50257 of 2048 (two tiles a wavefront) 40 for 33.
+constexpr int kFewRows = 16, kFewSteps = 8, kFewWaves = 4;
+
+inline int few_stride(int k) { return (k + 31) / 32 * 32 + 8; }       // of a row in LDS: 16 of them on all banks
+
+template <typename T>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_vocab_few(VocabArgs a, int stride)
+{
+    extern __shared__ __align__(16) char lds[];
+    T *const x = reinterpret_cast<T *>(lds);
+    __shared__ float2 part[kFewWaves][kFewRows];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int i = lane & 15, q = lane >> 4;              // column of W (row of X), its 8 of a step's 32 features
+    const int n = (int)a.n, vecs = (stride - 8) / 8;
+    for (int u = threadIdx.x; u < kFewRows * vecs; u += kFewWaves * kWave) {
+        const int r = u / vecs, v = u % vecs;
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (r < n && 8 * v < a.k) w = load_vec8(static_cast<const T *>(a.X) + (int64_t)r * a.k, v, a.k);
+        *reinterpret_cast<uint4 *>(x + r * stride + 8 * v) = w;
+    }
+    __syncthreads();
+    const int64_t col0 = ((int64_t)blockIdx.x * kFewWaves + wave) * 16;
+    const int cols = (int)(a.V - col0 < 16 ? a.V - col0 > 0 ? a.V - col0 : 0 : 16);
+    const Buffer W = buffer_of(static_cast<const T *>(a.W) + (cols ? col0 : 0) * a.k, (int64_t)cols * a.k * 2);
+    const uint32_t row = (uint32_t)i * (uint32_t)a.k * 2u;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int x0 = 0; x0 < a.k; x0 += 32 * kFewSteps) {
+        uint4 w[kFewSteps];
+#pragma unroll
+        for (int u = 0; u < kFewSteps; ++u) {
+            // pieces at the row's end are read from its last 8 elements, those past it from nowhere
+            const int at = x0 + 32 * u + 8 * q;
+            w[u] = load16(W, at < a.k ? row + (uint32_t)(at + 8 <= a.k ? at : a.k - 8) * 2u : kNowhere);
+        }
+#pragma unroll
+        for (int u = 0; u < kFewSteps; ++u) {
+            if (x0 + 32 * u >= a.k) break;               // (uniform)
+            if (x0 + 32 * u + 32 > a.k) w[u] = shift_down(w[u], x0 + 32 * u + 8 * q + 8 - a.k);
+            acc = mfma_16x16x32<T>(w[u], *reinterpret_cast<const uint4 *>(x + i * stride + x0 + 32 * u + 8 * q), acc);
+        }
+    }
+    float m = -INFINITY, z = 0.f, v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool in = 4 * q + e < cols;
+        v[e] = in ? (acc[e] + (a.bias ? a.bias[col0 + 4 * q + e] : 0.f)) * a.per_z : -INFINITY;
+        m = fmaxf(m, v[e]);
+    }
+    const auto base = [](float top) { return top == -INFINITY ? 0.f : top; };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z += __builtin_amdgcn_exp2f(v[e] - base(m));
+    const auto merge = [&](float m2, float z2) {
+        const float top = fmaxf(m, m2), from = base(top);
+        z = z * __builtin_amdgcn_exp2f(m - from) + z2 * __builtin_amdgcn_exp2f(m2 - from);
+        m = top;
+    };
+    for (int half = 16; half < kWave; half *= 2) {
+        const float m2 = __shfl_xor(m, half), z2 = __shfl_xor(z, half);
+        merge(m2, z2);
+    }
+    if (q == 0) part[wave][i] = make_float2(m, z);
+    __syncthreads();
+    if (wave != 0 || lane >= n) return;
+    m = part[0][lane].x;
+    z = part[0][lane].y;
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) merge(part[w][lane].x, part[w][lane].y);
+    a.part[(int64_t)blockIdx.x * a.block + lane] = make_float2(m, z);
+}
+
 // The slots of a row joined to its lse, and the loss from its targets' logits.  R rows a workgroup (a power of
 // two up to 16), 256 / R threads each.  Of rows as they were given, which count, and their targets' logits, are found
 // here.  8192 rows, 2048 slots 27 us (4.9 TB/s).
@@ -530,6 +605,21 @@ bool vocab_wide(int64_t n, int64_t cols, int32_t k, const void *W)
     return (float)((w + 255) / 256) * kWideChunk < (float)((s + 511) / 512) * (s <= 256 ? kNarrowChunk : kNarrowChunks);
 }
 
+// k_vocab_few where its rule holds.
+template <typename T>
+cogdl_status few_launch(const VocabArgs &a, bool &done, hipStream_t stream)
+{
+    const size_t lds = (size_t)kFewRows * few_stride(a.k) * 2;
+    done = a.plain && on_grid(a.W, a.k) && a.n <= kFewRows && a.k >= 8 && lds <= (156 << 10);
+    if (!done) return COGDL_OK;
+    const int64_t resident = resident_blocks(reinterpret_cast<const void *>(k_vocab_few<T>), kFewWaves * kWave, lds, 0);
+    if (resident < 1) return COGDL_ERR_LAUNCH;
+    done = a.slots <= resident;
+    if (!done) return COGDL_OK;
+    COGDL_LAUNCH_SHM("vocab_few", k_vocab_few<T>, (unsigned)a.slots, kFewWaves * kWave, lds, stream, a, few_stride(a.k));
+    return COGDL_OK;
+}
+
 cogdl_status vocab_rows_launch(const VocabArgs &a, cogdl_dtype dtype, bool backward, hipStream_t stream)
 {
     if (a.distill && a.n > 0) {
@@ -624,7 +714,9 @@ cogdl_status run_forward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_t
     int64_t blocks = (a.block + R - 1) / R;
     if (blocks > 4096) blocks = 4096;
     for (a.p0 = 0; a.p0 < a.n; a.p0 += a.block) {
-        s = vocab_logits_launch(a, dtype, false, wide, stream);
+        bool few = false;
+        s = dtype == COGDL_BF16 ? few_launch<bf16_t>(a, few, stream) : few_launch<f16_t>(a, few, stream);
+        if (s == COGDL_OK && !few) s = vocab_logits_launch(a, dtype, false, wide, stream);
         if (s != COGDL_OK) return s;
         if (dtype == COGDL_BF16) COGDL_LAUNCH("vocab_finish", k_vocab_finish<bf16_t>, (unsigned)blocks, kBlock, stream, a, R);
         else COGDL_LAUNCH("vocab_finish", k_vocab_finish<f16_t>, (unsigned)blocks, kBlock, stream, a, R);

@@ -48,8 +48,9 @@ def check_cross_entropy(X, W, t, b, g):
     return loss, lse, out
 
 
-SIZES = [(1, 1, 1), (1, 2, 8), (1, 500, 64), (2, 3, 7), (5, 129, 65), (33, 64, 16), (64, 1000, 128), (130, 257, 100),
-         (257, 1433, 33), (300, 700, 602), (1000, 41, 256), (128, 5000, 24)]
+SIZES = [(1, 1, 1), (1, 2, 8), (1, 500, 64), (1, 70, 40), (16, 1000, 264), (17, 15, 31), (3, 3000, 4102),
+         (33, 4097, 520), (48, 300, 1030), (64, 17, 9), (2, 3, 7), (5, 129, 65), (33, 64, 16), (64, 1000, 128), (130, 257, 100),
+         (257, 1433, 33), (300, 700, 602), (1000, 41, 256), (128, 5000, 24), (33000, 41, 16)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
