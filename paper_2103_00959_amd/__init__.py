@@ -31,6 +31,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import operator
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -1140,6 +1141,14 @@ def _scratch(workspace, need, like, device):
     return _take(workspace, "workspace", None, device), workspace.numel() * workspace.element_size(), workspace
 
 
+def _i32(size, name):
+    """A size that the C ABI takes in 32 bits."""
+    size = operator.index(size)
+    if size > 2 ** 31 - 1:
+        raise CogdlError(f"{name} is {size}, past 32 bits")
+    return size
+
+
 def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
     """Rows of a table [V, k] (fp32, bf16 or fp16) by an int32 index [n], times ``scale``: Y [n, k] in out_dtype (the
     table's by default).  An index outside [0, V) stands for a padded place: a row of zeros.  A given ``out``
@@ -1148,6 +1157,7 @@ def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
     V, k = _dims(table, "table", 2)
     if V < 1:
         raise CogdlError("table needs at least one row")
+    V, k = _i32(V, "the table's rows"), _i32(k, "the table's width")
     n = _index_array(index, "index")
     _numel(out, "out", n * k)
     device, here = _home(table, "table")
@@ -1156,7 +1166,7 @@ def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
         out = table.new_empty((n, k), dtype=out_dtype or table.dtype)
     po = _take(out, "out", None, device)
     with here:
-        _check(lib().cogdl_embedding(n, V, k, pt, _dtype_code(table), pi, scale, po, _dtype_code(out),
+        _check(lib().cogdl_embedding(n, V, k, pt, _dtype_code(table), pi, float(scale), po, _dtype_code(out),
                                      _stream_of(device)), "cogdl_embedding")
     return out
 
@@ -1179,6 +1189,7 @@ def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, ou
     bytes."""
     import torch
     n, k = _dims(dY, "dY", 2)
+    V, k = _i32(V, "V"), _i32(k, "dY's width")
     if V < 1:
         raise CogdlError("the table needs at least one row")
     _index_array(index, "index")
@@ -1194,7 +1205,7 @@ def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, ou
     po = _take(out, "out", None, device)
     pw, bytes_, workspace = _scratch(workspace, need, dY, device)
     with here:
-        _check(lib().cogdl_embedding_backward(n, V, k, pd, _dtype_code(dY), pi, scale, po, _dtype_code(out),
+        _check(lib().cogdl_embedding_backward(n, V, k, pd, _dtype_code(dY), pi, float(scale), po, _dtype_code(out),
                                               1 if accumulate else 0, pw, bytes_, _stream_of(device)),
                "cogdl_embedding_backward")
     return out
@@ -1228,6 +1239,7 @@ def _head(X, W, bias):
         raise CogdlError("X must be [n, k] and W [V, k] of the same dtype")
     if V < 1:
         raise CogdlError("W needs at least one row")
+    V, k = _i32(V, "W's rows"), _i32(k, "W's width")
     if bias is not None:
         _numel(bias, "bias", V)
     return n, V, k, _dtype_code(X)
@@ -1298,7 +1310,7 @@ def linear_distill(X, W, index, teacher, bias=None, temperature: float = 1.0, lo
     pl, ps, pp = _take(loss, "loss", f32, device), _take(lse, "lse", f32, device), _take(logp, "logp", f32, device)
     ws, bytes_, workspace = _scratch(workspace, need, X, device)
     with here:
-        _check(lib().cogdl_linear_distill(n, V, k, K, px, pw, dt, pb, pi, pt, temperature, pl, ps, pp, ws, bytes_,
+        _check(lib().cogdl_linear_distill(n, V, k, K, px, pw, dt, pb, pi, pt, float(temperature), pl, ps, pp, ws, bytes_,
                                           _stream_of(device)), "cogdl_linear_distill")
     return loss, lse, logp
 
@@ -1369,6 +1381,6 @@ def linear_distill_backward(dloss, X, W, index, teacher, lse, logp, bias=None, t
     o, dx, dw, db = _head_gradients(X, W, bias, out, device)
     ws, bytes_, workspace = _scratch(workspace, need, X, device)
     with here:
-        _check(lib().cogdl_linear_distill_backward(n, V, k, K, pd, px, pw, dt, pb, pi, pt, temperature, ps, pp, dx, dw,
+        _check(lib().cogdl_linear_distill_backward(n, V, k, K, pd, px, pw, dt, pb, pi, pt, float(temperature), ps, pp, dx, dw,
                                                    db, ws, bytes_, _stream_of(device)), "cogdl_linear_distill_backward")
     return o

@@ -336,10 +336,10 @@ __global__ __launch_bounds__(kBlock) void k_scatter_sums(ScatterArgs a)
         if (token < (uint32_t)a.V) flush(begun ? 0 : token == after ? 1 : -1);
     }
 }
-// more where rows are short.  Latency, mostly: 1M tokens, 10417 pieces of 256 columns, 17 us.
+
 // Tokens that reach over pieces: the slot of the piece that begins one, then those of the pieces after.  A
 // wavefront looks at a piece; tokens of more pieces than kShort are summed by the whole workgroup, in 16 parts, or
-// more where rows are short.
+// more where rows are short.  Latency, mostly: 1M tokens, 10417 pieces of 256 columns, 17 us.
 constexpr int kShort = 16;
 
 // The sums of slots [q0, q1) of a token that begins in `piece`, columns [c, c + 4) below k.

@@ -38,10 +38,10 @@ struct RowsHead {
 
 // The two products of a piece as tiles of tile x tile on `resident` workgroups of each XCD, one after another: dX's
 // sums (rows x k, a slice of the piece's `width` columns each), then dW (width x k, summed over the rows, a part of
-// `parts` each).  The time of
-// the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile costs its chunks and
-// kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  4096 rows, 30% of them padded, 40943 x 512
-// fp16: the products in launches of their own, slices by the rows given, 319 us, together by the rows that count 270.
+// `parts` each).  The time of the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile
+// costs its chunks and kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  4096 rows, 30% of
+// them padded, 40943 x 512 fp16: the products in launches of their own, slices by the rows given, 319 us, together by
+// the rows that count 270.
 constexpr int kTileStart = 4, kTileSums = 2;
 
 struct ProductsPlan {
@@ -235,8 +235,8 @@ __device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, M
 }
 
 // The pitch of rows of `cols` 16-bit elements: an odd number of 256 bytes, so that the rows of a tile start on
-// different channels of the memory.  (4096 rows, 30% of them padded, 40943 x 512
-// fp16: dz 177 us, so 172; the products 271 and 261.)
+// different channels of the memory.  (4096 rows, 30% of them padded, 40943 x 512 fp16: dz 177 us, so 172; the
+// products 271 and 261.)
 inline int64_t odd_pitch(int64_t cols)
 {
     const int64_t lines = (cols + 127) / 128;

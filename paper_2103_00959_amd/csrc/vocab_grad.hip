@@ -215,7 +215,8 @@ __device__ __forceinline__ void sum_slots(const float *__restrict__ from, int64_
 }
 
 // The piece's db from the row tiles' sums and the entries' part (`db_blocks` workgroups from `dx_blocks` on), its dW from
-// its parts' sums (those behind), and, with the last piece, dX of the live rows from their slices' sums.  Bound by memory: 8192 x 1024 of two slices 20 us (4.3 TB/s).
+// its parts' sums (those behind), and, with the last piece, dX of the live rows from their slices' sums.  Bound by
+// memory: 8192 x 1024 of two slices 20 us (4.3 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int db_blocks, int rows_a_part)
 {
@@ -271,8 +272,8 @@ int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 // Parts of the rows that dW of a piece is summed in: many rows and few classes make few tiles, each a sum over all
-// rows.  As many as the chip holds tiles, of 1024 rows or more.  232965 rows, 41
-// classes, 128 features: the products 3248 us with one part, 46 so.
+// rows.  As many as the chip holds tiles, of 1024 rows or more.  232965 rows, 41 classes, 128 features: the products
+// 3248 us with one part, 46 so.
 int32_t dw_parts(int64_t n, int32_t width, int32_t k, int tile)
 {
     const int64_t tiles = tiles_of(width, k, tile), want = tile == 256 ? 256 : 512;

@@ -173,3 +173,16 @@ def test_distill_sizes():
     refused(lambda: b(v, X, W, index, teacher, v, teacher[:, :2]), "logp has 8 elements, expected 12")
     refused(lambda: b(v, X, W, index, teacher, v[:2], teacher), "lse has 2 elements, expected 4")
     refused(lambda: b(v, X, W, index, teacher, v, teacher, temperature=0.0), "temperature must be positive")
+
+
+def test_sizes_past_32_bits():
+    far = 2 ** 32 + 5
+    index, t = torch.zeros(3, dtype=i32), torch.zeros(3, dtype=i32)
+    refused(lambda: cg.embedding(torch.zeros(far, 0), index), "past 32 bits")
+    refused(lambda: cg.embedding_backward(torch.zeros(3, 8), index, far), "past 32 bits")
+    refused(lambda: cg.embedding_backward(torch.zeros(0, far), index[:0], 9), "past 32 bits")
+    refused(lambda: cg.linear_cross_entropy(torch.zeros(3, 0, dtype=bf16), torch.zeros(far, 0, dtype=bf16), t), "past 32 bits")
+    refused(lambda: cg.linear_distill(torch.zeros(3, 0, dtype=bf16), torch.zeros(far, 0, dtype=bf16), index.view(3, 1),
+                                      torch.zeros(3, 1)), "past 32 bits")
+    with pytest.raises(TypeError):
+        cg.embedding_backward(torch.zeros(3, 8), index, 9.0)
