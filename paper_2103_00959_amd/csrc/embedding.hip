@@ -104,6 +104,8 @@ struct ScatterArgs {
     const uint32_t *sorted;      // n
     const uint32_t *order;       // n: their places
     float *slots;                // [2 x pieces][k]: partial sums of a piece's first token, begun before, and of its last
+    int32_t *counts;             // [digit][tile] (lists of the middle lengths)
+    int32_t tiles;
     int32_t per, pieces;
     int32_t lanes, log_lanes, vecs, chunks;
 };
@@ -122,12 +124,17 @@ __device__ __forceinline__ void write_zeros(const ScatterArgs &a, int64_t me, in
     }
 }
 
+__device__ __forceinline__ uint32_t key_of(const ScatterArgs &a, int64_t i)
+{
+    const uint32_t t = (uint32_t)a.index[i];
+    return t < (uint32_t)a.V ? t : (uint32_t)a.V;
+}
+
 __global__ __launch_bounds__(kBlock) void k_tokens(ScatterArgs a)
 {
     const int64_t me = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
     for (int64_t i = me; i < a.n; i += all) {
-        const uint32_t t = (uint32_t)a.index[i];
-        a.keys[i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
+        a.keys[i] = key_of(a, i);
     }
     if (!a.add) write_zeros(a, me, all);
 }
@@ -153,8 +160,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_short(ScatterArgs a, int 
     }
     const int n = (int)a.n, lane = lane_id(), wave = threadIdx.x / kWave;
     for (int i = threadIdx.x; i < n; i += kSortThreads) {
-        const uint32_t t = (uint32_t)a.index[i];
-        keys[0][i] = t < (uint32_t)a.V ? t : (uint32_t)a.V;
+        keys[0][i] = key_of(a, i);
         vals[0][i] = (uint16_t)i;
     }
     const int run = ((n + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
@@ -214,6 +220,150 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_short(ScatterArgs a, int 
     for (int i = threadIdx.x; i < n; i += kSortThreads) {
         const_cast<uint32_t *>(a.sorted)[i] = keys[now][i];
         const_cast<uint32_t *>(a.order)[i] = vals[now][i];
+    }
+}
+
+// Lists up to kMiddleList are sorted so in tiles of kTile keys, by digits of up to 9 bits: a launch counts each tile's
+// digits (the first one of the tokens themselves, its further workgroups writing the zeros), one sums a digit's
+// counts over the tiles, one moves the keys.  262144 tokens of 18 bits 53 us, by the library's sort of 8 bits a pass
+// behind a launch that makes its keys 85; 1M 60 and 88, 4M 102 and 132; 16M 302 and 308, of 13 bits 231 and 220: short
+// runs of a digit cost there.
+constexpr int kTile = 4096, kTileEach = kTile / kSortThreads, kTileBits = 9;
+constexpr int64_t kMiddleList = 1 << 23;
+
+__global__ __launch_bounds__(kSortThreads) void k_token_counts(ScatterArgs a, const uint32_t *__restrict__ keys, int shift, int dbits)
+{
+    __shared__ int counts[kSortWaves << kTileBits];
+    if ((int)blockIdx.x >= a.tiles) {
+        write_zeros(a, (int64_t)(blockIdx.x - a.tiles) * kSortThreads + threadIdx.x, (int64_t)(gridDim.x - a.tiles) * kSortThreads);
+        return;
+    }
+    const int64_t from = (int64_t)blockIdx.x * kTile;
+    const int wave = threadIdx.x / kWave;
+    const uint32_t mask = (1u << dbits) - 1;
+    uint32_t key[kTileEach];
+#pragma unroll
+    for (int u = 0; u < kTileEach; ++u) {
+        const int64_t i = from + u * kSortThreads + threadIdx.x, in = i < a.n ? i : a.n - 1;
+        key[u] = keys ? keys[in] : key_of(a, in);
+    }
+    for (int e = threadIdx.x; e < kSortWaves << dbits; e += kSortThreads) counts[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kTileEach; ++u)
+        if (from + u * kSortThreads + threadIdx.x < a.n) atomicAdd(&counts[(wave << dbits) + (key[u] >> shift & mask)], 1);
+    __syncthreads();
+    if ((int)threadIdx.x > (int)mask) return;
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) all += counts[(w << dbits) + threadIdx.x];
+    a.counts[(int64_t)threadIdx.x * a.tiles + blockIdx.x] = all;
+}
+
+// Inclusive sums over the tiles, a wavefront a digit.
+__global__ __launch_bounds__(kBlock) void k_token_scan(ScatterArgs a, int digits)
+{
+    constexpr int each = 4;
+    const int digit = (int)(blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave);
+    if (digit >= digits) return;
+    int32_t *__restrict__ row = a.counts + (int64_t)digit * a.tiles;
+    int carry = 0;
+    for (int base = 0; base < a.tiles; base += each * kWave) {
+        int v[each], sum = 0;
+#pragma unroll
+        for (int e = 0; e < each; ++e) {
+            const int at = base + lane_id() * each + e;
+            sum += v[e] = at < a.tiles ? row[at] : 0;
+        }
+        const int scan = wave_inclusive_scan(sum);
+        int run = carry + scan - sum;
+#pragma unroll
+        for (int e = 0; e < each; ++e) {
+            const int at = base + lane_id() * each + e;
+            run += v[e];
+            if (at < a.tiles) row[at] = run;
+        }
+        carry += __builtin_amdgcn_readlane(scan, kWave - 1);
+    }
+}
+
+__global__ __launch_bounds__(kSortThreads) void k_token_move(ScatterArgs a, const uint32_t *__restrict__ keys,
+                                                             const uint32_t *__restrict__ vals, uint32_t *__restrict__ keys_out,
+                                                             uint32_t *__restrict__ vals_out, int shift, int dbits)
+{
+    __shared__ int counts[kSortWaves << kTileBits];
+    __shared__ int to[1 << kTileBits];                   // where a digit's keys go, less where they lie in the tile
+    __shared__ uint32_t stage[2][kTile];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const uint32_t mask = (1u << dbits) - 1;
+    // (an XCD takes neighbouring tiles, whose runs of a digit share cache lines)
+    const int xcd = blockIdx.x % 8, per = a.tiles / 8, rest = a.tiles % 8;
+    const int tile = xcd * per + (xcd < rest ? xcd : rest) + (int)blockIdx.x / 8;
+    const int64_t from = (int64_t)tile * kTile;
+    const int count = a.n - from < kTile ? (int)(a.n - from) : kTile;
+    const int run = wave * (kTile / kSortWaves);
+    uint32_t key[kTileEach], val[kTileEach];
+    int place[kTileEach];
+#pragma unroll
+    for (int u = 0; u < kTileEach; ++u) {
+        const int64_t i = from + run + u * kWave + lane, in = i < a.n ? i : a.n - 1;
+        key[u] = keys ? keys[in] : key_of(a, in);
+        val[u] = vals ? vals[in] : (uint32_t)in;
+    }
+    const bool mine = (int)threadIdx.x <= (int)mask;
+    const int32_t *__restrict__ row = a.counts + (int64_t)(mine ? threadIdx.x : 0) * a.tiles;
+    const int whole = mine ? row[a.tiles - 1] : 0, before = mine && tile > 0 ? row[tile - 1] : 0;
+    for (int e = threadIdx.x; e < kSortWaves << dbits; e += kSortThreads) counts[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kTileEach; ++u) {
+        const bool in = run + u * kWave + lane < count;
+        const uint32_t digit = key[u] >> shift & mask;
+        uint64_t same = __ballot(in);
+        for (int b = 0; b < dbits; ++b) {
+            const uint64_t ones = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? ones : ~ones;
+        }
+        if (in) {
+            int *const so_far = &counts[(wave << dbits) + digit];
+            place[u] = *so_far + __popcll(same & ((1ull << lane) - 1));
+            // (the last lane of a digit moves it on; the next round reads it behind this write)
+            if (same >> lane == 1) *so_far = place[u] + 1;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    int first[2] = {0, whole}, all[2];
+    if (mine) {
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) first[0] += counts[(w << dbits) + threadIdx.x];
+    }
+    block_exclusive_scans<2, kSortWaves>(first, all);
+    if (mine) {
+        int at = first[0];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int c = counts[(w << dbits) + threadIdx.x];
+            counts[(w << dbits) + threadIdx.x] = at;
+            at += c;
+        }
+        to[threadIdx.x] = first[1] + before - first[0];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kTileEach; ++u) {
+        if (run + u * kWave + lane >= count) continue;
+        const int at = place[u] + counts[(wave << dbits) + (key[u] >> shift & mask)];
+        stage[0][at] = key[u];
+        stage[1][at] = val[u];
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < count; q += kSortThreads) {
+        const uint32_t k = stage[0][q];
+        const int at = to[k >> shift & mask] + q;
+        keys_out[at] = k;
+        vals_out[at] = stage[1][q];
     }
 }
 
@@ -476,7 +626,7 @@ cogdl_status check_table(int64_t n, int32_t V, int32_t k)
 }
 
 struct Scatter {
-    size_t keys, ping_k, ping_v, sorted, order, radix, slots, total;
+    size_t keys, ping_k, ping_v, sorted, order, sort, slots, total;
 };
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
@@ -514,7 +664,7 @@ Scatter scatter_layout(int64_t n, int32_t k)
     s.ping_v = off; off += al(8 * (size_t)n);
     s.sorted = off; off += al(4 * (size_t)n);
     s.order = off; off += al(4 * (size_t)n);
-    s.radix = off; off += al(radix_workspace_bytes(n));
+    s.sort = off; off += al(n <= kMiddleList ? (4ull << kTileBits) * ((n + kTile - 1) / kTile) : radix_workspace_bytes(n));
     s.slots = off; off += al(8 * (size_t)pieces * k);
     s.total = off;
     return s;
@@ -628,6 +778,27 @@ cogdl_status cogdl_embedding_backward(int64_t n, int32_t V, int32_t k, const voi
         int64_t blocks = (zeros + kSortThreads - 1) / kSortThreads;
         if (blocks > 1024) blocks = 1024;
         COGDL_LAUNCH("embedding_sort", k_sort_short, (unsigned)(blocks + 1), kSortThreads, stream, a, bits);
+    } else if (n > 0 && n <= kMiddleList) {
+        char *ws = static_cast<char *>(workspace);
+        const Scatter s = scatter_layout(n, k);
+        a.counts = reinterpret_cast<int32_t *>(ws + s.sort);
+        a.tiles = (int32_t)((n + kTile - 1) / kTile);
+        int64_t blocks = (zeros + kSortThreads - 1) / kSortThreads;
+        if (blocks > 1024) blocks = 1024;
+        const int passes = (bits + kTileBits - 1) / kTileBits;
+        const uint32_t *keys = nullptr, *vals = nullptr;
+        for (int p = 0, shift = 0; p < passes; ++p) {
+            const int dbits = (bits - shift) / (passes - p);
+            const bool last = p == passes - 1;
+            uint32_t *const keys_to = last ? const_cast<uint32_t *>(a.sorted) : reinterpret_cast<uint32_t *>(ws + s.ping_k) + (p & 1) * n;
+            uint32_t *const vals_to = last ? const_cast<uint32_t *>(a.order) : reinterpret_cast<uint32_t *>(ws + s.ping_v) + (p & 1) * n;
+            COGDL_LAUNCH("embedding_count", k_token_counts, (unsigned)(a.tiles + (p == 0 ? blocks : 0)), kSortThreads, stream, a, keys, shift, dbits);
+            COGDL_LAUNCH("embedding_scan", k_token_scan, (1u << dbits) / 4 + 1, kBlock, stream, a, 1 << dbits);
+            COGDL_LAUNCH("embedding_move", k_token_move, (unsigned)a.tiles, kSortThreads, stream, a, keys, vals, keys_to, vals_to, shift, dbits);
+            keys = keys_to;
+            vals = vals_to;
+            shift += dbits;
+        }
     } else {
         int64_t blocks = ((n > zeros ? n : zeros) + kBlock - 1) / kBlock;
         if (blocks > 4096) blocks = 4096;
@@ -637,7 +808,7 @@ cogdl_status cogdl_embedding_backward(int64_t n, int32_t V, int32_t k, const voi
         const Scatter s = scatter_layout(n, k);
         COGDL_HIP_TRY(radix_sort_pairs(a.keys, nullptr, const_cast<uint32_t *>(a.sorted), const_cast<uint32_t *>(a.order),
                                        n, bits, reinterpret_cast<uint32_t *>(ws + s.ping_k),
-                                       reinterpret_cast<uint32_t *>(ws + s.ping_v), ws + s.radix, stream));
+                                       reinterpret_cast<uint32_t *>(ws + s.ping_v), ws + s.sort, stream));
     }
     return by_type(dtype, [&](auto ti) {
         using TI = decltype(ti);

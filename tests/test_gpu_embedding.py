@@ -181,6 +181,13 @@ def test_gradient_around_the_lengths_of_the_sorts(n):
         check_gradient(n, V, k, "f32", "f32", 1.3, n % 2 == 0, n + V)
 
 
+@pytest.mark.parametrize("n,V", [(12288, 511), (12289, 512), (40_961, 200_000), (100_001, 292_969),
+                                 (2 ** 23, 70_000), (2 ** 23 + 1, 70_000)])
+def test_gradient_of_longer_lists(n, V):
+    """Whole tiles of 4096 tokens and not, digits of 9 bits one and several times, and the lists past them."""
+    check_gradient(n, V, 2 if n > 2 ** 20 else 9, "f32", "f32", 2.0, n % 2 == 0, n + V)
+
+
 def test_gradient_is_summed_in_the_order_of_the_batch():
     """One token's rows that only add up right in order: 2^24 + 1 + 1 ... stays 2^24 in fp32, 1 + 1 + ... + 2^24 does
     not.  (15 rows: one piece.)"""
