@@ -183,6 +183,30 @@ def test_any_alignment():
     assert ox[0] == 3 and ow[0] == 3
 
 
+@pytest.mark.parametrize("x,w", [(1, 0), (0, 1), (2, 4), (1, 1)])
+@pytest.mark.parametrize("n", [1, 5, 16])
+def test_few_rows_at_any_alignment(n, x, w):
+    """Up to 16 rows, X or W some elements off the grid, between NaN."""
+    X, W, t, b, g, _ = layer(n, 333, 46, "f16", 30 + n, True)
+    bx, bw = (torch.full((v.numel() + 8,), float("nan"), dtype=v.dtype, device="cuda") for v in (X, W))
+    bx[x:x + X.numel()], bw[w:w + W.numel()] = X.flatten().cuda(), W.flatten().cuda()
+    Xo, Wo = bx[x:x + X.numel()].view(X.shape), bw[w:w + W.numel()].view(W.shape)
+    loss, lse = cg.linear_cross_entropy(Xo, Wo, dev(t), dev(b))
+    f = ex.loss(X, W, *one_hot(t, 333), b)
+    ex.close("loss", loss, *f["loss"])
+    ex.close("lse", lse, *f["lse"])
+
+
+def test_db_of_many_rows_alone():
+    """More row tiles than one launch joins: db without the other gradients, with rows left out at the end."""
+    X, W, t, b, g, _ = layer(40_000, 70, 24, "bf16", 15, True)
+    t[-9000:] = -1
+    d = [dev(v) for v in (X, W, t, b)]
+    loss, lse = cg.linear_cross_entropy(*d)
+    out = cg.linear_cross_entropy_backward(dev(g), d[0], d[1], d[2], loss, lse, d[3], out={"dX": None, "dW": None})
+    ex.close("db", out["db"], *ex.gradients(X, W, *one_hot(t, 70), g, b)["db"])
+
+
 def test_each_gradient_alone_and_the_same_bits_again():
     X, W, t, b, g, _ = layer(300, 2000, 136, "bf16", 14, True)
     d = [dev(v) for v in (X, W, t, b)]

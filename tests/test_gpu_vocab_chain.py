@@ -123,7 +123,7 @@ def model(K, seed=0, n=300):
 
 
 @pytest.mark.parametrize("K", [0, 6])
-@pytest.mark.parametrize("n", [40, 300, 9000])
+@pytest.mark.parametrize("n", [16, 40, 300, 9000, 40_000])
 def test_captured_steps_replay(n, K):
     """A whole step captured into a graph: every replay, with eager work and new contents between, equals the eager
     one (the number of rows that count changes from replay to replay)."""
