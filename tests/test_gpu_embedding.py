@@ -188,6 +188,26 @@ def test_gradient_of_longer_lists(n, V):
     check_gradient(n, V, 2 if n > 2 ** 20 else 9, "f32", "f32", 2.0, n % 2 == 0, n + V)
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("n", [1, 15, 17, 1000, 8192])
+@pytest.mark.parametrize("V,k,dt,out", [(1, 40, "bf16", "f32"), (2, 1, "f32", "bf16"), (90, 64, "f32", "f32"),
+                                        (128, 1025, "f16", "bf16"), (683, 199, "f32", "f16"), (2048, 128, "bf16", "bf16"),
+                                        (2049, 128, "bf16", "bf16"), (1024, 200, "bf16", "f16"), (1025, 7, "f16", "f32")])
+def test_gradient_of_small_tables(V, k, dt, out, n, add):
+    """Short lists over tables of few tokens and chunks (up to 2048 of both together, the last chunk ragged), and just
+    past them; tokens in every place, in none, and all of the list's."""
+    check_gradient(n, V, k, dt, out, 8.0 if n == 1000 else 1.3, add, n + V)
+
+
+def test_gradient_of_unused_tokens_is_zero_whatever_the_factor():
+    index = torch.tensor([3, 3, -1], dtype=torch.int32, device="cuda")
+    for V, n in ((5, 3), (9000, 3), (9000, 9000)):
+        full = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+        full[:3] = index
+        got = cg.embedding_backward(torch.ones(n, 12, device="cuda"), full, V, scale=float("inf"))
+        assert torch.isinf(got[3]).all() and int((got != 0).any(1).sum()) == 1 and not torch.isnan(got).any()
+
+
 def test_gradient_is_summed_in_the_order_of_the_batch():
     """One token's rows that only add up right in order: 2^24 + 1 + 1 ... stays 2^24 in fp32, 1 + 1 + ... + 2^24 does
     not.  (15 rows: one piece.)"""
