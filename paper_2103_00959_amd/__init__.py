@@ -1141,12 +1141,13 @@ def _scratch(workspace, need, like, device):
     return _take(workspace, "workspace", None, device), workspace.numel() * workspace.element_size(), workspace
 
 
-def _i32(size, name):
-    """A size that the C ABI takes in 32 bits."""
-    size = operator.index(size)
-    if size > 2 ** 31 - 1:
-        raise CogdlError(f"{name} is {size}, past 32 bits")
-    return size
+_I32_MAX = 2 ** 31 - 1
+
+
+def _in_32_bits(V, k):
+    """Refuses a table whose sizes the C ABI does not take."""
+    if V > _I32_MAX or k > _I32_MAX:
+        raise CogdlError(f"a table of {V} rows of {k} has a size past 32 bits")
 
 
 def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
@@ -1157,7 +1158,7 @@ def embedding(table, index, scale: float = 1.0, out_dtype=None, out=None):
     V, k = _dims(table, "table", 2)
     if V < 1:
         raise CogdlError("table needs at least one row")
-    V, k = _i32(V, "the table's rows"), _i32(k, "the table's width")
+    _in_32_bits(V, k)
     n = _index_array(index, "index")
     _numel(out, "out", n * k)
     device, here = _home(table, "table")
@@ -1189,9 +1190,10 @@ def embedding_backward(dY, index, V: int, scale: float = 1.0, out_dtype=None, ou
     bytes."""
     import torch
     n, k = _dims(dY, "dY", 2)
-    V, k = _i32(V, "V"), _i32(k, "dY's width")
+    V = operator.index(V)
     if V < 1:
         raise CogdlError("the table needs at least one row")
+    _in_32_bits(V, k)
     _index_array(index, "index")
     _numel(index, "index", n)
     _numel(out, "out", V * k)
@@ -1239,7 +1241,7 @@ def _head(X, W, bias):
         raise CogdlError("X must be [n, k] and W [V, k] of the same dtype")
     if V < 1:
         raise CogdlError("W needs at least one row")
-    V, k = _i32(V, "W's rows"), _i32(k, "W's width")
+    _in_32_bits(V, k)
     if bias is not None:
         _numel(bias, "bias", V)
     return n, V, k, _dtype_code(X)
