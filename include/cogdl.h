@@ -616,6 +616,8 @@ cogdl_status cogdl_linear_cross_entropy_backward(int64_t n, int32_t V, int32_t k
  * counts where its index lies inside [0, V) (a padded one has logp 0); a teacher's
  * logit of -inf has q = 0.  The same index twice in a row is two entries.  A row
  * without an entry that counts, or with -inf alone, is left out as above (logp 0).
+ * A NaN or +inf among the teacher's logits that count makes its row's loss and dX
+ * NaN, and its entries' rows of dW and values of db.
  * Everything else as cogdl_linear_cross_entropy.  Gradients, from lse and logp:
  *   dz[i, v] = dloss[i] * T * (exp(z[i, v] / T - lse[i]) - sum_{e: index[i, e] = v} q[i, e])
  * and the rest as cogdl_linear_cross_entropy_backward (no gradient of the

@@ -187,7 +187,10 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         }
     }
     if (BACKWARD && a.db_q) {
-        for (int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x; v < a.V; v += (int64_t)gridDim.x * kBlock) a.db_q[v] = 0;
+        for (int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x; v < a.V; v += (int64_t)gridDim.x * kBlock) {
+            a.db_q[v] = 0;
+            a.db_odd[v] = 0;
+        }
     }
     const T *__restrict__ X = static_cast<const T *>(a.X);
     T *__restrict__ Xr = static_cast<T *>(a.Xr);

@@ -27,6 +27,8 @@ constexpr int64_t kMaxRows = 1 << 24;
 
 // Runs that many rows are counted in before they are gathered.
 constexpr int kMostRuns = 4096;
+// Terms of a sum that are not finite, together: any two of them make NaN.
+constexpr uint32_t kOddPlus = 1, kOddMinus = 2, kOddNan = 4;
 constexpr int64_t kManyRows = 16384;
 
 // Header of a workspace, written by k_vocab_rows.
@@ -103,7 +105,8 @@ struct VocabArgs {
     float *db_part;              // [row tile][pitch]: a piece's
     float *db_join;              // [kJoin row tiles][pitch] (many row tiles)
     int32_t row_tiles;
-    unsigned long long *db_q;    // V: the targets' part, in units of 2^-unit_bits
+    unsigned long long *db_q;    // V: the entries' part of db, in units of 2^-unit_bits (distillation)
+    uint32_t *db_odd;            // V: what of db is not finite, kOdd... (distillation)
     int32_t unit_bits;
     // this launch
     int32_t v0, width;           // the vocabulary piece [v0, v0 + width)

@@ -8,10 +8,21 @@ namespace {
 
 constexpr int kBlock = 256;
 
+// Notes a term of db[v] that is not finite.
+__device__ __forceinline__ void note_odd(const VocabArgs &a, int32_t v, float term)
+{
+    if (fabsf(term) < INFINITY) return;
+    const uint32_t bit = term == INFINITY ? kOddPlus : term == -INFINITY ? kOddMinus : kOddNan;
+    if (!(a.db_odd[v] & bit)) atomicOr(&a.db_odd[v], bit);
+}
+
 // The entries' part of dz (distillation), in fp32 from their log-probabilities: dz = g T (p - sum q), where p may
 // be near sum q and dz of it was rounded as g T p.  Several entries of a row on the same answer all write their
 // common value.  On the first piece also the entries' part of db, in whole numbers (any order gives the same
-// sum).  A wavefront a row, an entry a lane.  4096 rows of 64 entries 16 us, every store a cache line of its own.
+// sum).  Those hold no infinity and no NaN, and db's other part has g T p where dz is g T (p - sum q): terms of db
+// that are not finite are noted apart, those of an entry (a teacher's NaN or +inf makes its row's q NaN) and, of a row
+// whose weight or lse is not finite, dz of every answer.  A wavefront a row, an entry a lane.  4096 rows of 64 entries
+// 16 us, every store a cache line of its own.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
 {
@@ -37,12 +48,21 @@ __global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
                     if (index[o] == v) q += o == e ? mine : expf(log_share(teacher[o], a.T, tlse));
                 const float one[1] = {(expf(a.logp_in[i * a.entries + e]) - q) * g};
                 store_out<T, 1>(dz + p * a.pitch, v - a.v0, one);
+                if (a.db_q) note_odd(a, v, one[0]);
             }
             if (db) {
                 const float w = ldexpf(mine * g, a.unit_bits);
-                // (a row whose gradient is not finite makes all of db NaN by its dz)
+                // (past that only where the term is noted as odd, or beside a weight that is infinite: then all of db is)
                 if (fabsf(w) < 9e18f) atomicAdd(&a.db_q[v], (unsigned long long)(long long)rintf(w));
             }
+        }
+        if (!a.db_q || (fabsf(g) < INFINITY && fabsf(a.lse2[p]) < INFINITY)) continue;       // (uniform)
+        __threadfence_block();                           // (the entries' dz, by other lanes)
+        __builtin_amdgcn_wave_barrier();
+        for (int c = lane_id(); c < a.width; c += kWave) {
+            float term[1];
+            load_vec<T, 1>(dz + p * a.pitch, c, term);
+            note_odd(a, a.v0 + c, term[0]);
         }
     }
 }
@@ -243,7 +263,11 @@ __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks
         float t = 0.f;
 #pragma unroll 8
         for (int p = 0; p < parts; ++p) t += part[(int64_t)p * a.pitch + c];
-        if (a.db_q) t = (float)((double)t - ldexp((double)(long long)a.db_q[a.v0 + c], -a.unit_bits));
+        if (a.db_q) {
+            t = (float)((double)t - ldexp((double)(long long)a.db_q[a.v0 + c], -a.unit_bits));
+            const uint32_t odd = a.db_odd[a.v0 + c];
+            if (odd) t = odd == kOddPlus ? INFINITY : odd == kOddMinus ? -INFINITY : NAN;
+        }
         a.db[a.v0 + c] = t * unscale;
         return;
     }
@@ -347,6 +371,7 @@ size_t lay_backward(VocabArgs &a, char *ws)
     a.db_part = reinterpret_cast<float *>(ws + l.take(4 * (size_t)a.row_tiles * a.pitch));
     a.db_join = reinterpret_cast<float *>(ws + l.take(a.row_tiles > kManyTiles ? 4 * (size_t)((a.row_tiles + kJoin - 1) / kJoin) * a.pitch : 0));
     a.db_q = reinterpret_cast<unsigned long long *>(ws + l.take(a.distill ? 8 * (size_t)a.V : 0));
+    a.db_odd = reinterpret_cast<uint32_t *>(ws + l.take(a.distill ? 4 * (size_t)a.V : 0));
     return l.total;
 }
 
