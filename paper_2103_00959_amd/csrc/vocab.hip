@@ -321,7 +321,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
             if (col0 >= a.width || r0 >= s.have) return;
             const int lane = lane_of_outputs();
             // the bias, and -inf behind the last column: no part of a sum, no gradient
-            if (EXTRA || col0 + 32 * WC > a.width) {
+            // (col0 + 32 WC may pass 32 bits)
+            if (EXTRA || col0 > a.width - 32 * WC) {
 #pragma unroll
                 for (int j = 0; j < WC; ++j)
 #pragma unroll
