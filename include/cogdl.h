@@ -618,6 +618,9 @@ cogdl_status cogdl_linear_cross_entropy_backward(int64_t n, int32_t V, int32_t k
  * without an entry that counts, or with -inf alone, is left out as above (logp 0).
  * A NaN or +inf among the teacher's logits that count makes its row's loss and dX
  * NaN, and its entries' rows of dW and values of db.
+ * The loss is not cut off at 0: rounding may bring it a little below where student
+ * and teacher agree, and entries on one answer do where the student gives it more
+ * than each of them (two of q = 1/2 on a certain answer: T^2 log(1/2)).
  * Everything else as cogdl_linear_cross_entropy.  Gradients, from lse and logp:
  *   dz[i, v] = dloss[i] * T * (exp(z[i, v] / T - lse[i]) - sum_{e: index[i, e] = v} q[i, e])
  * and the rest as cogdl_linear_cross_entropy_backward (no gradient of the

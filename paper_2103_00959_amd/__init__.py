@@ -1293,7 +1293,8 @@ def linear_distill(X, W, index, teacher, bias=None, temperature: float = 1.0, lo
     vocabulary and never kept, against q = softmax(teacher / T) over the K entries of a row.  Returns (loss, lse,
     logp): loss = T^2 sum q (log q - logp) [n], lse = logsumexp(z / T) [n], logp = z[index] / T - lse [n, K], all
     fp32.  index int32 [n, K] (outside [0, V): no entry), teacher fp32 [n, K]; a row without entries is left out
-    (zeros).  Everything else as linear_cross_entropy; the gradients are linear_distill_backward's."""
+    (zeros).  A loss may lie below 0: by rounding, or where entries share an answer.  Everything else as
+    linear_cross_entropy; the gradients are linear_distill_backward's."""
     import torch
     n, V, k, dt = _head(X, W, bias)
     K = _teacher(index, teacher, n, temperature)
