@@ -266,10 +266,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         at += __popcll(mask);
     }
     if (to == a.n && wave == 0) {
-        if (lane == 0) {
-            a.head->off[0] = 0;
-            a.head->off[1] = at;
-        }
+        if (lane == 0) a.head->live = at;
         if constexpr (BACKWARD) {
             // the slices of dX's sums that end soonest for so many rows: a candidate a lane
             static_assert(kMostSlices == kWave, "a candidate a lane");
@@ -297,7 +294,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
     const int wr = wave / WAVES_C, wc = wave % WAVES_C;
     const int r0 = wr * (32 * WR), c0 = wc * (32 * WC);
     GridWalk walk;
-    int64_t rows = !GRAD && a.plain ? a.n : a.head->off[1];
+    int64_t rows = !GRAD && a.plain ? a.n : a.head->live;
     if constexpr (!GRAD) {
         rows -= a.p0;
         rows = rows < 0 ? 0 : rows < a.block ? rows : a.block;
@@ -494,7 +491,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_finish(VocabArgs a, int R)
     __shared__ float2 part[kBlock];
     __shared__ float lse_of[16], dots[16];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    int64_t live = a.plain ? a.n : a.head->off[1];
+    int64_t live = a.plain ? a.n : a.head->live;
     live = live < a.p0 + a.block ? live : a.p0 + a.block;
     const int r = threadIdx.x & (R - 1), sg = threadIdx.x / R, S = kBlock / R;
     for (int64_t r0 = a.p0 + (int64_t)blockIdx.x * R; r0 < live; r0 += (int64_t)gridDim.x * R) {

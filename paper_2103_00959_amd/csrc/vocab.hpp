@@ -33,7 +33,7 @@ constexpr int64_t kManyRows = 16384;
 
 // Header of a workspace, written by k_vocab_rows.
 struct RowsHead {
-    int32_t off[2];              // 0, live rows
+    int32_t live;                // rows that count
     float scale, unscale;        // |g T| scale <= 2^15 for every live row, and 1 / scale
     int32_t slices;              // of dX's sums over a piece
 };
@@ -111,8 +111,7 @@ struct VocabArgs {
     // this launch
     int32_t v0, width;           // the vocabulary piece [v0, v0 + width)
     int32_t pitch;               // of dz
-    int32_t tiles_c;             // column tiles of the logits, of dX's sums
-    int32_t tiles_w;             // column tiles of dW
+    int32_t tiles_c;             // column tiles of the logits, of both products
     float *dw_part;              // [part][piece's width][kp] (more than one part)
     bool first;                  // the first piece
     bool direct;                 // dX leaves the products as it is: one piece, one slice

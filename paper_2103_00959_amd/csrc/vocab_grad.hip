@@ -26,7 +26,7 @@ __device__ __forceinline__ void note_odd(const VocabArgs &a, int32_t v, float te
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
 {
-    const int64_t live = a.head->off[1];
+    const int64_t live = a.head->live;
     const float scale = a.head->scale;
     T *__restrict__ dz = static_cast<T *>(a.dz);
     const int64_t waves = (int64_t)gridDim.x * (kBlock / kWave);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     extern __shared__ __align__(16) char lds[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int r0 = wave / WAVES_C * (32 * WR), c0 = wave % WAVES_C * (32 * WC);
-    const int live = a.head->off[1];
+    const int live = a.head->live;
     char *const mine = lds + 2 * (TM + TN) * kX * 2 + wave * kOutBytes;
     const auto busy = [&](const Span &s) { return r0 < s.have && s.tile * TN + c0 < a.k; };
     const auto nothing = [](const Span &) {};
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a
     if (a.dW) {
         const float unscale = a.head->unscale;
         const int parts = a.plan.parts, per = ((live + parts - 1) / parts + kX - 1) / kX * kX;
-        walk.start(a.width, TM, a.tiles_w, parts, block, kPanel, false);
+        walk.start(a.width, TM, a.tiles_c, parts, block, kPanel, false);
         ColOperand<T, TM, N, kDirect, false> A;
         ColOperand<T, TN, N, kDirect, false> B;
         const auto open = [&](const Span &s) {
@@ -202,7 +202,7 @@ constexpr int kJoin = 64, kManyTiles = 256;
 __global__ __launch_bounds__(kBlock) void k_vocab_db(VocabArgs a, int rows_a_part)
 {
     __shared__ float sums[kBlock];
-    const int64_t live = a.head->off[1];
+    const int64_t live = a.head->live;
     const int parts = (int)((live + rows_a_part - 1) / rows_a_part);
     const int c = (int)blockIdx.y * kWave + lane_id(), q = threadIdx.x / kWave;
     const int from = (int)blockIdx.x * kJoin + q * (kJoin / 4);
@@ -240,7 +240,7 @@ __device__ __forceinline__ void sum_slots(const float *__restrict__ from, int64_
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_out(VocabArgs a, int dx_blocks, int db_blocks, int rows_a_part)
 {
-    const int64_t live = a.head->off[1];
+    const int64_t live = a.head->live;
     const float unscale = a.head->unscale;
     if ((int)blockIdx.x >= dx_blocks + db_blocks) {
         const int vecs = a.kp / 8;
@@ -423,7 +423,7 @@ cogdl_status run_backward(VocabArgs a, cogdl_dtype dtype, void *workspace, size_
             }
         }
         if (a.dX || a.dW) {
-            a.tiles_c = a.tiles_w = (a.k + tile - 1) / tile;
+            a.tiles_c = (a.k + tile - 1) / tile;
             const int64_t tiles = (a.dX ? tiles_of(a.n, a.k, tile) * a.plan.most : 0) + (a.dW ? tiles_of(a.width, a.k, tile) * a.plan.parts : 0);
             COGDL_TRY(launch_vocab("vocab_products", bf16 ? pick_products<bf16_t>(wide, on_grid(a.W, a.k)) : pick_products<f16_t>(wide, on_grid(a.W, a.k)),
                                    a, tiles, waves, lds_of(waves, tile, tile), stream));
