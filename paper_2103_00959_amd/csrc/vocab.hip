@@ -281,8 +281,12 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
 // Tiles of logits.  GRAD: dz of the piece, else each row's (max, sum) over the wavefront's columns.  EXTRA: with a
 // bias, or db's sums over the tile's rows.  Bound by the matrix cores and, of narrow features, by what is done with
 // their outputs (an exponential each, a quarter of the other instructions' rate; about 3 chunks of 64 features' time
-// a tile): 8192 x 131072 of 1024 features the statistics 1930 us (1.14 PFLOP/s; a library product that writes the logits
-// 1.16), dz 2170; 2867 x 40943 of 512 131 (0.92 PFLOP/s) and 160; 2048 x 14951 of 200 26 (0.47).
+// a tile): 8192 x 131072 of 1024 features the statistics 1912 us (1.15 PFLOP/s; a library product that writes the logits
+// 1.16 to 1.21), dz 2103; 2867 x 40943 of 512 125 (0.96 PFLOP/s) and 148; 2048 x 14951 of 200 27 (0.45).
+// dz is rounded to T, by half a step at most: the matrix instructions of the products behind take 16 bits, and W and X
+// are T.  The gradients are then 0.0018 to 0.0023 of their size off in bf16 and 0.0003 to 0.0004 in fp16, where the
+// rounding of the outputs alone makes 0.0017 and 0.0002 to 0.0004.  dz in two parts of 16 bits would take that away and
+// double the products: 3750 us more of the 7900 of the first of those sizes.
 template <typename T, int WAVES, int TM, int TN, int SRCB, bool GRAD, bool EXTRA>
 __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_logits(VocabArgs a)
 {

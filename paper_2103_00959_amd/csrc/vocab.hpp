@@ -43,7 +43,7 @@ struct RowsHead {
 // `parts` each).  The time of the busiest workgroup where dX's sums are cut into s slices, in chunks of 64: a tile
 // costs its chunks and kTileStart more, dX's kTileSums besides (its sums go to memory in fp32).  4096 rows, 30% of
 // them padded, 40943 x 512 fp16: the products in launches of their own, slices by the rows given, 319 us, together by
-// the rows that count 270.
+// the rows that count 270 (both before rows of dz lay apart as odd_pitch has them; 235 to 250 since).
 constexpr int kTileStart = 4, kTileSums = 2;
 
 struct ProductsPlan {
@@ -148,9 +148,9 @@ using VocabKernel = void (*)(VocabArgs);
 // numbered slice by slice, then in panels of so many row tiles, in a panel column by column; the XCDs take equal runs
 // of them, their workgroups one after another: those that run together on an XCD take a panel's rows of tiles by a
 // few columns, and share both operands in its L2.  TURNED: each XCD begins an eighth of its run further on than the
-// one before.  The XCDs that go through the same columns side by side share them in the Infinity Cache (the
-// statistics of 8192 x 131072 logits, 1024 features: 1935 us, turned 2025), but their stores to rows a power of two
-// apart meet on the same channels (dz there: 2440 us, turned 2190).
+// one before.  Those that go through the same columns side by side store to the same channels of the memory: dz of
+// 8192 x 131072 logits, 1024 features, 2390 us, turned 2110.  The statistics store little (1920 us, turned 1905), and so
+// do the products.
 constexpr int kPanel = 4;
 
 struct GridWalk {
@@ -205,8 +205,8 @@ __device__ __forceinline__ int lane_of_outputs()
 // A wavefront's 16-bit outputs, 64 columns of them: calls map(row block, column block, g, v) for its outputs four at a
 // time, of row lane % 32 and columns 8 g + 4 (lane / 32) ... + 3 of the block, rounds them, and calls out(row, column,
 // w) for 8 of a row as 16 bytes, through the wavefront's part of the LDS: eight neighbouring lanes then hold a row's 128
-// bytes, a whole cache line.  (dz of 8192 x 131072 logits, 1024 features, 2440 us; straight from the accumulators, 32
-// bytes of a row at a time, 2990.)
+// bytes, a whole cache line.  (dz of 8192 x 131072 logits, 1024 features, not turned, 2440 us; straight from the
+// accumulators, 32 bytes of a row at a time, 2990.)
 template <typename T, int WR, int WC, typename Map, typename Out>
 __device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, Map map, Out out)
 {
@@ -237,8 +237,8 @@ __device__ __forceinline__ void for_rows16(char *mine, const Acc<WR, WC> &acc, M
 }
 
 // The pitch of rows of `cols` 16-bit elements: an odd number of 256 bytes, so that the rows of a tile start on
-// different channels of the memory.  (4096 rows, 30% of them padded, 40943 x 512 fp16: dz 177 us, so 172; the
-// products 271 and 261.)
+// different channels of the memory.  (4096 rows, 30% of them padded, 40943 x 512 fp16, between events: dz 173 us, so
+// 168; the products 258 and 255.)
 inline int64_t odd_pitch(int64_t cols)
 {
     const int64_t lines = (cols + 127) / 128;

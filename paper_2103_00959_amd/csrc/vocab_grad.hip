@@ -83,8 +83,9 @@ __device__ __forceinline__ void store_packed(T *__restrict__ row, int c, int wid
 
 // Both products of a piece, each workgroup's tiles of dX's sums (rows by k, a slice of the piece's columns each),
 // then its tiles of dW (vocabulary by k, over the live rows): workgroups that have no tile of the first begin with
-// the second.  Bound by the matrix cores: 8192 rows, vocabulary 131072, 1024 features 3810 us in four pieces (1.15
-// PFLOP/s; library products of these sizes 1.17); 2867 rows, 40943 x 512, 252 us (0.95): tiles do not come out even.
+// the second.  Bound by the matrix cores: 8192 rows, vocabulary 131072, 1024 features 3750 us in four pieces (1.17
+// PFLOP/s; library products of these sizes 1.19); 2867 rows, 40943 x 512, 235 to 250 us (0.96 to 1.02): tiles do not come
+// out even.
 template <typename T, int WAVES, int TM, int TN, int SRCB>
 __global__ __launch_bounds__(WAVES * kWave, 2) void k_vocab_products(VocabArgs a)
 {
@@ -291,8 +292,9 @@ VocabKernel pick_products(bool wide, bool direct)
 
 int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return (rows + tile - 1) / tile * ((cols + tile - 1) / tile); }
 
-// The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).  With 256 MB, 512 and 1024:
-// 8192 rows, vocabulary 131072, 1024 features 8440, 8420 and 8305 us; 4096 rows, 65536 x 768, 1800, 1727 and 1719.
+// The columns of a piece: its dz takes at most so many bytes (and 256 columns at least).  With 256 MB, 512 and 1024,
+// loss and gradients: 8192 rows, vocabulary 131072, 1024 features 8000, 7900 and 7900 us; 4096 rows, 65536 x 768, 1730,
+// 1623 and 1625.
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 // Parts of the rows that dW of a piece is summed in: many rows and few classes make few tiles, each a sum over all
