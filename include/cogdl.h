@@ -589,7 +589,7 @@ cogdl_status cogdl_linear_cross_entropy(int64_t n, int32_t V, int32_t k, const v
  *   dX = dz W (n x k of dtype),  dW = dz^T X (V x k of dtype),  db[v] = sum_i dz[i, v] (V fp32)
  * The logits are computed again, for a piece of the vocabulary at a time; the
  * products take dz rounded to dtype (each by at most half a step, after a
- * factor for the whole call has brought the largest dloss to 2^15; fp16 keeps
+ * factor for the whole call has brought the largest finite dloss to 2^15; fp16 keeps
  * what is above 2^-39 of the largest), db sums it unrounded.  dX, dW and db may
  * each be NULL (not computed).  Rows left out get dX = 0 and enter no sum.  fp32
  * accumulation in a fixed order.  workspace as above, of the size that

@@ -13,6 +13,14 @@ constexpr int kBlock = 256;
 
 __device__ __forceinline__ bool counts(int32_t t, int32_t V) { return (uint32_t)t < (uint32_t)V; }
 
+// |g T| for the call's factor: a weight that is not finite makes its own row NaN or infinite under any, and has no part
+// in what the others' is.
+__device__ __forceinline__ float finite_weight(float dloss, float T)
+{
+    const float w = fabsf(dloss * T);
+    return w < INFINITY ? w : 0.f;
+}
+
 // 8 features from column 8 v on of a row of k, zeros behind its end.
 template <typename T>
 __device__ __forceinline__ uint4 load_vec8(const T *__restrict__ row, int v, int k)
@@ -101,7 +109,7 @@ __global__ __launch_bounds__(kBlock) void k_count_rows(VocabArgs a, int per)
     for (int64_t i = from + threadIdx.x; i < to; i += kBlock) {
         if (!counts(live[i], limit)) continue;
         ++count;
-        if (BACKWARD) top = fmaxf(top, fabsf(a.dloss[i] * a.T));
+        if (BACKWARD) top = fmaxf(top, finite_weight(a.dloss[i], a.T));
     }
     count = wave_inclusive_scan(count);
     top = group_reduce(top, kWave, [](float x, float y) { return fmaxf(x, y); });
@@ -156,7 +164,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
 #pragma unroll
     for (int w = 0; w < W; ++w) at += wsum[w];
     if (BACKWARD && blockIdx.x == 0) {
-        // The largest |g T| that counts, for a factor that brings it to 2^15: fp16 then keeps what it can of the small
+        // The largest finite |g T| that counts, for a factor that brings it to 2^15: fp16 then keeps what it can of the small
         // ones, and of rows that weigh the same, as in a mean, a target's dz, near -g T, lies just under a power of
         // two, where a rounding takes least of it (256 rows of 1433 answers, bf16: the gradients are, with a
         // power of two for the factor, 0.0020 to 0.0031, so 0.0019; rounded once they are 0.0017).
@@ -172,7 +180,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
                 g[u] = i < a.n && counts(live[i], limit) ? a.dloss[i] : 0.f;
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) top = fmaxf(top, fabsf(g[u] * a.T));
+            for (int u = 0; u < 8; ++u) top = fmaxf(top, finite_weight(g[u], a.T));
         }
         top = group_reduce(top, kWave, [](float x, float y) { return fmaxf(x, y); });
         if (lane == 0) wmax[wave] = top;
@@ -180,7 +188,6 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(VocabArgs a, int per)
         if (threadIdx.x == 0) {
 #pragma unroll
             for (int w = 0; w < W; ++w) top = fmaxf(top, wmax[w]);
-            if (!(top <= 3.4e38f)) top = 32768.f;          // (an infinite one makes NaN by itself)
             top = fmaxf(top, 0x1p-100f);
             a.head->scale = 32768.f / top;
             a.head->unscale = top / 32768.f;

@@ -34,7 +34,7 @@ constexpr int64_t kManyRows = 16384;
 // Header of a workspace, written by k_vocab_rows.
 struct RowsHead {
     int32_t live;                // rows that count
-    float scale, unscale;        // |g T| scale <= 2^15 for every live row, and 1 / scale
+    float scale, unscale;        // |g T| scale <= 2^15 for every live row where it is finite, and 1 / scale
     int32_t slices;              // of dX's sums over a piece
 };
 

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_entries(VocabArgs a)
             }
             if (db) {
                 const float w = ldexpf(mine * g, a.unit_bits);
-                // (past that only where the term is noted as odd, or beside a weight that is infinite: then all of db is)
+                // (2^61 at most where it is finite; else the term is noted as odd)
                 if (fabsf(w) < 9e18f) atomicAdd(&a.db_q[v], (unsigned long long)(long long)rintf(w));
             }
         }

@@ -38,3 +38,28 @@ def test_small_weights_in_fp16(which, x, w, distill):
     assert float((value[rows].abs() > 4 * bound[rows]).double().mean()) > 0.9
     for name in ("dX", "dW", "db"):
         ex.close(name, out[name], *want[name])
+
+
+@pytest.mark.parametrize("n", [150, 20_000])
+@pytest.mark.parametrize("wrong", [float("inf"), -float("inf"), float("nan")])
+def test_small_weights_beside_one_that_is_not_finite(wrong, n):
+    """dX of the other rows is what it is without that row."""
+    g = torch.Generator().manual_seed(7)
+    V, k = 300, 48
+    X = (torch.randn((n, k), generator=g) * 2.0 ** -11).half()
+    W = (torch.randn((V, k), generator=g) * 2.0 ** 11 * k ** -0.5).half()
+    weights = (torch.rand(n, generator=g) + 1) * 2.0 ** -27
+    t = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    held = t[:, None] >= 0
+    want, bound = (v[torch.arange(n) != 5] for v in ex.gradients(X, W, t[:, None], held.double(), held, held[:, 0], weights)["dX"])
+    weights[5] = wrong
+    d = [v.cuda() for v in (X, W, t)]
+    loss, lse = cg.linear_cross_entropy(*d)
+    dX = cg.linear_cross_entropy_backward(weights.cuda(), *d, loss, lse)["dX"].cpu()
+    assert not torch.isfinite(dX[5]).any()
+    ex.close("dX", dX[torch.arange(n) != 5], want, bound)
+    one = torch.ones((n, 1))
+    loss, lse, logp = cg.linear_distill(d[0], d[1], d[2][:, None].contiguous(), one.cuda())
+    dX = cg.linear_distill_backward(weights.cuda(), d[0], d[1], d[2][:, None].contiguous(), one.cuda(), lse, logp)["dX"].cpu()
+    assert not torch.isfinite(dX[5]).any()
+    ex.close("dX", dX[torch.arange(n) != 5], want, bound)
