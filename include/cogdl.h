@@ -530,8 +530,8 @@ cogdl_status cogdl_grouped_linear_backward(int64_t n, int32_t E, int32_t k, int3
  *   Y[i] = scale * table[index[i]]
  * table: V x k of dtype; index: n int32; Y: n x k of y_dtype; dtypes fp32, bf16
  * or fp16, the product formed in fp32.  An index outside [0, V) stands for a
- * padded place and gives a row of zeros.  n up to COGDL_MAX_NNZ, k up to 2^22
- * (COGDL_ERR_TOO_LARGE past these), V >= 1.
+ * padded place and gives a row of zeros.  n up to COGDL_MAX_NNZ, k up to 2^22,
+ * V from 1 to 2^31 - 2 (COGDL_ERR_TOO_LARGE past these).
  * ---------------------------------------------------------------------- */
 cogdl_status cogdl_embedding(int64_t n, int32_t V, int32_t k, const void *table, cogdl_dtype dtype,
                              const int32_t *index, float scale, void *Y, cogdl_dtype y_dtype,
